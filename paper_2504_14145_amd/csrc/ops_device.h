@@ -1,0 +1,214 @@
+// ops_device.h -- what the stage operators' kernels share: element types, vector
+// accesses, activations, dropout draws and the epilogue of the matrix products.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "dip_ops.h"
+
+namespace dipops {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <class T>
+struct Vec8;
+template <>
+struct Vec8<__bf16> {
+  typedef bf16x8 type;
+};
+template <>
+struct Vec8<_Float16> {
+  typedef f16x8 type;
+};
+
+// D[i][j] += sum_k a[i][k] b[j][k], 16 x 16 x 32: lane l holds row l % 16 and
+// k = 8 (l / 16) .. + 7 of either operand, and D's column l % 16, rows
+// 4 (l / 16) .. + 3.
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight consecutive elements.  `vec`: their address is a multiple of 16 bytes
+// (wave-uniform by construction: it is a property of the array's base and
+// stride); else, or with fewer than 8 columns left, element by element.
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int left, bool vec, float (&v)[8]) {
+  if (vec && left >= 8) {
+    if constexpr (sizeof(T) == 2) {
+      const typename Vec8<T>::type t = *reinterpret_cast<const typename Vec8<T>::type *>(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = float(t[i]);
+    } else {
+      const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? float(p[i]) : 0.f;
+  }
+}
+template <class T>
+__device__ __forceinline__ void store8(T *p, int left, bool vec, const float (&v)[8]) {
+  if (vec && left >= 8) {
+    if constexpr (sizeof(T) == 2) {
+      typename Vec8<T>::type t;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = T(v[i]);
+      *reinterpret_cast<typename Vec8<T>::type *>(p) = t;
+    } else {
+      f32x4 a, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = v[i], b[i] = v[4 + i];
+      reinterpret_cast<f32x4 *>(p)[0] = a;
+      reinterpret_cast<f32x4 *>(p)[1] = b;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = T(v[i]);
+  }
+}
+
+// ------------------------------------------------------------ activations
+
+// 1 / (1 + exp(-z)) with the hardware's exponential and reciprocal: within 1e-6
+// of the value for the z at which an output of it is not rounded to 0 or 1.
+__device__ __forceinline__ float logistic(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+}
+
+constexpr float kGeluA = 0.7978845608028654f;   // sqrt(2 / pi)
+constexpr float kGeluC = 0.044715f;
+
+__device__ __forceinline__ float act_of(float z, int act) {
+  switch (act) {
+    case DIP_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+    case DIP_ACT_SILU: return z * logistic(z);
+    case DIP_ACT_GELU: return z * logistic(2.f * kGeluA * z * (1.f + kGeluC * z * z));
+    default: return z;
+  }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+  switch (act) {
+    case DIP_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    case DIP_ACT_SILU: {
+      const float e = logistic(z);
+      return e * (1.f + z * (1.f - e));
+    }
+    case DIP_ACT_GELU: {
+      if (fabsf(z) > 12.f) return z > 0.f ? 1.f : 0.f;   // e is 0 or 1 there, z^2 may overflow
+      const float e = logistic(2.f * kGeluA * z * (1.f + kGeluC * z * z));
+      return e * (1.f + z * (1.f - e) * 2.f * kGeluA * (1.f + 3.f * kGeluC * z * z));
+    }
+    default: return 1.f;
+  }
+}
+
+// ------------------------------------------------------------ dropout
+
+struct Drop {
+  uint32_t k0, k1, c2, c3, row0, drop_of;
+  float scale;
+};
+
+inline Drop make_drop(const dip_dropout &d) {
+  return Drop{uint32_t(d.seed), uint32_t(d.seed >> 32), uint32_t(d.offset),
+              uint32_t(d.offset >> 32), d.row0, d.drop_of,
+              65536.f / float(65536u - d.drop_of)};
+}
+
+// The 128 bits of one counter: 16 bits for each of eight consecutive columns.
+__device__ __forceinline__ uint4 draws(const Drop &d, uint32_t block, uint32_t row) {
+  uint32_t c0 = block, c1 = d.row0 + row, c2 = d.c2, c3 = d.c3, k0 = d.k0, k1 = d.k1;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = uint64_t(0xD2511F53u) * c0, p1 = uint64_t(0xCD9E8D57u) * c2;
+    c0 = uint32_t(p1 >> 32) ^ c1 ^ k0;
+    c1 = uint32_t(p1);
+    c2 = uint32_t(p0 >> 32) ^ c3 ^ k1;
+    c3 = uint32_t(p0);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return make_uint4(c0, c1, c2, c3);
+}
+
+// Drops and scales columns 8 block .. + 7 of a row.  Dropped values are set to
+// zero, not multiplied by it, so an infinity or NaN under the mask is gone.
+__device__ __forceinline__ void drop8(const Drop &d, uint32_t block, uint32_t row, float (&v)[8]) {
+  const uint4 r = draws(d, block, row);
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t u = (i & 1) ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+    v[i] = u >= d.drop_of ? v[i] * d.scale : 0.f;
+  }
+}
+
+// ------------------------------------------------------------ epilogues
+
+// What follows a matrix product: out = residual + D(act(acc + bias)), or with
+// no bias, activation or mask an output of either type, added to or not.
+struct Epilogue {
+  const void *bias, *residual;
+  void *out, *pre;
+  int64_t ldr, ldo, ldp;
+  Drop drop;
+  int32_t act;
+  uint8_t vec_bias, vec_res, vec_out, vec_pre;   // 16-byte aligned rows
+  uint8_t out_f32, accumulate;
+};
+
+// Eight consecutive columns of one row; `left`: columns up to the matrix's end.
+template <class T>
+__device__ __forceinline__ void finish8(const Epilogue &e, int64_t row, int64_t col, int left,
+                                        float (&v)[8]) {
+  if (e.bias) {
+    float b[8];
+    load8(static_cast<const T *>(e.bias) + col, left, e.vec_bias, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += b[i];
+  }
+  if (e.pre) store8(static_cast<T *>(e.pre) + row * e.ldp + col, left, e.vec_pre, v);
+  if (e.act != DIP_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = act_of(v[i], e.act);
+  }
+  if (e.drop.drop_of) drop8(e.drop, uint32_t(col >> 3), uint32_t(row), v);
+  if (e.residual) {
+    float r[8];
+    load8(static_cast<const T *>(e.residual) + row * e.ldr + col, left, e.vec_res, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+  }
+  if (e.out_f32) {
+    float *o = static_cast<float *>(e.out) + row * e.ldo + col;
+    if (e.accumulate) {
+      float r[8];
+      load8(o, left, e.vec_out, r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    store8(o, left, e.vec_out, v);
+  } else {
+    T *o = static_cast<T *>(e.out) + row * e.ldo + col;
+    if (e.accumulate) {
+      float r[8];
+      load8(o, left, e.vec_out, r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    store8(o, left, e.vec_out, v);
+  }
+}
+
+}  // namespace dipops

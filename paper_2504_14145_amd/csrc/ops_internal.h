@@ -1,0 +1,60 @@
+// ops_internal.h -- launches of the stage operators' kernels, called by
+// host_ops.hip after it has checked the arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "ops_device.h"
+
+namespace dipops {
+
+// One operand of a matrix product: element (i, k), i the output's row or
+// column, k the contraction, at p[i * ld + k], or with k_rows at p[k * ld + i].
+struct Operand {
+  const void *p;
+  int64_t ld;
+  bool k_rows;
+};
+
+// out[m][n] = epilogue(sum_k a(m, k) b(n, k))
+hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
+                       const Operand &b, const Epilogue &e, hipStream_t stream);
+
+// g = D(dy) act'(pre) to out (ld a multiple of 8, padding columns zero; null:
+// not wanted), and its column sums before rounding to partial[row_chunks][n]
+// (null: not wanted).
+struct GradIn {
+  int64_t m, n;
+  const void *dy, *pre;
+  int64_t ldy, ldp;
+  Drop drop;
+  int32_t act;
+  uint8_t vec_dy, vec_pre;
+  void *out;
+  int64_t ldo;
+  float *partial;
+  int32_t row_chunks;
+};
+int32_t grad_row_chunks(int64_t m, int64_t n);
+hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream);
+// out[c] (+)= sum over the rows of partial[rows][cols], in row order
+hipError_t launch_sum_rows(const float *partial, int64_t rows, int64_t cols, void *out,
+                           int out_dtype, int accumulate, hipStream_t stream);
+
+hipError_t launch_dropout_add(int dtype, int64_t m, int64_t n, const void *x, int64_t ldx,
+                              const void *residual, int64_t ldr, const Drop &drop, void *y,
+                              int64_t ldy, hipStream_t stream);
+
+hipError_t launch_group_norm(const dip_group_norm_args &a, hipStream_t stream);
+hipError_t launch_group_norm_grad(const dip_group_norm_grad_args &a, hipStream_t stream);
+int64_t group_norm_workspace(const dip_group_norm_args &a);
+int64_t group_norm_grad_workspace(const dip_group_norm_grad_args &a);
+
+inline bool aligned16(const void *p, int64_t ld, int elem) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * elem % 16 == 0;
+}
+inline int64_t up16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+}  // namespace dipops
