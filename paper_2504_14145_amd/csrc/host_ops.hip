@@ -17,7 +17,7 @@ bool known_type(int32_t t) { return t == DIP_F32 || t == DIP_F16 || t == DIP_BF1
 bool known_act(int32_t a) { return a >= DIP_ACT_NONE && a <= DIP_ACT_GELU; }
 
 constexpr int64_t kMaxRows = int64_t(1) << 31;     // rows of an array
-constexpr int64_t kMaxCols = int64_t(1) << 24;     // columns and strides of a matrix
+constexpr int64_t kMaxCols = int64_t(1) << 22;     // columns and strides of a matrix: 256 rows of 2-byte elements stay below 2^31 bytes
 
 int hip_code(hipError_t e) {
   if (e == hipSuccess) return DIP_OK;
@@ -97,29 +97,81 @@ int check_linear_grad(const dip_linear_grad_args *a) {
   return check_vector(a->db, ge);
 }
 
-// g needs an array of its own where it is not dy itself
-bool own_g(const dip_linear_grad_args *a) {
-  return (a->dx || a->dw) && (a->act != DIP_ACT_NONE || a->drop.drop_of);
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Whether the products can read an array where it is: aligned rows, and along a
+// contraction that ends inside 16 bytes the zeros that only a copy has.
+bool direct(const void *p, int64_t ld, int64_t cols, bool contracted) {
+  return aligned16(p, ld, 2) && !(contracted && cols % 8);
+}
+
+// The workspace: arrays one after another, 16-byte aligned.
+struct Space {
+  int64_t total = 0;
+  int64_t take(int64_t bytes) {
+    const int64_t at = total;
+    total += up16(bytes);
+    return at;
+  }
+};
+
+struct LinearPlan {
+  GemmPlan gemm;
+  int64_t x_at = -1, w_at = -1, partial_at = 0, total = 0;   // -1: read in place
+};
+LinearPlan plan_linear(const dip_linear_args *a) {
+  LinearPlan p;
+  if (a->m == 0 || a->n == 0) return p;
+  Space s;
+  p.gemm = plan_gemm(a->m, a->n, a->k);
+  if (!direct(a->x, a->ldx, a->k, true)) p.x_at = s.take(a->m * up8(a->k) * 2);
+  if (!direct(a->w, a->ldw, a->k, true)) p.w_at = s.take(a->n * up8(a->k) * 2);
+  p.partial_at = s.take(p.gemm.bytes);
+  p.total = s.total;
+  return p;
 }
 
 struct GradPlan {
-  int64_t g_ld = 0, g_at = 0, partial_at = 0, total = 0;
+  GemmPlan dx, dw;
+  int64_t g_at = -1, x_at = -1, w_at = -1, sums_at = -1, partial_at = 0, total = 0;
   int32_t chunks = 0;
 };
 GradPlan plan_grad(const dip_linear_grad_args *a) {
   GradPlan p;
   if (a->m == 0 || a->n == 0) return p;
-  if (own_g(a)) {
-    p.g_ld = (a->n + 7) / 8 * 8;
-    p.g_at = p.total;
-    p.total += up16(a->m * p.g_ld * 2);
-  }
+  Space s;
+  // g needs an array of its own where it is not dy itself or dy cannot be read
+  // in place
+  if ((a->dx || a->dw) &&
+      (a->act != DIP_ACT_NONE || a->drop.drop_of || !direct(a->dy, a->ldy, a->n, a->dx != nullptr)))
+    p.g_at = s.take(a->m * up8(a->n) * 2);
   if (a->db) {
     p.chunks = grad_row_chunks(a->m, a->n);
-    p.partial_at = p.total;
-    p.total += up16(int64_t(p.chunks) * a->n * 4);
+    p.sums_at = s.take(int64_t(p.chunks) * a->n * 4);
   }
+  int64_t partial = 0;
+  if (a->dx && a->k > 0) {
+    if (!direct(a->w, a->ldw, a->k, false)) p.w_at = s.take(a->n * up8(a->k) * 2);
+    p.dx = plan_gemm(a->m, a->k, a->n);
+    partial = p.dx.bytes;
+  }
+  if (a->dw && a->k > 0) {
+    if (!direct(a->x, a->ldx, a->k, false)) p.x_at = s.take(a->m * up8(a->k) * 2);
+    p.dw = plan_gemm(a->n, a->k, a->m);
+    partial = partial > p.dw.bytes ? partial : p.dw.bytes;
+  }
+  p.partial_at = s.take(partial);   // the two products run one after the other
+  p.total = s.total;
   return p;
+}
+
+// An operand of a product: in place, or its copy made first.
+int place(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld, bool k_rows, char *ws,
+          int64_t at, hipStream_t st, Operand *out) {
+  *out = Operand{p, ld, k_rows};
+  if (at < 0 || rows == 0 || cols == 0) return DIP_OK;
+  *out = Operand{ws + at, up8(cols), k_rows};
+  return hip_code(launch_pack(dtype, p, rows, cols, ld, ws + at, out->ld, st));
 }
 
 int check_norm(int64_t b, int64_t s, int64_t c, int32_t groups, int32_t dtype, int32_t act) {
@@ -174,12 +226,19 @@ extern "C" {
 
 int64_t dip_linear_workspace(const dip_linear_args *a) {
   OPS_CHECK(check_linear(a));
-  return 0;
+  return plan_linear(a).total;
 }
 
 int dip_linear(const dip_linear_args *a, void *stream) {
   OPS_CHECK(check_linear(a));
+  const LinearPlan p = plan_linear(a);
+  OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
   if (a->m == 0 || a->n == 0) return DIP_OK;
+  const hipStream_t st = hipStream_t(stream);
+  char *ws = static_cast<char *>(a->workspace);
+  Operand x, w;
+  OPS_CHECK(place(a->dtype, a->x, a->m, a->k, a->ldx, false, ws, p.x_at, st, &x));
+  OPS_CHECK(place(a->dtype, a->w, a->n, a->k, a->ldw, false, ws, p.w_at, st, &w));
   Epilogue e{};
   e.bias = a->bias;
   e.residual = a->residual;
@@ -194,8 +253,8 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   e.vec_res = aligned16(a->residual, a->ldr, 2);
   e.vec_out = aligned16(a->y, a->ldy, 2);
   e.vec_pre = aligned16(a->pre, a->ldp, 2);
-  return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, Operand{a->x, a->ldx, false},
-                              Operand{a->w, a->ldw, false}, e, hipStream_t(stream)));
+  return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm,
+                              reinterpret_cast<float *>(ws + p.partial_at), st));
 }
 
 int64_t dip_linear_grad_workspace(const dip_linear_grad_args *a) {
@@ -211,7 +270,8 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
   char *ws = static_cast<char *>(a->workspace);
   const void *g = a->dy;
   int64_t ldg = a->ldy;
-  if (p.total > 0) {
+  float *partial = reinterpret_cast<float *>(ws + p.partial_at);
+  if (p.g_at >= 0 || p.sums_at >= 0) {
     GradIn gi{};
     gi.m = a->m;
     gi.n = a->n;
@@ -223,24 +283,26 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     gi.act = a->act;
     gi.vec_dy = aligned16(a->dy, a->ldy, 2);
     gi.vec_pre = aligned16(a->pre, a->ldp, 2);
-    if (p.g_ld) {
+    if (p.g_at >= 0) {
       g = gi.out = ws + p.g_at;
-      ldg = gi.ldo = p.g_ld;
+      ldg = gi.ldo = up8(a->n);
     }
     gi.row_chunks = p.chunks ? p.chunks : grad_row_chunks(a->m, a->n);
-    gi.partial = a->db ? reinterpret_cast<float *>(ws + p.partial_at) : nullptr;
+    gi.partial = a->db ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr;
     OPS_CHECK(hip_code(launch_grad_in(a->dtype, gi, st)));
   }
   if (a->db && a->n > 0 && !(a->m == 0 && a->accumulate))
-    OPS_CHECK(hip_code(launch_sum_rows(reinterpret_cast<const float *>(ws + p.partial_at),
+    OPS_CHECK(hip_code(launch_sum_rows(reinterpret_cast<const float *>(ws + p.sums_at),
                                        p.chunks, a->n, a->db, a->grad_dtype, a->accumulate, st)));
   if (a->dx && a->m > 0 && a->k > 0) {
     Epilogue e{};
     e.out = a->dx;
     e.ldo = a->lddx;
     e.vec_out = aligned16(a->dx, a->lddx, 2);
-    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false},
-                                   Operand{a->w, a->ldw, true}, e, st)));
+    Operand w;
+    OPS_CHECK(place(a->dtype, a->w, a->n, a->k, a->ldw, true, ws, p.w_at, st, &w));
+    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
+                                   partial, st)));
   }
   if (a->dw && a->n > 0 && a->k > 0) {
     Epilogue e{};
@@ -249,8 +311,10 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     e.out_f32 = a->grad_dtype == DIP_F32;
     e.accumulate = a->accumulate != 0;
     e.vec_out = aligned16(a->dw, a->lddw, elem_bytes(a->grad_dtype));
-    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true},
-                                   Operand{a->x, a->ldx, true}, e, st)));
+    Operand x;
+    OPS_CHECK(place(a->dtype, a->x, a->m, a->k, a->ldx, true, ws, p.x_at, st, &x));
+    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,
+                                   partial, st)));
   }
   return DIP_OK;
 }

@@ -1,76 +1,352 @@
 // kern_linear.hip -- matrix products of the stage operators.
+#include <algorithm>
+
 #include "ops_internal.h"
 
 namespace dipops {
 namespace {
 
-constexpr int kTile = 64, kStep = 32, kPad = 40, kThreads = 256;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) s16x8 lds_s16x8;
 
-// out tile 64 x 64, four waves of 32 x 32; operands go to LDS element by element
-// as [row][k], whatever their layout, zeros beyond their ends.  The product is
-// taken transposed (the weight's rows as the matrix instruction's rows), and
-// the tile goes through LDS so that a lane finishes eight columns of a row.
-template <class T>
-__global__ __launch_bounds__(kThreads) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
-                                                        Operand b, Epilogue e) {
-  typedef typename Vec8<T>::type V;
-  __shared__ __align__(16) T sa[kTile][kPad], sb[kTile][kPad];
-  __shared__ float sc[kTile][kTile + 1];
-  const int64_t tiles_n = (n + kTile - 1) / kTile;
-  const int64_t m0 = int64_t(blockIdx.x) / tiles_n * kTile;
-  const int64_t n0 = int64_t(blockIdx.x) % tiles_n * kTile;
-  const int t = threadIdx.x, lane = t % 64, wave = t / 64;
-  const int wm = wave / 2 * 32, wn = wave % 2 * 32;
-  f32x4 acc[2][2] = {};
-  auto stage = [&](T(&s)[kTile][kPad], const Operand &o, int64_t i0, int64_t rows, int64_t k0) {
-    for (int j = t; j < kTile * kStep; j += kThreads) {
-      const int r = o.k_rows ? j % kTile : j / kStep, c = o.k_rows ? j / kTile : j % kStep;
-      const int64_t i = i0 + r, kk = k0 + c;
-      T v = T(0.f);
-      if (i < rows && kk < k) v = static_cast<const T *>(o.p)[o.k_rows ? kk * o.ld + i : i * o.ld + kk];
-      s[r][c] = v;
-    }
-  };
-  for (int64_t k0 = 0; k0 < k; k0 += kStep) {
-    stage(sa, a, m0, m, k0);
-    stage(sb, b, n0, n, k0);
-    __syncthreads();
-    for (int i = 0; i < 2; ++i)
-      for (int j = 0; j < 2; ++j) {
-        const V x = *reinterpret_cast<const V *>(&sa[wm + 16 * i + lane % 16][lane / 16 * 8]);
-        const V w = *reinterpret_cast<const V *>(&sb[wn + 16 * j + lane % 16][lane / 16 * 8]);
-        acc[i][j] = mfma16(w, x, acc[i][j]);
+constexpr int kStep = 64;                  // contraction elements a staged tile
+constexpr uint32_t kOutside = 0x80000000u; // a buffer offset that reads zeros
+
+// A descriptor of `bytes` bytes from p: loads beyond them return zeros.
+__device__ __forceinline__ i32x4 descriptor(const void *p, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  i32x4 d;
+  d[0] = int(uint32_t(a));
+  d[1] = int(uint32_t(a >> 32) & 0xffffu);
+  d[2] = int(bytes);
+  d[3] = 0x00020000;
+  return d;
+}
+
+// 16 bytes a lane from the buffer straight to LDS, at lds + 16 lane.  Written
+// out, because for the builtin the compiler waits for all of them before any
+// LDS read that follows; the waits below are this file's own.  No register
+// receives the data, and the offset is read when the instruction issues.
+__device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t lds, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds), "v"(offset), "s"(d)
+               : "memory");
+}
+
+// One operand's share of a workgroup: ROWS output rows (or columns) times
+// kStep contraction elements a step, THREADS threads.
+//
+// K_ROWS false: the array is [i][k].  LDS holds 128 bytes a row i, the 16-byte
+// chunk of k = 8 c .. at slot c ^ ((i >> 1) & 7), so that the 16 rows a matrix
+// instruction reads at one c spread over all banks.
+// K_ROWS true: the array is [k][i].  LDS holds 2 ROWS bytes a row k, 64-byte
+// pieces of a row exchanged by k & 3, and the transposing LDS read gives a lane
+// four consecutive k of its column.
+template <bool K_ROWS, int ROWS, int THREADS>
+struct Stage {
+  static constexpr int kLoads = ROWS * kStep * 2 / 16 / THREADS;
+  static constexpr int kBytes = ROWS * kStep * 2;
+  static_assert(kLoads >= 1 && ROWS * kStep * 2 % (16 * THREADS) == 0);
+  const unsigned char *base;   // of the current step
+  uint32_t voff[kLoads];
+  uint32_t k_at;               // K_ROWS: first k row of the thread; else its first k in the step
+  uint32_t valid_rows, row_bytes, end;   // rows inside the array, bytes a row, columns' bytes
+
+  __device__ void init(const Operand &o, int64_t i0, int64_t rows, int64_t k0, int t) {
+    row_bytes = uint32_t(o.ld) * 2;
+    valid_rows = uint32_t(min(int64_t(ROWS), rows - i0));
+    if constexpr (!K_ROWS) {
+      base = static_cast<const unsigned char *>(o.p) + (i0 * o.ld + k0) * 2;
+      const uint32_t row = t / 8, chunk = (t % 8) ^ ((row >> 1) & 7);
+      k_at = chunk * 8;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const uint32_t r = row + i * (THREADS / 8);
+        voff[i] = r < valid_rows ? r * row_bytes + chunk * 16 : kOutside;
       }
-    __syncthreads();
+    } else {
+      base = static_cast<const unsigned char *>(o.p) + (k0 * o.ld + i0) * 2;
+      constexpr int per_row = ROWS * 2 / 16;
+      const uint32_t kr = t / per_row, slot = (t % per_row) ^ ((kr & 3) << 2);
+      k_at = kr;
+      static_assert(THREADS / per_row % 4 == 0);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        voff[i] = slot * 8 < valid_rows ? (kr + i * (THREADS / per_row)) * row_bytes + slot * 16 : kOutside;
+    }
   }
-  for (int i = 0; i < 2; ++i)
-    for (int j = 0; j < 2; ++j)
-      for (int q = 0; q < 4; ++q)
-        sc[wm + 16 * i + lane % 16][wn + 16 * j + lane / 16 * 4 + q] = acc[i][j][q];
-  __syncthreads();
-  for (int j = t; j < kTile * kTile / 8; j += kThreads) {
-    const int r = j / (kTile / 8), c = j % (kTile / 8) * 8;
-    if (m0 + r >= m || n0 + c >= n) continue;
-    float v[8];
-    for (int q = 0; q < 8; ++q) v[q] = sc[r][c + q];
-    finish8<T>(e, m0 + r, n0 + c, int(min(int64_t(8), n - n0 - c)), v);
+  // Loads the step at `base`, of which k_left contraction elements exist, to
+  // LDS address lds (of the workgroup's tile), and advances.
+  __device__ __forceinline__ void load(uint32_t lds, int64_t k_left, int t) {
+    const uint32_t kl = uint32_t(min(int64_t(kStep), k_left));
+    uint32_t bytes;
+    if constexpr (!K_ROWS)
+      bytes = (valid_rows - 1) * row_bytes + kl * 2;
+    else
+      bytes = (kl - 1) * row_bytes + valid_rows * 2;
+    const i32x4 d = descriptor(base, (bytes + 3) & ~3u);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + (t / 64) * 1024);
+    if (kl == kStep) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load_lds(d, at + i * THREADS * 16, voff[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const uint32_t k = K_ROWS ? k_at + i * (THREADS / (ROWS * 2 / 16)) : k_at;
+        load_lds(d, at + i * THREADS * 16, k < kl ? voff[i] : kOutside);
+      }
+    }
+    base += K_ROWS ? uint64_t(row_bytes) * kStep : uint64_t(kStep) * 2;
+  }
+};
+
+// Reads fragments (16 rows x 32 k) of a wave's rows r0 .. from a staged tile.
+// PAIRED: fragment 2 p + f holds, as its row 4 q + i, row 32 p + 8 q + 4 f + i,
+// so that the two fragments' results give a lane eight consecutive rows.
+template <bool K_ROWS, int ROWS, bool PAIRED, int FRAGS>
+struct Reader {
+  static constexpr int kBases = !K_ROWS ? (PAIRED ? 4 : 2) : (PAIRED ? (FRAGS + 1) / 2 : (FRAGS + 1) / 2);
+  uint32_t at[kBases];
+  __device__ __forceinline__ void init(uint32_t r0, int lane) {
+    const uint32_t l = lane % 16, g = lane / 16;
+    if constexpr (!K_ROWS) {
+#pragma unroll
+      for (int j = 0; j < kBases; ++j) {
+        const uint32_t kk = j & 1, f = j >> 1;
+        const uint32_t row = r0 + (PAIRED ? 8 * (l / 4) + 4 * f + l % 4 : l);
+        at[j] = row * 128 + (((kk * 4 + g) ^ ((row >> 1) & 7)) << 4);
+      }
+    } else {
+      const uint32_t kx = l / 4, q = l % 4, k = 8 * g + kx;
+#pragma unroll
+      for (int j = 0; j < kBases; ++j) {
+        const uint32_t col = r0 + 32 * j + (PAIRED ? 8 * q : 4 * q);
+        at[j] = k * (ROWS * 2) + (((col / 8) ^ (kx << 2)) << 4) + (col % 8) * 2;
+      }
+    }
+  }
+  template <class V>
+  __device__ __forceinline__ V read(uint32_t tile, int frag, int kk) const {
+    if constexpr (!K_ROWS) {
+      const uint32_t a = PAIRED ? at[(frag & 1) * 2 + kk] + (frag >> 1) * 32 * 128 : at[kk] + frag * 16 * 128;
+      const s16x8 v = *reinterpret_cast<lds_s16x8 *>(uintptr_t(tile + a));
+      return __builtin_bit_cast(V, v);
+    } else {
+      const uint32_t a = at[frag >> 1] + (frag & 1) * (PAIRED ? 8 : 32) + kk * 32 * (ROWS * 2);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(uintptr_t(tile + a)));
+      const s16x4 hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(uintptr_t(tile + a + 4 * (ROWS * 2))));
+      return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((lds_byte *)p));
+}
+
+struct Split {
+  float *partial;       // [splits][m][n4], n4 = n rounded up to 8
+  int64_t steps;        // contraction steps a split
+  int64_t n8;
+};
+
+// Tiles in the order in which the eight XCDs, which take workgroups in turn, see
+// each a contiguous run of them, in strips of kGroup tile rows.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm,
+                                        uint32_t &tn) {
+  const uint32_t all = tiles_m * tiles_n, x = id % 8, each = all / 8, rest = all % 8;
+  id = x * each + min(x, rest) + id / 8;
+  constexpr uint32_t kGroup = 4;
+  const uint32_t strip = id / (kGroup * tiles_n), first = strip * kGroup;
+  const uint32_t high = min(kGroup, tiles_m - first), in = id % (kGroup * tiles_n);
+  tm = first + in % high;
+  tn = in / high;
+}
+
+// out tile BM x BN by WM x WN waves.
+template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, bool PARTIAL>
+__global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
+                                                            Operand b, Epilogue e, Split split) {
+  typedef typename Vec8<T>::type V;
+  constexpr int kThreads = 64 * WM * WN;
+  constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  typedef Stage<A_K, BM, kThreads> StageA;
+  typedef Stage<B_K, BN, kThreads> StageB;
+  constexpr int kBuf = StageA::kBytes + StageB::kBytes;
+  __shared__ __align__(1024) unsigned char s[2 * kBuf];
+  const uint32_t lds = lds_address(s);
+  const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64);
+  uint32_t tm, tn;
+  tile_of(blockIdx.x, uint32_t((m + BM - 1) / BM), uint32_t((n + BN - 1) / BN), tm, tn);
+  const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+  int64_t k0 = 0, k1 = k;
+  if constexpr (PARTIAL) {
+    k0 = int64_t(blockIdx.y) * split.steps * kStep;
+    k1 = min(k, k0 + split.steps * kStep);
+  }
+  StageA sa;
+  StageB sb;
+  sa.init(a, m0, m, k0, t);
+  sb.init(b, n0, n, k0, t);
+  const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  Reader<A_K, BM, false, FM> ra;
+  Reader<B_K, BN, true, FN> rb;
+  ra.init(wm, lane);
+  rb.init(wn, lane);
+  f32x4 acc[FM][FN] = {};
+  int64_t left = k1 - k0;
+  uint32_t buf = 0;
+  if (left > 0) {
+    sa.load(lds, left, t);
+    sb.load(lds + StageA::kBytes, left, t);
+  }
+  while (left > 0) {
+    // this step's tile has come in, for every wave; and no wave reads the other
+    // buffer any more
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const uint32_t ta = lds + buf * kBuf, tb = ta + StageA::kBytes;
+    left -= kStep;
+    buf ^= 1;
+    if (left > 0) {
+      sa.load(lds + buf * kBuf, left, t);
+      sb.load(lds + buf * kBuf + StageA::kBytes, left, t);
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      V x[FM], w[FN];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) w[j] = rb.template read<V>(tb, j, kk);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) x[i] = ra.template read<V>(ta, i, kk);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mfma16(w[j], x[i], acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int p = 0; p < FN / 2; ++p) {
+      const int64_t row = m0 + wm + 16 * i + lane % 16;
+      const int64_t col = n0 + wn + 32 * p + 8 * (lane / 16);
+      if (row >= m || col >= n) continue;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = acc[i][2 * p][q], v[4 + q] = acc[i][2 * p + 1][q];
+      if constexpr (PARTIAL)
+        store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, true, v);
+      else
+        finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v);
+    }
+}
+
+// Sums the splits' partial products in their order and finishes.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(int64_t m, int64_t n, Epilogue e, Split split, int splits) {
+  const int64_t per = split.n8 / 8, all = m * per;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= all) return;
+  const int64_t row = i / per, col = i % per * 8;
+  float v[8];
+  load8(split.partial + row * split.n8 + col, 8, true, v);
+  for (int s = 1; s < splits; ++s) {
+    float q[8];
+    load8(split.partial + (int64_t(s) * m + row) * split.n8 + col, 8, true, q);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += q[j];
+  }
+  finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v);
+}
+
+template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN>
+hipError_t run(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const Epilogue &e,
+               const GemmPlan &plan, float *partial, hipStream_t stream) {
+  const int64_t tiles = ((m + BM - 1) / BM) * ((n + BN - 1) / BN);
+  const dim3 block(64 * WM * WN);
+  Split s{partial, plan.steps, (n + 7) / 8 * 8};
+  if (plan.splits <= 1) {
+    gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, false><<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
+    return hipGetLastError();
+  }
+  gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, true>
+      <<<dim3(uint32_t(tiles), uint32_t(plan.splits)), block, 0, stream>>>(m, n, k, a, b, e, s);
+  const hipError_t rc = hipGetLastError();
+  if (rc != hipSuccess) return rc;
+  join_kernel<T><<<dim3(uint32_t((m * (s.n8 / 8) + 255) / 256)), dim3(256), 0, stream>>>(m, n, e, s, plan.splits);
+  return hipGetLastError();
+}
+
+template <class T, bool A_K, bool B_K>
+hipError_t pick(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const Epilogue &e,
+                const GemmPlan &plan, float *partial, hipStream_t stream) {
+  switch (plan.tile) {
+    case 0: return run<T, A_K, B_K, 256, 256, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
+    default: return run<T, A_K, B_K, 128, 128, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
   }
 }
 
+// Copies rows to where the products can take them: 16-byte aligned, the stride
+// a multiple of 8, zeros in the columns up to it.
 template <class T>
-hipError_t run(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
-               const Epilogue &e, hipStream_t stream) {
-  const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
-  gemm_kernel<T><<<dim3(uint32_t(tiles)), dim3(kThreads), 0, stream>>>(m, n, k, a, b, e);
-  return hipGetLastError();
+__global__ __launch_bounds__(256) void pack_kernel(const T *p, int64_t rows, int64_t cols, int64_t ld, T *out,
+                                                   int64_t ldo) {
+  const int64_t per = ldo / 8;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= rows * per) return;
+  const int64_t row = i / per, col = i % per * 8;
+  float v[8];
+  load8(p + row * ld + col, int(max(int64_t(0), min(int64_t(8), cols - col))), false, v);
+  store8(out + row * ldo + col, 8, true, v);
 }
 
 }  // namespace
 
-hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
-                       const Operand &b, const Epilogue &e, hipStream_t stream) {
-  return dtype == DIP_BF16 ? run<__bf16>(m, n, k, a, b, e, stream)
-                           : run<_Float16>(m, n, k, a, b, e, stream);
+GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k) {
+  GemmPlan p;
+  const int64_t steps = (k + kStep - 1) / kStep;
+  const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
+  p.tile = big >= 192 ? 0 : 1;
+  const int64_t tiles = p.tile == 0 ? big : ((m + 127) / 128) * ((n + 127) / 128);
+  const int64_t slots = p.tile == 0 ? 256 : 512;
+  p.splits = 1;
+  if (tiles * 2 <= slots) p.splits = int(std::max<int64_t>(1, std::min<int64_t>(slots / tiles, steps / 4)));
+  p.steps = (steps + p.splits - 1) / p.splits;
+  if (p.steps > 0) p.splits = int((steps + p.steps - 1) / p.steps);
+  p.bytes = p.splits > 1 ? up16(int64_t(p.splits) * m * ((n + 7) / 8 * 8) * 4) : 0;
+  return p;
+}
+
+hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
+                       const Epilogue &e, const GemmPlan &plan, float *partial, hipStream_t stream) {
+  if (dtype == DIP_BF16) {
+    if (!a.k_rows && !b.k_rows) return pick<__bf16, false, false>(m, n, k, a, b, e, plan, partial, stream);
+    if (!a.k_rows) return pick<__bf16, false, true>(m, n, k, a, b, e, plan, partial, stream);
+    return pick<__bf16, true, true>(m, n, k, a, b, e, plan, partial, stream);
+  }
+  if (!a.k_rows && !b.k_rows) return pick<_Float16, false, false>(m, n, k, a, b, e, plan, partial, stream);
+  if (!a.k_rows) return pick<_Float16, false, true>(m, n, k, a, b, e, plan, partial, stream);
+  return pick<_Float16, true, true>(m, n, k, a, b, e, plan, partial, stream);
+}
+
+hipError_t launch_pack(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld, void *out, int64_t ldo,
+                       hipStream_t stream) {
+  const dim3 grid(uint32_t((rows * (ldo / 8) + 255) / 256));
+  if (dtype == DIP_BF16)
+    pack_kernel<<<grid, dim3(256), 0, stream>>>(static_cast<const __bf16 *>(p), rows, cols, ld,
+                                               static_cast<__bf16 *>(out), ldo);
+  else
+    pack_kernel<<<grid, dim3(256), 0, stream>>>(static_cast<const _Float16 *>(p), rows, cols, ld,
+                                               static_cast<_Float16 *>(out), ldo);
+  return hipGetLastError();
 }
 
 }  // namespace dipops

@@ -18,9 +18,22 @@ struct Operand {
   bool k_rows;
 };
 
-// out[m][n] = epilogue(sum_k a(m, k) b(n, k))
+// out[m][n] = epilogue(sum_k a(m, k) b(n, k)).  Operands are 16-byte aligned with
+// strides that are multiples of 8; one whose contraction runs along its rows
+// (k_rows false) has zeros, or k itself, up to the next multiple of 8 of k.
+struct GemmPlan {
+  int32_t tile = 0, splits = 1;
+  int64_t steps = 0;           // contraction steps a split
+  int64_t bytes = 0;           // of partial products
+};
+GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k);
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
-                       const Operand &b, const Epilogue &e, hipStream_t stream);
+                       const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
+                       hipStream_t stream);
+// rows x cols from p to out (16-byte aligned, stride ldo a multiple of 8), zeros
+// in columns cols .. ldo - 1
+hipError_t launch_pack(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld, void *out,
+                       int64_t ldo, hipStream_t stream);
 
 // g = D(dy) act'(pre) to out (ld a multiple of 8, padding columns zero; null:
 // not wanted), and its column sums before rounding to partial[row_chunks][n]
