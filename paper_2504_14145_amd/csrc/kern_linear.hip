@@ -83,24 +83,20 @@ struct Stage {
   // Loads the step at `base`, of which k_left contraction elements exist, to
   // LDS address lds (of the workgroup's tile), and advances.
   __device__ __forceinline__ void load(uint32_t lds, int64_t k_left, int t) {
-    const uint32_t kl = uint32_t(min(int64_t(kStep), k_left));
-    uint32_t bytes;
-    if constexpr (!K_ROWS)
-      bytes = (valid_rows - 1) * row_bytes + kl * 2;
-    else
-      bytes = (kl - 1) * row_bytes + valid_rows * 2;
-    const i32x4 d = descriptor(base, (bytes + 3) & ~3u);
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + (t / 64) * 1024);
-    if (kl == kStep) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) load_lds(d, at + i * THREADS * 16, voff[i]);
-    } else {
+    uint32_t kl = kStep;
+    if (k_left < kStep) {   // the last step: nothing is loaded after it
+      kl = uint32_t(k_left);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const uint32_t k = K_ROWS ? k_at + i * (THREADS / (ROWS * 2 / 16)) : k_at;
-        load_lds(d, at + i * THREADS * 16, k < kl ? voff[i] : kOutside);
+        voff[i] = k < kl ? voff[i] : kOutside;
       }
     }
+    const uint32_t bytes = K_ROWS ? (kl - 1) * row_bytes + valid_rows * 2 : (valid_rows - 1) * row_bytes + kl * 2;
+    const i32x4 d = descriptor(base, (bytes + 3) & ~3u);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + (t / 64) * 1024);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_lds(d, at + i * THREADS * 16, voff[i]);
     base += K_ROWS ? uint64_t(row_bytes) * kStep : uint64_t(kStep) * 2;
   }
 };
@@ -213,6 +209,15 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const uint32_t ta = lds + buf * kBuf, tb = ta + StageA::kBytes;
+    // Steps of one x fragment and FN products.  x is read two steps ahead of its
+    // products, the second half's w during the first half's steps; the schedule is
+    // pinned, since left alone every product waits for its own reads.
+    constexpr int kXReads = A_K ? 2 : 1, kWReads = B_K ? 2 : 1;
+    V w[2][FN], x[4];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) w[0][j] = rb.template read<V>(tb, j, 0);
+    x[0] = ra.template read<V>(ta, 0, 0);
+    x[1] = ra.template read<V>(ta, 1 % FM, 1 / FM);
     left -= kStep;
     buf ^= 1;
     if (left > 0) {
@@ -220,16 +225,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
       sb.load(lds + buf * kBuf + StageA::kBytes, left, t);
     }
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      V x[FM], w[FN];
+    for (int step = 0; step < 2 * FM; ++step) {
+      if (step + 2 < 2 * FM) {
+        x[(step + 2) % 4] = ra.template read<V>(ta, (step + 2) % FM, (step + 2) / FM);
+        __builtin_amdgcn_sched_group_barrier(0x100, kXReads, 0);
+      }
+      if (step < FN && step < FM) {
+        constexpr int per = FN > FM ? FN / FM : 1;
 #pragma unroll
-      for (int j = 0; j < FN; ++j) w[j] = rb.template read<V>(tb, j, kk);
+        for (int j = step * per; j < step * per + per; ++j) w[1][j] = rb.template read<V>(tb, j, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, kWReads * per, 0);
+      }
 #pragma unroll
-      for (int i = 0; i < FM; ++i) x[i] = ra.template read<V>(ta, i, kk);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma16(w[j], x[i], acc[i][j]);
+      for (int j = 0; j < FN; ++j)
+        acc[step % FM][j] = mfma16(w[step / FM][j], x[step % 4], acc[step % FM][j]);
+      __builtin_amdgcn_sched_group_barrier(0x008, FN, 0);
     }
   }
 #pragma unroll
