@@ -1,5 +1,7 @@
 // kern_linear.hip -- matrix products of the stage operators.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "ops_internal.h"
 
@@ -20,9 +22,9 @@ constexpr uint32_t kOutside = 0x80000000u; // a buffer offset that reads zeros
 __device__ __forceinline__ i32x4 descriptor(const void *p, uint32_t bytes) {
   const uint64_t a = reinterpret_cast<uint64_t>(p);
   i32x4 d;
-  d[0] = int(uint32_t(a));
-  d[1] = int(uint32_t(a >> 32) & 0xffffu);
-  d[2] = int(bytes);
+  d[0] = __builtin_amdgcn_readfirstlane(int(uint32_t(a)));
+  d[1] = __builtin_amdgcn_readfirstlane(int(uint32_t(a >> 32) & 0xffffu));
+  d[2] = __builtin_amdgcn_readfirstlane(int(bytes));
   d[3] = 0x00020000;
   return d;
 }
@@ -80,12 +82,13 @@ struct Stage {
         voff[i] = slot * 8 < valid_rows ? (kr + i * (THREADS / per_row)) * row_bytes + slot * 16 : kOutside;
     }
   }
-  // Loads the step at `base`, of which k_left contraction elements exist, to
-  // LDS address lds (of the workgroup's tile), and advances.
-  __device__ __forceinline__ void load(uint32_t lds, int64_t k_left, int t) {
-    uint32_t kl = kStep;
-    if (k_left < kStep) {   // the last step: nothing is loaded after it
-      kl = uint32_t(k_left);
+  // Makes the step at `base` ready to load: to LDS address lds (of the workgroup's
+  // tile), with kl of its contraction elements present (none: all zeros; fewer
+  // than kStep only where no step follows).  Then kLoads calls of load().
+  i32x4 desc;
+  uint32_t to;
+  __device__ __forceinline__ void begin(uint32_t lds, uint32_t kl, uint32_t wave) {
+    if (kl < kStep) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const uint32_t k = K_ROWS ? k_at + i * (THREADS / (ROWS * 2 / 16)) : k_at;
@@ -93,54 +96,69 @@ struct Stage {
       }
     }
     const uint32_t bytes = K_ROWS ? (kl - 1) * row_bytes + valid_rows * 2 : (valid_rows - 1) * row_bytes + kl * 2;
-    const i32x4 d = descriptor(base, (bytes + 3) & ~3u);
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + (t / 64) * 1024);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_lds(d, at + i * THREADS * 16, voff[i]);
+    desc = descriptor(base, kl ? (bytes + 3) & ~3u : 0u);
+    to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
     base += K_ROWS ? uint64_t(row_bytes) * kStep : uint64_t(kStep) * 2;
   }
+  __device__ __forceinline__ void load(int i) const { load_lds(desc, to + i * THREADS * 16, voff[i]); }
 };
 
 // Reads fragments (16 rows x 32 k) of a wave's rows r0 .. from a staged tile.
 // PAIRED: fragment 2 p + f holds, as its row 4 q + i, row 32 p + 8 q + 4 f + i,
 // so that the two fragments' results give a lane eight consecutive rows.
-template <bool K_ROWS, int ROWS, bool PAIRED, int FRAGS>
+// Addresses are a few registers and offsets known at compile time.
+template <class V, bool K_ROWS, int ROWS, bool PAIRED, int FRAGS>
 struct Reader {
-  static constexpr int kBases = !K_ROWS ? (PAIRED ? 4 : 2) : (PAIRED ? (FRAGS + 1) / 2 : (FRAGS + 1) / 2);
+  static constexpr int kBases = !K_ROWS ? (PAIRED ? 4 : 2) : (FRAGS + 1) / 2;
   uint32_t at[kBases];
-  __device__ __forceinline__ void init(uint32_t r0, int lane) {
+  __device__ __forceinline__ void init(uint32_t lds, uint32_t r0, int lane) {
     const uint32_t l = lane % 16, g = lane / 16;
     if constexpr (!K_ROWS) {
 #pragma unroll
       for (int j = 0; j < kBases; ++j) {
         const uint32_t kk = j & 1, f = j >> 1;
         const uint32_t row = r0 + (PAIRED ? 8 * (l / 4) + 4 * f + l % 4 : l);
-        at[j] = row * 128 + (((kk * 4 + g) ^ ((row >> 1) & 7)) << 4);
+        at[j] = lds + row * 128 + (((kk * 4 + g) ^ ((row >> 1) & 7)) << 4);
       }
     } else {
       const uint32_t kx = l / 4, q = l % 4, k = 8 * g + kx;
 #pragma unroll
       for (int j = 0; j < kBases; ++j) {
         const uint32_t col = r0 + 32 * j + (PAIRED ? 8 * q : 4 * q);
-        at[j] = k * (ROWS * 2) + (((col / 8) ^ (kx << 2)) << 4) + (col % 8) * 2;
+        at[j] = lds + k * (ROWS * 2) + (((col / 8) ^ (kx << 2)) << 4) + (col % 8) * 2;
       }
     }
   }
-  template <class V>
-  __device__ __forceinline__ V read(uint32_t tile, int frag, int kk) const {
+  // the tile in the other of two buffers `by` bytes apart
+  __device__ __forceinline__ void move(uint32_t by) {
+#pragma unroll
+    for (int j = 0; j < kBases; ++j) at[j] += by;
+  }
+  __device__ __forceinline__ V read(int frag, int kk) const {
     if constexpr (!K_ROWS) {
-      const uint32_t a = PAIRED ? at[(frag & 1) * 2 + kk] + (frag >> 1) * 32 * 128 : at[kk] + frag * 16 * 128;
-      const s16x8 v = *reinterpret_cast<lds_s16x8 *>(uintptr_t(tile + a));
-      return __builtin_bit_cast(V, v);
+      const uint32_t base = PAIRED ? at[(frag & 1) * 2 + kk] : at[kk];
+      const uint32_t off = (PAIRED ? (frag >> 1) * 32 * 128 : frag * 16 * 128);
+      return __builtin_bit_cast(V, *reinterpret_cast<lds_s16x8 *>(uintptr_t(base + off)));
     } else {
-      const uint32_t a = at[frag >> 1] + (frag & 1) * (PAIRED ? 8 : 32) + kk * 32 * (ROWS * 2);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(uintptr_t(tile + a)));
-      const s16x4 hi =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(uintptr_t(tile + a + 4 * (ROWS * 2))));
+      const uint32_t off = (frag & 1) * (PAIRED ? 8 : 32) + kk * 32 * (ROWS * 2);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<lds_s16x4 *>(uintptr_t(at[frag >> 1] + off)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<lds_s16x4 *>(uintptr_t(at[frag >> 1] + off + 4 * (ROWS * 2))));
       return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
 };
+
+// f(0) .. f(N - 1), the argument known at compile time.
+template <class F, int... I>
+__device__ __forceinline__ void unrolled_(F &&f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F &&f) {
+  unrolled_(f, std::make_integer_sequence<int, N>{});
+}
 
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
   return uint32_t(reinterpret_cast<uintptr_t>((lds_byte *)p));
@@ -191,72 +209,128 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   sa.init(a, m0, m, k0, t);
   sb.init(b, n0, n, k0, t);
   const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-  Reader<A_K, BM, false, FM> ra;
-  Reader<B_K, BN, true, FN> rb;
-  ra.init(wm, lane);
-  rb.init(wn, lane);
-  f32x4 acc[FM][FN] = {};
-  int64_t left = k1 - k0;
-  uint32_t buf = 0;
-  if (left > 0) {
-    sa.load(lds, left, t);
-    sb.load(lds + StageA::kBytes, left, t);
-  }
-  while (left > 0) {
-    // this step's tile has come in, for every wave; and no wave reads the other
-    // buffer any more
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    const uint32_t ta = lds + buf * kBuf, tb = ta + StageA::kBytes;
-    // Steps of one x fragment and FN products.  x is read two steps ahead of its
-    // products, the second half's w during the first half's steps; the schedule is
-    // pinned, since left alone every product waits for its own reads.
-    constexpr int kXReads = A_K ? 2 : 1, kWReads = B_K ? 2 : 1;
-    V w[2][FN], x[4];
-#pragma unroll
-    for (int j = 0; j < FN; ++j) w[0][j] = rb.template read<V>(tb, j, 0);
-    x[0] = ra.template read<V>(ta, 0, 0);
-    x[1] = ra.template read<V>(ta, 1 % FM, 1 / FM);
-    left -= kStep;
-    buf ^= 1;
-    if (left > 0) {
-      sa.load(lds + buf * kBuf, left, t);
-      sb.load(lds + buf * kBuf + StageA::kBytes, left, t);
-    }
-#pragma unroll
-    for (int step = 0; step < 2 * FM; ++step) {
-      if (step + 2 < 2 * FM) {
-        x[(step + 2) % 4] = ra.template read<V>(ta, (step + 2) % FM, (step + 2) / FM);
-        __builtin_amdgcn_sched_group_barrier(0x100, kXReads, 0);
-      }
-      if (step < FN && step < FM) {
-        constexpr int per = FN > FM ? FN / FM : 1;
-#pragma unroll
-        for (int j = step * per; j < step * per + per; ++j) w[1][j] = rb.template read<V>(tb, j, 1);
-        __builtin_amdgcn_sched_group_barrier(0x100, kWReads * per, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-        acc[step % FM][j] = mfma16(w[step / FM][j], x[step % 4], acc[step % FM][j]);
-      __builtin_amdgcn_sched_group_barrier(0x008, FN, 0);
-    }
-  }
+  const uint32_t lds_a = lds, lds_b = lds + 2 * StageA::kBytes;   // two buffers each
+  Reader<V, A_K, BM, false, FM> ra;
+  Reader<V, B_K, BN, true, FN> rb;
+  ra.init(lds_a, wm, lane);
+  rb.init(lds_b, wn, lane);
+  f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // A staged tile is NS steps of one x fragment and FN products.  x is read L
+  // steps ahead of its products, w half a tile ahead, across tiles: L steps
+  // before a tile's end nothing of it is left to read, so its buffer is filled
+  // again from there, a tile and L steps ahead, and the next one's first
+  // fragments are read.  Nothing but that point waits.  With few waves a SIMD a
+  // product covers the issue of three other instructions, so the reads and loads
+  // of a step are dealt out between its products.
+  constexpr int NS = 2 * FM, L = FM / 2 > 1 ? FM / 2 : 1, X = 2 * L;
+  constexpr int kLoads = StageA::kLoads + StageB::kLoads;
+  // The loads of a tile are spread over the D steps that follow: all at once
+  // they would fill the address queue and hold up the products behind them.
+  constexpr int D = NS * 5 / 8 > L ? NS * 5 / 8 : L;
+  constexpr int kWay = (FN + L - 1) / L, kDma = (kLoads + D - 1) / D;
+  constexpr int kFirst = kDma * L < kLoads ? kDma * L : kLoads;   // those before the tile's end
+  static_assert(NS % X == 0);
+  V w[2][FN], x[X];
+  // steps to take, and the contraction elements of the last one
+  int left = __builtin_amdgcn_readfirstlane(int((k1 - k0 + kStep - 1) / kStep));
+  const uint32_t last = uint32_t(k1 - k0 - int64_t(left - 1) * kStep);
+  auto present = [&](int steps) { return steps > 1 ? uint32_t(kStep) : steps == 1 ? last : 0u; };
+  auto load = [&](auto j_) __attribute__((always_inline)) {
+    constexpr int j = decltype(j_)::value;
+    if constexpr (j < StageA::kLoads) sa.load(j);
+    else sb.load(j - StageA::kLoads);
+  };
+  if (left > 0) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      sa.begin(lds_a + p * StageA::kBytes, present(left - p), wave);
+      sb.begin(lds_b + p * StageB::kBytes, present(left - p), wave);
+      if (p == 0) unrolled<kLoads>(load);
+      else unrolled<kFirst>(load);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kFirst) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < FN; ++j) w[0][j] = rb.read(j, 0);
+#pragma unroll
+    for (int j = 0; j < L; ++j) x[j] = ra.read(j, 0);
+  }
+  uint32_t now = 0, to_next_a = StageA::kBytes, to_next_b = StageB::kBytes;   // buffer, and where the other is
+  for (; left > 0; --left) {
+    unrolled<NS>([&](auto s_) __attribute__((always_inline)) {
+      constexpr int s = decltype(s_)::value, r = s - (NS - L);
+      constexpr bool ahead = r >= 0;
+      if constexpr (r == 0) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        sa.begin(lds_a + now * StageA::kBytes, present(left - 2), wave);
+        sb.begin(lds_b + now * StageB::kBytes, present(left - 2), wave);
+        ra.move(to_next_a);
+        rb.move(to_next_b);
+        to_next_a = -to_next_a;
+        to_next_b = -to_next_b;
+        now ^= 1;
+      }
+      // the step's other work: one x fragment, w fragments, loads
+      constexpr int q = (r + NS) % NS, n_w = s < L || ahead ? kWay : 0, others = 1 + n_w + (q < D ? kDma : 0);
+      unrolled<FN>([&](auto j_) __attribute__((always_inline)) {
+        constexpr int j = decltype(j_)::value, o0 = j * others / FN, o1 = (j + 1) * others / FN;
+        unrolled<o1 - o0>([&](auto o_) __attribute__((always_inline)) {
+          constexpr int o = o0 + decltype(o_)::value;
+          if constexpr (o == 0) {
+            x[(s + L) % X] = ra.read((s + L) % FM, (s + L) % NS / FM);
+          } else if constexpr (o <= n_w) {
+            constexpr int at = (ahead ? r : s) * kWay + o - 1;
+            if constexpr (at < FN) w[ahead ? 0 : 1][at] = rb.read(at, ahead ? 0 : 1);
+          } else {
+            constexpr int at = q * kDma + o - 1 - n_w;
+            if constexpr (at < kLoads) load(std::integral_constant<int, at>{});
+          }
+        });
+        mfma16(w[s / FM][j], x[s % X], acc[s % FM][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+  }
+  // the loads after the last tile write zeros to LDS: they end before the wave
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  products_wait();
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int p = 0; p < FN / 2; ++p) products_done(acc[i][2 * p], acc[i][2 * p + 1]);
+  // One copy of the epilogue, looped over the rows of fragments: the loop picks
+  // its fragments by uniform branches, since registers have no index.
+#pragma unroll 1
+  for (int i = 0; i < FM; ++i) {
+    f32x4 c[FN];
+    unrolled<FM>([&](auto i_) __attribute__((always_inline)) {
+      if (i == decltype(i_)::value) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) c[j] = acc[decltype(i_)::value][j];
+      }
+    });
+    const int64_t row = m0 + wm + 16 * i + lane % 16;
+    if (row >= m) continue;
+#pragma unroll
     for (int p = 0; p < FN / 2; ++p) {
-      const int64_t row = m0 + wm + 16 * i + lane % 16;
       const int64_t col = n0 + wn + 32 * p + 8 * (lane / 16);
-      if (row >= m || col >= n) continue;
+      if (col >= n) continue;
       float v[8];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = acc[i][2 * p][q], v[4 + q] = acc[i][2 * p + 1][q];
+      for (int q = 0; q < 4; ++q) v[q] = c[2 * p][q], v[4 + q] = c[2 * p + 1][q];
       if constexpr (PARTIAL)
         store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, true, v);
       else
         finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v);
     }
+  }
 }
 
 // Sums the splits' partial products in their order and finishes.
@@ -299,7 +373,7 @@ template <class T, bool A_K, bool B_K>
 hipError_t pick(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const Epilogue &e,
                 const GemmPlan &plan, float *partial, hipStream_t stream) {
   switch (plan.tile) {
-    case 0: return run<T, A_K, B_K, 256, 256, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
+    case 0: return run<T, A_K, B_K, 256, 256, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
     default: return run<T, A_K, B_K, 128, 128, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
   }
 }
