@@ -230,7 +230,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   constexpr int kLoads = StageA::kLoads + StageB::kLoads;
   // The loads of a tile are spread over the D steps that follow: all at once
   // they would fill the address queue and hold up the products behind them.
-  constexpr int D = NS * 5 / 8 > L ? NS * 5 / 8 : L;
+  constexpr int D = NS * 7 / 8 > L ? NS * 7 / 8 : L;
   constexpr int kWay = (FN + L - 1) / L, kDma = (kLoads + D - 1) / D;
   constexpr int kFirst = kDma * L < kLoads ? kDma * L : kLoads;   // those before the tile's end
   static_assert(NS % X == 0);
