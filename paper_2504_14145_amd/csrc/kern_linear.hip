@@ -40,12 +40,19 @@ __device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t lds, uint32_t 
                : "memory");
 }
 
+// Where a row's 16-byte chunks sit in LDS when the contraction runs along rows:
+// 128 bytes a row, chunk c at slot c ^ spread(row).  The LDS serves a 16-byte read
+// sixteen lanes at a time, eight rows at c and eight others at c ^ 1 (lanes 0-3,
+// 12-15 of one sixteen with 4-11 of the next): with this those fall on all banks,
+// for sixteen rows in a row and for the pairs of fragments below.
+__device__ __forceinline__ uint32_t spread(uint32_t row) {
+  return (row >> 1 & 1) | ((row >> 2 ^ row >> 4) & 1) << 1 | (row >> 3 & 1) << 2;
+}
+
 // One operand's share of a workgroup: ROWS output rows (or columns) times
 // kStep contraction elements a step, THREADS threads.
 //
-// K_ROWS false: the array is [i][k].  LDS holds 128 bytes a row i, the 16-byte
-// chunk of k = 8 c .. at slot c ^ ((i >> 1) & 7), so that the 16 rows a matrix
-// instruction reads at one c spread over all banks.
+// K_ROWS false: the array is [i][k].  LDS holds 128 bytes a row i, spread as above.
 // K_ROWS true: the array is [k][i].  LDS holds 2 ROWS bytes a row k, 64-byte
 // pieces of a row exchanged by k & 3, and the transposing LDS read gives a lane
 // four consecutive k of its column.
@@ -64,7 +71,7 @@ struct Stage {
     valid_rows = uint32_t(min(int64_t(ROWS), rows - i0));
     if constexpr (!K_ROWS) {
       base = static_cast<const unsigned char *>(o.p) + (i0 * o.ld + k0) * 2;
-      const uint32_t row = t / 8, chunk = (t % 8) ^ ((row >> 1) & 7);
+      const uint32_t row = t / 8, chunk = (t % 8) ^ spread(row);
       k_at = chunk * 8;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
@@ -109,7 +116,7 @@ struct Stage {
 // Addresses are a few registers and offsets known at compile time.
 template <class V, bool K_ROWS, int ROWS, bool PAIRED, int FRAGS>
 struct Reader {
-  static constexpr int kBases = !K_ROWS ? (PAIRED ? 4 : 2) : (FRAGS + 1) / 2;
+  static constexpr int kBases = !K_ROWS ? 4 : (FRAGS + 1) / 2;
   uint32_t at[kBases];
   __device__ __forceinline__ void init(uint32_t lds, uint32_t r0, int lane) {
     const uint32_t l = lane % 16, g = lane / 16;
@@ -117,8 +124,8 @@ struct Reader {
 #pragma unroll
       for (int j = 0; j < kBases; ++j) {
         const uint32_t kk = j & 1, f = j >> 1;
-        const uint32_t row = r0 + (PAIRED ? 8 * (l / 4) + 4 * f + l % 4 : l);
-        at[j] = lds + row * 128 + (((kk * 4 + g) ^ ((row >> 1) & 7)) << 4);
+        const uint32_t row = r0 + (PAIRED ? 8 * (l / 4) + 4 * f + l % 4 : 16 * f + l);
+        at[j] = lds + row * 128 + (((kk * 4 + g) ^ spread(row)) << 4);
       }
     } else {
       const uint32_t kx = l / 4, q = l % 4, k = 8 * g + kx;
@@ -136,9 +143,8 @@ struct Reader {
   }
   __device__ __forceinline__ V read(int frag, int kk) const {
     if constexpr (!K_ROWS) {
-      const uint32_t base = PAIRED ? at[(frag & 1) * 2 + kk] : at[kk];
-      const uint32_t off = (PAIRED ? (frag >> 1) * 32 * 128 : frag * 16 * 128);
-      return __builtin_bit_cast(V, *reinterpret_cast<lds_s16x8 *>(uintptr_t(base + off)));
+      return __builtin_bit_cast(
+          V, *reinterpret_cast<lds_s16x8 *>(uintptr_t(at[(frag & 1) * 2 + kk] + (frag >> 1) * 32 * 128)));
     } else {
       const uint32_t off = (frag & 1) * (PAIRED ? 8 : 32) + kk * 32 * (ROWS * 2);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
