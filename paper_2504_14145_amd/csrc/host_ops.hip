@@ -253,6 +253,7 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   e.vec_res = aligned16(a->residual, a->ldr, 2);
   e.vec_out = aligned16(a->y, a->ldy, 2);
   e.vec_pre = aligned16(a->pre, a->ldp, 2);
+  e.fast = e.vec_bias && (!a->residual || e.vec_res) && e.vec_out && (!a->pre || e.vec_pre);
   return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm,
                               reinterpret_cast<float *>(ws + p.partial_at), st));
 }
@@ -298,7 +299,7 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     Epilogue e{};
     e.out = a->dx;
     e.ldo = a->lddx;
-    e.vec_out = aligned16(a->dx, a->lddx, 2);
+    e.vec_out = e.fast = aligned16(a->dx, a->lddx, 2);
     Operand w;
     OPS_CHECK(place(a->dtype, a->w, a->n, a->k, a->ldw, true, ws, p.w_at, st, &w));
     OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
@@ -311,6 +312,7 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     e.out_f32 = a->grad_dtype == DIP_F32;
     e.accumulate = a->accumulate != 0;
     e.vec_out = aligned16(a->dw, a->lddw, elem_bytes(a->grad_dtype));
+    e.fast = e.vec_out && !e.out_f32 && !e.accumulate;
     Operand x;
     OPS_CHECK(place(a->dtype, a->x, a->m, a->k, a->ldx, true, ws, p.x_at, st, &x));
     OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,

@@ -29,15 +29,17 @@ __device__ __forceinline__ i32x4 descriptor(const void *p, uint32_t bytes) {
   return d;
 }
 
-// 16 bytes a lane from the buffer straight to LDS, at lds + 16 lane.  Written
-// out, because for the builtin the compiler waits for all of them before any
-// LDS read that follows; the waits below are this file's own.  No register
+// 16 bytes a lane from the buffer straight to LDS: lds_at(to, OFF), then, after
+// at least one other instruction, load_lds(d, offset) loads to to + OFF + 16 lane.
+// Written out, because for the builtin the compiler waits for all loads before
+// any LDS read that follows; the waits below are this file's own.  No register
 // receives the data, and the offset is read when the instruction issues.
-__device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t lds, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :
-               : "s"(lds), "v"(offset), "s"(d)
-               : "memory");
+template <int OFF>
+__device__ __forceinline__ void lds_at(uint32_t to) {
+  asm volatile("s_add_u32 m0, %0, %1" : : "s"(to), "n"(OFF) : "scc", "memory");
+}
+__device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t offset) {
+  asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(d) : "memory");
 }
 
 // Where a row's 16-byte chunks sit in LDS when the contraction runs along rows:
@@ -61,14 +63,17 @@ struct Stage {
   static constexpr int kLoads = ROWS * kStep * 2 / 16 / THREADS;
   static constexpr int kBytes = ROWS * kStep * 2;
   static_assert(kLoads >= 1 && ROWS * kStep * 2 % (16 * THREADS) == 0);
-  const unsigned char *base;   // of the current step
+  const unsigned char *base;   // of the next step to load
   uint32_t voff[kLoads];
   uint32_t k_at;               // K_ROWS: first k row of the thread; else its first k in the step
-  uint32_t valid_rows, row_bytes, end;   // rows inside the array, bytes a row, columns' bytes
+  uint32_t valid_rows, row_bytes;   // rows inside the array, bytes a row
+  i32x4 desc;
+  uint32_t to;                 // LDS address of the wave's first load
 
   __device__ void init(const Operand &o, int64_t i0, int64_t rows, int64_t k0, int t) {
     row_bytes = uint32_t(o.ld) * 2;
     valid_rows = uint32_t(min(int64_t(ROWS), rows - i0));
+    desc = descriptor(o.p, bytes(kStep));
     if constexpr (!K_ROWS) {
       base = static_cast<const unsigned char *>(o.p) + (i0 * o.ld + k0) * 2;
       const uint32_t row = t / 8, chunk = (t % 8) ^ spread(row);
@@ -89,11 +94,14 @@ struct Stage {
         voff[i] = slot * 8 < valid_rows ? (kr + i * (THREADS / per_row)) * row_bytes + slot * 16 : kOutside;
     }
   }
+  // from `base` to the end of a step of which kl contraction elements exist
+  __device__ __forceinline__ uint32_t bytes(uint32_t kl) const {
+    const uint32_t b = K_ROWS ? (kl - 1) * row_bytes + valid_rows * 2 : (valid_rows - 1) * row_bytes + kl * 2;
+    return kl ? (b + 3) & ~3u : 0u;
+  }
   // Makes the step at `base` ready to load: to LDS address lds (of the workgroup's
   // tile), with kl of its contraction elements present (none: all zeros; fewer
-  // than kStep only where no step follows).  Then kLoads calls of load().
-  i32x4 desc;
-  uint32_t to;
+  // than kStep only where no step follows).
   __device__ __forceinline__ void begin(uint32_t lds, uint32_t kl, uint32_t wave) {
     if (kl < kStep) {
 #pragma unroll
@@ -101,13 +109,21 @@ struct Stage {
         const uint32_t k = K_ROWS ? k_at + i * (THREADS / (ROWS * 2 / 16)) : k_at;
         voff[i] = k < kl ? voff[i] : kOutside;
       }
+      desc[2] = __builtin_amdgcn_readfirstlane(int(bytes(kl)));
     }
-    const uint32_t bytes = K_ROWS ? (kl - 1) * row_bytes + valid_rows * 2 : (valid_rows - 1) * row_bytes + kl * 2;
-    desc = descriptor(base, kl ? (bytes + 3) & ~3u : 0u);
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    desc[0] = __builtin_amdgcn_readfirstlane(int(uint32_t(at)));
+    desc[1] = __builtin_amdgcn_readfirstlane(int(uint32_t(at >> 32)));
     to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
     base += K_ROWS ? uint64_t(row_bytes) * kStep : uint64_t(kStep) * 2;
   }
-  __device__ __forceinline__ void load(int i) const { load_lds(desc, to + i * THREADS * 16, voff[i]); }
+  // Whether load i brings what the last L steps before a tile read of it: the
+  // first 32 k, and of a row operand read by fragment (x) its waves' first rows.
+  template <bool BY_FRAGMENT>
+  static constexpr bool early(int i, int wave_rows, int l) {
+    if (K_ROWS) return i < kLoads / 2;
+    return !BY_FRAGMENT || i * (THREADS / 8) % wave_rows < 16 * l;
+  }
 };
 
 // Reads fragments (16 rows x 32 k) of a wave's rows r0 .. from a staged tile.
@@ -161,6 +177,13 @@ template <class F, int... I>
 __device__ __forceinline__ void unrolled_(F &&f, std::integer_sequence<int, I...>) {
   (f(std::integral_constant<int, I>{}), ...);
 }
+template <int P, class F>
+__device__ __forceinline__ void each(F &&f) {
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) f(p, q);
+}
 template <int N, class F>
 __device__ __forceinline__ void unrolled(F &&f) {
   unrolled_(f, std::make_integer_sequence<int, N>{});
@@ -169,6 +192,29 @@ __device__ __forceinline__ void unrolled(F &&f) {
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
   return uint32_t(reinterpret_cast<uintptr_t>((lds_byte *)p));
 }
+
+// The order of a tile's loads: first those that its first fragments need.
+template <class A, class B, int WAVE_ROWS, int L>
+struct LoadOrder {
+  static constexpr int kLoads = A::kLoads + B::kLoads;
+  static constexpr bool early(int i) {
+    return i < B::kLoads ? B::template early<false>(i, 1, L) : A::template early<true>(i - B::kLoads, WAVE_ROWS, L);
+  }
+  static constexpr int count(bool e) {
+    int n = 0;
+    for (int i = 0; i < kLoads; ++i) n += early(i) == e;
+    return n;
+  }
+  static constexpr int kLate = count(false);
+  static constexpr int nth(int j) {   // b's loads, then a's
+    for (int e = 1; e >= 0; --e)
+      for (int i = 0; i < kLoads; ++i)
+        if (early(i) == bool(e) && j-- == 0) return i;
+    return 0;
+  }
+  static constexpr bool of_a(int j) { return nth(j) >= B::kLoads; }
+  static constexpr int index(int j) { return of_a(j) ? nth(j) - B::kLoads : nth(j); }
+};
 
 struct Split {
   float *partial;       // [splits][m][n4], n4 = n rounded up to 8
@@ -189,8 +235,11 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
   tn = in / high;
 }
 
+// what a workgroup does with its tile
+constexpr int kForward = 0, kGradient = 1, kPartial = 2;
+
 // out tile BM x BN by WM x WN waves.
-template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, bool PARTIAL>
+template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int KIND>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
                                                             Operand b, Epilogue e, Split split) {
   typedef typename Vec8<T>::type V;
@@ -206,7 +255,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   tile_of(blockIdx.x, uint32_t((m + BM - 1) / BM), uint32_t((n + BN - 1) / BN), tm, tn);
   const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
   int64_t k0 = 0, k1 = k;
-  if constexpr (PARTIAL) {
+  if constexpr (KIND == kPartial) {
     k0 = int64_t(blockIdx.y) * split.steps * kStep;
     k1 = min(k, k0 + split.steps * kStep);
   }
@@ -233,31 +282,39 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   // product covers the issue of three other instructions, so the reads and loads
   // of a step are dealt out between its products.
   constexpr int NS = 2 * FM, L = FM / 2 > 1 ? FM / 2 : 1, X = 2 * L;
-  constexpr int kLoads = StageA::kLoads + StageB::kLoads;
-  // The loads of a tile are spread over the D steps that follow: all at once
-  // they would fill the address queue and hold up the products behind them.
-  constexpr int D = NS * 7 / 8 > L ? NS * 7 / 8 : L;
-  constexpr int kWay = (FN + L - 1) / L, kDma = (kLoads + D - 1) / D;
-  constexpr int kFirst = kDma * L < kLoads ? kDma * L : kLoads;   // those before the tile's end
+  // The loads of a tile are spread over D steps: all at once they would fill the
+  // address queue and hold up the products behind them.  Those that the tile's
+  // first fragments need come first, and the others may arrive L steps later.
+  typedef LoadOrder<StageA, StageB, BM / WM, L> Order;
+  constexpr int kLoads = Order::kLoads, kLate = Order::kLate, D = NS * 3 / 4;
+  constexpr int kFirst = L * kLoads / D;                  // loads before the tile's end
+  constexpr int kWay = (FN + L - 1) / L;
   static_assert(NS % X == 0);
   V w[2][FN], x[X];
   // steps to take, and the contraction elements of the last one
   int left = __builtin_amdgcn_readfirstlane(int((k1 - k0 + kStep - 1) / kStep));
   const uint32_t last = uint32_t(k1 - k0 - int64_t(left - 1) * kStep);
   auto present = [&](int steps) { return steps > 1 ? uint32_t(kStep) : steps == 1 ? last : 0u; };
+  auto aim = [&](auto j_) __attribute__((always_inline)) {
+    constexpr int j = decltype(j_)::value, i = Order::index(j);
+    lds_at<i * kThreads * 16>(Order::of_a(j) ? sa.to : sb.to);
+  };
   auto load = [&](auto j_) __attribute__((always_inline)) {
-    constexpr int j = decltype(j_)::value;
-    if constexpr (j < StageA::kLoads) sa.load(j);
-    else sb.load(j - StageA::kLoads);
+    constexpr int j = decltype(j_)::value, i = Order::index(j);
+    if constexpr (Order::of_a(j)) load_lds(sa.desc, sa.voff[i]);
+    else load_lds(sb.desc, sb.voff[i]);
   };
   if (left > 0) {
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    unrolled<2>([&](auto p_) __attribute__((always_inline)) {
+      constexpr int p = decltype(p_)::value;
       sa.begin(lds_a + p * StageA::kBytes, present(left - p), wave);
       sb.begin(lds_b + p * StageB::kBytes, present(left - p), wave);
-      if (p == 0) unrolled<kLoads>(load);
-      else unrolled<kFirst>(load);
-    }
+      unrolled<p == 0 ? kLoads : kFirst>([&](auto j_) __attribute__((always_inline)) {
+        aim(j_);
+        asm volatile("s_nop 0");
+        load(j_);
+      });
+    });
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kFirst) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -271,8 +328,15 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
     unrolled<NS>([&](auto s_) __attribute__((always_inline)) {
       constexpr int s = decltype(s_)::value, r = s - (NS - L);
       constexpr bool ahead = r >= 0;
+      if constexpr (s == 0 && kLate > 0) {
+        // the rest of this tile
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kFirst) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
       if constexpr (r == 0) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // the first part of the next tile; and every wave has read this one
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLate) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         sa.begin(lds_a + now * StageA::kBytes, present(left - 2), wave);
@@ -284,7 +348,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
         now ^= 1;
       }
       // the step's other work: one x fragment, w fragments, loads
-      constexpr int q = (r + NS) % NS, n_w = s < L || ahead ? kWay : 0, others = 1 + n_w + (q < D ? kDma : 0);
+      constexpr int q = (r + NS) % NS, d0 = q < D ? q * kLoads / D : 0, d1 = q < D ? (q + 1) * kLoads / D : 0;
+      constexpr int n_w = s < L || ahead ? kWay : 0, others = 1 + n_w + d1 - d0;
       unrolled<FN>([&](auto j_) __attribute__((always_inline)) {
         constexpr int j = decltype(j_)::value, o0 = j * others / FN, o1 = (j + 1) * others / FN;
         unrolled<o1 - o0>([&](auto o_) __attribute__((always_inline)) {
@@ -295,11 +360,15 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
             constexpr int at = (ahead ? r : s) * kWay + o - 1;
             if constexpr (at < FN) w[ahead ? 0 : 1][at] = rb.read(at, ahead ? 0 : 1);
           } else {
-            constexpr int at = q * kDma + o - 1 - n_w;
-            if constexpr (at < kLoads) load(std::integral_constant<int, at>{});
+            aim(std::integral_constant<int, d0 + o - 1 - n_w>{});
+            if constexpr (o + 1 < o1) {   // the product lies between the last one's halves
+              asm volatile("s_nop 0");
+              load(std::integral_constant<int, d0 + o - 1 - n_w>{});
+            }
           }
         });
         mfma16(w[s / FM][j], x[s % X], acc[s % FM][j]);
+        if constexpr (o1 > o0 && o1 - 1 > n_w) load(std::integral_constant<int, d0 + o1 - 2 - n_w>{});
         __builtin_amdgcn_sched_barrier(0);
       });
     });
@@ -312,29 +381,65 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
     for (int p = 0; p < FN / 2; ++p) products_done(acc[i][2 * p], acc[i][2 * p + 1]);
   // One copy of the epilogue, looped over the rows of fragments: the loop picks
-  // its fragments by uniform branches, since registers have no index.
+  // its fragments by uniform branches, since registers have no index.  A wave
+  // whose part lies inside aligned arrays takes a row at a time through straight
+  // code; the others go eight columns by eight.
+  constexpr int P = FN / 2;
+  const int64_t col0 = n0 + wn + 8 * (lane / 16);
+  const bool whole = e.fast && m0 + wm + 16 * FM <= m && n0 + wn + 16 * FN <= n;
+  V bias[P];
+  if (KIND == kForward && whole && e.bias) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) bias[p] = reinterpret_cast<const V *>(static_cast<const T *>(e.bias) + col0)[4 * p];
+  }
 #pragma unroll 1
   for (int i = 0; i < FM; ++i) {
-    f32x4 c[FN];
+    float v[P][8];
     unrolled<FM>([&](auto i_) __attribute__((always_inline)) {
       if (i == decltype(i_)::value) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) c[j] = acc[decltype(i_)::value][j];
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[p][q] = acc[decltype(i_)::value][2 * p + q / 4][q % 4];
       }
     });
     const int64_t row = m0 + wm + 16 * i + lane % 16;
-    if (row >= m) continue;
+    if (KIND != kPartial && whole) {
+      if constexpr (KIND == kForward) {
+        if (e.bias) each<P>([&](int p, int q) { v[p][q] += float(bias[p][q]); });
+        if (e.pre) {
+          V *o = reinterpret_cast<V *>(static_cast<T *>(e.pre) + row * e.ldp + col0);
 #pragma unroll
-    for (int p = 0; p < FN / 2; ++p) {
-      const int64_t col = n0 + wn + 32 * p + 8 * (lane / 16);
-      if (col >= n) continue;
-      float v[8];
+          for (int p = 0; p < P; ++p) o[4 * p] = round8<T>(v[p]);
+        }
+        if (e.act == DIP_ACT_SILU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_SILU); });
+        else if (e.act == DIP_ACT_GELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_GELU); });
+        else if (e.act == DIP_ACT_RELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_RELU); });
+        if (e.drop.drop_of) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = c[2 * p][q], v[4 + q] = c[2 * p + 1][q];
-      if constexpr (PARTIAL)
-        store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, true, v);
-      else
-        finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v);
+          for (int p = 0; p < P; ++p) drop8(e.drop, uint32_t(col0 >> 3) + 4 * p, uint32_t(row), v[p]);
+        }
+        if (e.residual) {
+          const V *o = reinterpret_cast<const V *>(static_cast<const T *>(e.residual) + row * e.ldr + col0);
+          V r[P];
+#pragma unroll
+          for (int p = 0; p < P; ++p) r[p] = o[4 * p];
+          each<P>([&](int p, int q) { v[p][q] += float(r[p][q]); });
+        }
+      }
+      V *o = reinterpret_cast<V *>(static_cast<T *>(e.out) + row * e.ldo + col0);
+#pragma unroll
+      for (int p = 0; p < P; ++p) o[4 * p] = round8<T>(v[p]);
+    } else if (row < m) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int64_t col = col0 + 32 * p;
+        if (col >= n) continue;
+        if constexpr (KIND == kPartial)
+          store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, true, v[p]);
+        else
+          finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v[p]);
+      }
     }
   }
 }
@@ -364,10 +469,10 @@ hipError_t run(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand 
   const dim3 block(64 * WM * WN);
   Split s{partial, plan.steps, (n + 7) / 8 * 8};
   if (plan.splits <= 1) {
-    gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, false><<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
+    gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, B_K ? kGradient : kForward><<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
     return hipGetLastError();
   }
-  gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, true>
+  gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, kPartial>
       <<<dim3(uint32_t(tiles), uint32_t(plan.splits)), block, 0, stream>>>(m, n, k, a, b, e, s);
   const hipError_t rc = hipGetLastError();
   if (rc != hipSuccess) return rc;

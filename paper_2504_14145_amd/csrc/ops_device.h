@@ -64,13 +64,17 @@ __device__ __forceinline__ void load8(const T *p, int left, bool vec, float (&v)
   }
 }
 template <class T>
+__device__ __forceinline__ typename Vec8<T>::type round8(const float (&v)[8]) {
+  typename Vec8<T>::type t;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = T(v[i]);
+  return t;
+}
+template <class T>
 __device__ __forceinline__ void store8(T *p, int left, bool vec, const float (&v)[8]) {
   if (vec && left >= 8) {
     if constexpr (sizeof(T) == 2) {
-      typename Vec8<T>::type t;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t[i] = T(v[i]);
-      *reinterpret_cast<typename Vec8<T>::type *>(p) = t;
+      *reinterpret_cast<typename Vec8<T>::type *>(p) = round8<T>(v);
     } else {
       f32x4 a, b;
 #pragma unroll
@@ -173,6 +177,7 @@ struct Epilogue {
   int32_t act;
   uint8_t vec_bias, vec_res, vec_out, vec_pre;   // 16-byte aligned rows
   uint8_t out_f32, accumulate;
+  uint8_t fast;   // every array aligned, a plain output of the operands' type
 };
 
 // Eight consecutive columns of one row; `left`: columns up to the matrix's end.
