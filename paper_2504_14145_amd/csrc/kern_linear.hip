@@ -239,7 +239,7 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 constexpr int kForward = 0, kGradient = 1, kPartial = 2;
 
 // out tile BM x BN by WM x WN waves.
-template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int KIND>
+template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R, int KIND>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
                                                             Operand b, Epilogue e, Split split) {
   typedef typename Vec8<T>::type V;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   typedef Stage<A_K, BM, kThreads> StageA;
   typedef Stage<B_K, BN, kThreads> StageB;
   constexpr int kBuf = StageA::kBytes + StageB::kBytes;
-  __shared__ __align__(1024) unsigned char s[2 * kBuf];
+  __shared__ __align__(1024) unsigned char s[R * kBuf];
   const uint32_t lds = lds_address(s);
   const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64);
   uint32_t tm, tn;
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   sa.init(a, m0, m, k0, t);
   sb.init(b, n0, n, k0, t);
   const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-  const uint32_t lds_a = lds, lds_b = lds + 2 * StageA::kBytes;   // two buffers each
+  const uint32_t lds_a = lds, lds_b = lds + R * StageA::kBytes;
   Reader<V, A_K, BM, false, FM> ra;
   Reader<V, B_K, BN, true, FN> rb;
   ra.init(lds_a, wm, lane);
@@ -274,13 +274,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // A staged tile is NS steps of one x fragment and FN products.  x is read L
-  // steps ahead of its products, w half a tile ahead, across tiles: L steps
-  // before a tile's end nothing of it is left to read, so its buffer is filled
-  // again from there, a tile and L steps ahead, and the next one's first
-  // fragments are read.  Nothing but that point waits.  With few waves a SIMD a
-  // product covers the issue of three other instructions, so the reads and loads
-  // of a step are dealt out between its products.
+  // LDS is a ring of R staged tiles.  One is NS steps of one x fragment and FN
+  // products.  x is read L steps ahead of its products, w half a tile ahead,
+  // across tiles: L steps before a tile's end nothing of it is left to read, and
+  // from there its place is filled again, with the tile R further on, and the next
+  // one's first fragments are read.  Nothing but that point waits.  With few waves
+  // a SIMD a product covers the issue of three other instructions, so the reads
+  // and loads of a step are dealt out between its products.
   constexpr int NS = 2 * FM, L = FM / 2 > 1 ? FM / 2 : 1, X = 2 * L;
   // The loads of a tile are spread over D steps: all at once they would fill the
   // address queue and hold up the products behind them.  Those that the tile's
@@ -289,6 +289,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   constexpr int kLoads = Order::kLoads, kLate = Order::kLate, D = NS * 3 / 4;
   constexpr int kFirst = L * kLoads / D;                  // loads before the tile's end
   constexpr int kWay = (FN + L - 1) / L;
+  constexpr bool kSplit = R == 2 && kLate > 0;            // a longer ring has time for all of them
   static_assert(NS % X == 0);
   V w[2][FN], x[X];
   // steps to take, and the contraction elements of the last one
@@ -305,17 +306,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
     else load_lds(sb.desc, sb.voff[i]);
   };
   if (left > 0) {
-    unrolled<2>([&](auto p_) __attribute__((always_inline)) {
+    unrolled<R>([&](auto p_) __attribute__((always_inline)) {
       constexpr int p = decltype(p_)::value;
       sa.begin(lds_a + p * StageA::kBytes, present(left - p), wave);
       sb.begin(lds_b + p * StageB::kBytes, present(left - p), wave);
-      unrolled<p == 0 ? kLoads : kFirst>([&](auto j_) __attribute__((always_inline)) {
+      unrolled<p + 1 < R ? kLoads : kFirst>([&](auto j_) __attribute__((always_inline)) {
         aim(j_);
         asm volatile("s_nop 0");
         load(j_);
       });
     });
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kFirst) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((R - 2) * kLoads + kFirst) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
@@ -323,29 +324,28 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
     for (int j = 0; j < L; ++j) x[j] = ra.read(j, 0);
   }
-  uint32_t now = 0, to_next_a = StageA::kBytes, to_next_b = StageB::kBytes;   // buffer, and where the other is
+  uint32_t now = 0;   // place in the ring
   for (; left > 0; --left) {
     unrolled<NS>([&](auto s_) __attribute__((always_inline)) {
       constexpr int s = decltype(s_)::value, r = s - (NS - L);
       constexpr bool ahead = r >= 0;
-      if constexpr (s == 0 && kLate > 0) {
+      if constexpr (s == 0 && kSplit) {
         // the rest of this tile
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kFirst) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((R - 2) * kLoads + kFirst) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
       if constexpr (r == 0) {
         // the first part of the next tile; and every wave has read this one
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLate) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((R - 2) * kLoads + (kSplit ? kLate : 0)) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        sa.begin(lds_a + now * StageA::kBytes, present(left - 2), wave);
-        sb.begin(lds_b + now * StageB::kBytes, present(left - 2), wave);
-        ra.move(to_next_a);
-        rb.move(to_next_b);
-        to_next_a = -to_next_a;
-        to_next_b = -to_next_b;
-        now ^= 1;
+        sa.begin(lds_a + now * StageA::kBytes, present(left - R), wave);
+        sb.begin(lds_b + now * StageB::kBytes, present(left - R), wave);
+        const uint32_t by = now == R - 1 ? uint32_t(1 - R) : 1u;
+        ra.move(by * StageA::kBytes);
+        rb.move(by * StageB::kBytes);
+        now += by;
       }
       // the step's other work: one x fragment, w fragments, loads
       constexpr int q = (r + NS) % NS, d0 = q < D ? q * kLoads / D : 0, d1 = q < D ? (q + 1) * kLoads / D : 0;
@@ -462,17 +462,17 @@ __global__ __launch_bounds__(256) void join_kernel(int64_t m, int64_t n, Epilogu
   finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v);
 }
 
-template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN>
+template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R>
 hipError_t run(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const Epilogue &e,
                const GemmPlan &plan, float *partial, hipStream_t stream) {
   const int64_t tiles = ((m + BM - 1) / BM) * ((n + BN - 1) / BN);
   const dim3 block(64 * WM * WN);
   Split s{partial, plan.steps, (n + 7) / 8 * 8};
   if (plan.splits <= 1) {
-    gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, B_K ? kGradient : kForward><<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
+    gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, B_K ? kGradient : kForward><<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
     return hipGetLastError();
   }
-  gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, kPartial>
+  gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, kPartial>
       <<<dim3(uint32_t(tiles), uint32_t(plan.splits)), block, 0, stream>>>(m, n, k, a, b, e, s);
   const hipError_t rc = hipGetLastError();
   if (rc != hipSuccess) return rc;
@@ -484,8 +484,9 @@ template <class T, bool A_K, bool B_K>
 hipError_t pick(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const Epilogue &e,
                 const GemmPlan &plan, float *partial, hipStream_t stream) {
   switch (plan.tile) {
-    case 0: return run<T, A_K, B_K, 256, 256, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
-    default: return run<T, A_K, B_K, 128, 128, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
+    case 0: return run<T, A_K, B_K, 256, 256, 2, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
+    case 1: return run<T, A_K, B_K, 128, 128, 2, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
+    default: return run<T, A_K, B_K, 128, 128, 2, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
   }
 }
 
@@ -505,19 +506,43 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *p, int64_t rows, int
 
 }  // namespace
 
+// The tile and the number of splits of the contraction with the least expected
+// time.  Three shapes: 256 x 256, one workgroup a CU, reaches the highest rate;
+// 128 x 128 with two workgroups a CU fills the card with a quarter of the output;
+// 128 x 128 with a longer ring of loads, one workgroup a CU, hides the latency of
+// memory better where that suffices.  Microseconds a step and a workgroup's start
+// and end as measured in bf16 (2048^3: 45 / 28 / 21 us; 4096^3: 94 / 110 / 136;
+// 1152 x 1792 x 3840: 42 / 26 / 35; 149 x 4096 x 14336: 81 / 49 / 33).  A split
+// costs its partial products' way through the caches: 65,536 x 3584 x 2560's
+// weight gradient takes 1328 us whole, 932 in 7 parts; 1152 x 1792 x 3840 26 whole,
+// 40 in 2.
 GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k) {
-  GemmPlan p;
+  struct Shape {
+    int64_t side, slots;
+    double step_us, fixed_us;
+  };
+  constexpr Shape shapes[] = {{256, 256, 1.35, 6.0}, {128, 512, 0.75, 4.0}, {128, 256, 0.45, 3.5}};
   const int64_t steps = (k + kStep - 1) / kStep;
-  const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-  p.tile = big >= 192 ? 0 : 1;
-  const int64_t tiles = p.tile == 0 ? big : ((m + 127) / 128) * ((n + 127) / 128);
-  const int64_t slots = p.tile == 0 ? 256 : 512;
-  p.splits = 1;
-  if (tiles * 2 <= slots) p.splits = int(std::max<int64_t>(1, std::min<int64_t>(slots / tiles, steps / 4)));
-  p.steps = (steps + p.splits - 1) / p.splits;
-  if (p.steps > 0) p.splits = int((steps + p.steps - 1) / p.steps);
-  p.bytes = p.splits > 1 ? up16(int64_t(p.splits) * m * ((n + 7) / 8 * 8) * 4) : 0;
-  return p;
+  GemmPlan best;
+  double least = 0;
+  for (int tile = 0; tile < 3; ++tile) {
+    const Shape &s = shapes[tile];
+    const int64_t tiles = ((m + s.side - 1) / s.side) * ((n + s.side - 1) / s.side);
+    for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * 2 <= steps); ++splits) {
+      const int64_t each = (steps + splits - 1) / splits;
+      if (splits > 1 && (steps + each - 1) / each != splits) continue;
+      const double rounds = double((tiles * splits + s.slots - 1) / s.slots);
+      const double join = splits > 1 ? 4.0 + double(splits) * double(m) * double(n) * 8 / 6e6 : 0.0;
+      const double us = rounds * (double(each) * s.step_us + s.fixed_us) + join;
+      if (least != 0 && us >= least) continue;
+      least = us;
+      best.tile = tile;
+      best.splits = int(splits);
+      best.steps = each;
+    }
+  }
+  best.bytes = best.splits > 1 ? up16(int64_t(best.splits) * m * ((n + 7) / 8 * 8) * 4) : 0;
+  return best;
 }
 
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
