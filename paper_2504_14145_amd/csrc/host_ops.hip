@@ -165,13 +165,14 @@ GradPlan plan_grad(const dip_linear_grad_args *a) {
   return p;
 }
 
-// An operand of a product: in place, or its copy made first.
-int place(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld, bool k_rows, char *ws,
-          int64_t at, hipStream_t st, Operand *out) {
-  *out = Operand{p, ld, k_rows};
-  if (at < 0 || rows == 0 || cols == 0) return DIP_OK;
-  *out = Operand{ws + at, up8(cols), k_rows};
-  return hip_code(launch_pack(dtype, p, rows, cols, ld, ws + at, out->ld, st));
+// An operand of a product: in place, or the copy that `job` is to make.
+Operand place(const void *p, int64_t rows, int64_t cols, int64_t ld, bool k_rows, char *ws, int64_t at, PackJob *job) {
+  if (at < 0 || rows == 0 || cols == 0) return Operand{p, ld, k_rows};
+  *job = PackJob{p, rows, cols, ld, ws + at, up8(cols)};
+  return Operand{job->out, job->ldo, k_rows};
+}
+int pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t st) {
+  return a.rows || b.rows ? hip_code(launch_pack(dtype, a, b, st)) : int(DIP_OK);
 }
 
 int check_norm(int64_t b, int64_t s, int64_t c, int32_t groups, int32_t dtype, int32_t act) {
@@ -236,9 +237,10 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   if (a->m == 0 || a->n == 0) return DIP_OK;
   const hipStream_t st = hipStream_t(stream);
   char *ws = static_cast<char *>(a->workspace);
-  Operand x, w;
-  OPS_CHECK(place(a->dtype, a->x, a->m, a->k, a->ldx, false, ws, p.x_at, st, &x));
-  OPS_CHECK(place(a->dtype, a->w, a->n, a->k, a->ldw, false, ws, p.w_at, st, &w));
+  PackJob px, pw;
+  const Operand x = place(a->x, a->m, a->k, a->ldx, false, ws, p.x_at, &px);
+  const Operand w = place(a->w, a->n, a->k, a->ldw, false, ws, p.w_at, &pw);
+  OPS_CHECK(pack(a->dtype, px, pw, st));
   Epilogue e{};
   e.bias = a->bias;
   e.residual = a->residual;
@@ -249,11 +251,6 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   e.ldp = a->ldp;
   e.drop = make_drop(a->drop);
   e.act = a->act;
-  e.vec_bias = aligned16(a->bias, 0, 2);
-  e.vec_res = aligned16(a->residual, a->ldr, 2);
-  e.vec_out = aligned16(a->y, a->ldy, 2);
-  e.vec_pre = aligned16(a->pre, a->ldp, 2);
-  e.fast = e.vec_bias && (!a->residual || e.vec_res) && e.vec_out && (!a->pre || e.vec_pre);
   return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm,
                               reinterpret_cast<float *>(ws + p.partial_at), st));
 }
@@ -282,8 +279,6 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     gi.ldp = a->ldp;
     gi.drop = make_drop(a->drop);
     gi.act = a->act;
-    gi.vec_dy = aligned16(a->dy, a->ldy, 2);
-    gi.vec_pre = aligned16(a->pre, a->ldp, 2);
     if (p.g_at >= 0) {
       g = gi.out = ws + p.g_at;
       ldg = gi.ldo = up8(a->n);
@@ -293,15 +288,17 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     OPS_CHECK(hip_code(launch_grad_in(a->dtype, gi, st)));
   }
   if (a->db && a->n > 0 && !(a->m == 0 && a->accumulate))
-    OPS_CHECK(hip_code(launch_sum_rows(reinterpret_cast<const float *>(ws + p.sums_at),
-                                       p.chunks, a->n, a->db, a->grad_dtype, a->accumulate, st)));
+    OPS_CHECK(hip_code(launch_sum_rows(SumRows{reinterpret_cast<const float *>(ws + p.sums_at), p.chunks, a->n, a->n,
+                                               a->db, nullptr, a->accumulate},
+                                       a->grad_dtype, st)));
+  PackJob px, pw;
+  const Operand x = place(a->x, a->dw ? a->m : 0, a->k, a->ldx, true, ws, p.x_at, &px);
+  const Operand w = place(a->w, a->dx ? a->n : 0, a->k, a->ldw, true, ws, p.w_at, &pw);
+  OPS_CHECK(pack(a->dtype, px, pw, st));
   if (a->dx && a->m > 0 && a->k > 0) {
     Epilogue e{};
     e.out = a->dx;
     e.ldo = a->lddx;
-    e.vec_out = e.fast = aligned16(a->dx, a->lddx, 2);
-    Operand w;
-    OPS_CHECK(place(a->dtype, a->w, a->n, a->k, a->ldw, true, ws, p.w_at, st, &w));
     OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
                                    partial, st)));
   }
@@ -311,10 +308,6 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     e.ldo = a->lddw;
     e.out_f32 = a->grad_dtype == DIP_F32;
     e.accumulate = a->accumulate != 0;
-    e.vec_out = aligned16(a->dw, a->lddw, elem_bytes(a->grad_dtype));
-    e.fast = e.vec_out && !e.out_f32 && !e.accumulate;
-    Operand x;
-    OPS_CHECK(place(a->dtype, a->x, a->m, a->k, a->ldx, true, ws, p.x_at, st, &x));
     OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,
                                    partial, st)));
   }
@@ -344,7 +337,7 @@ int64_t dip_group_norm_workspace(const dip_group_norm_args *a) {
 int dip_group_norm(const dip_group_norm_args *a, void *stream) {
   OPS_CHECK(check_group_norm(a));
   OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, group_norm_workspace(*a)));
-  if (a->b == 0) return DIP_OK;
+  if (a->b == 0 || a->c == 0) return DIP_OK;
   return hip_code(launch_group_norm(*a, hipStream_t(stream)));
 }
 

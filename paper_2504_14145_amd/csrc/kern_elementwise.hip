@@ -9,38 +9,58 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Eight columns of a row a thread.
-template <class T>
-__global__ __launch_bounds__(kThreads) void dropout_add_kernel(int64_t m, int64_t n, const T *x,
-                                                               int64_t ldx, const T *r,
-                                                               int64_t ldr, Drop d, T *y,
-                                                               int64_t ldy, bool vx, bool vr,
-                                                               bool vy) {
-  const int64_t per = (n + 7) / 8, all = m * per;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < all;
-       i += int64_t(gridDim.x) * kThreads) {
-    const int64_t row = i / per, col = i % per * 8;
-    const int left = int(min(int64_t(8), n - col));
-    float v[8], q[8];
-    load8(x + row * ldx + col, left, vx, v);
-    if (d.drop_of) drop8(d, uint32_t(col / 8), uint32_t(row), v);
-    if (r) {
-      load8(r + row * ldr + col, left, vr, q);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += q[j];
-    }
-    store8(y + row * ldy + col, left, vy, v);
+// n / d for n below 2^31, d at least 1, by one high product.
+struct Divide {
+  uint32_t by, mul, shift;
+  explicit Divide(uint32_t d) : by(d), mul(0), shift(0) {
+    while ((uint64_t(1) << shift) < d) ++shift;
+    // ceil(2^(32 + shift) / d) - 2^32, below 2^32
+    mul = uint32_t(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - d)) / d + 1);
   }
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
+
+// Bound by memory while a counter's 128 bits serve eight elements: its twenty
+// 32 x 32 products take 320 cycles a wave, less than the wave's 24 bytes a lane
+// take to come and go.  Eight columns of a row a thread.
+template <class T, bool RESIDUAL>
+__global__ __launch_bounds__(kThreads) void dropout_add_kernel(uint32_t items, uint32_t row0, Divide per, int64_t n,
+                                                               const T *x, int64_t ldx, const T *r, int64_t ldr,
+                                                               Drop d, T *y, int64_t ldy) {
+  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
+  if (i >= items) return;
+  const uint32_t in = per(i), row = row0 + in;
+  const int64_t col = int64_t(i - in * per.by) * 8;
+  const int left = int(min(int64_t(8), n - col));
+  float v[8], q[8];
+  load8(x + row * ldx + col, left, v);
+  if constexpr (RESIDUAL) load8(r + row * ldr + col, left, q);
+  if (d.drop_of) drop8(d, uint32_t(col / 8), row, v);
+  if constexpr (RESIDUAL) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += q[j];
+  }
+  store8(y + row * ldy + col, left, v);
 }
 
 template <class T>
 hipError_t dropout_add(int64_t m, int64_t n, const void *x, int64_t ldx, const void *r, int64_t ldr,
                        const Drop &d, void *y, int64_t ldy, hipStream_t stream) {
-  const int64_t blocks = (m * ((n + 7) / 8) + kThreads - 1) / kThreads;
-  dropout_add_kernel<T><<<dim3(uint32_t(std::min<int64_t>(blocks, 1 << 20))), dim3(kThreads), 0, stream>>>(
-      m, n, static_cast<const T *>(x), ldx, static_cast<const T *>(r), ldr, d, static_cast<T *>(y),
-      ldy, aligned16(x, ldx, sizeof(T)), aligned16(r, ldr, sizeof(T)), aligned16(y, ldy, sizeof(T)));
-  return hipGetLastError();
+  const int64_t per = (n + 7) / 8, most = ((int64_t(1) << 31) - 1) / per;   // rows a launch
+  for (int64_t row0 = 0; row0 < m; row0 += most) {
+    const uint32_t items = uint32_t(std::min(most, m - row0) * per);
+    const dim3 grid((items + kThreads - 1) / kThreads);
+    auto go = [&](auto kernel) {
+      kernel<<<grid, dim3(kThreads), 0, stream>>>(items, uint32_t(row0), Divide(uint32_t(per)), n,
+                                                  static_cast<const T *>(x), ldx, static_cast<const T *>(r), ldr, d,
+                                                  static_cast<T *>(y), ldy);
+    };
+    if (r) go(dropout_add_kernel<T, true>);
+    else go(dropout_add_kernel<T, false>);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // A block takes 256 columns (32 threads of eight) of one chunk of rows, eight
@@ -57,10 +77,10 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   if (left > 0) {
     for (int64_t row = r0 + ty; row < r1; row += 8) {
       float v[8], z[8];
-      load8(static_cast<const T *>(g.dy) + row * g.ldy + col, left, g.vec_dy, v);
+      load8(static_cast<const T *>(g.dy) + row * g.ldy + col, left, v);
       if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row), v);
       if (g.pre) {
-        load8(static_cast<const T *>(g.pre) + row * g.ldp + col, left, g.vec_pre, z);
+        load8(static_cast<const T *>(g.pre) + row * g.ldp + col, left, z);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= act_slope(z[j], g.act);
       }
@@ -69,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
         if (j >= left) v[j] = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] += v[j];
-      if (g.out) store8(static_cast<T *>(g.out) + row * g.ldo + col, 8, true, v);
+      if (g.out) store8(static_cast<T *>(g.out) + row * g.ldo + col, 8, v);
     }
   }
   if (!g.partial) return;
@@ -85,15 +105,44 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   }
 }
 
-template <class O>
-__global__ __launch_bounds__(kThreads) void sum_rows_kernel(const float *p, int64_t rows,
-                                                            int64_t cols, O *out, int accumulate) {
-  const int64_t c = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (c >= cols) return;
+// 64 columns a workgroup, LANES threads a column.
+template <class O, int LANES>
+__global__ __launch_bounds__(64 * LANES) void sum_rows_kernel(SumRows a) {
+  __shared__ float s[LANES][64];
+  const int tx = threadIdx.x % 64, ty = threadIdx.x / 64;
+  const int64_t col = int64_t(blockIdx.x) * 64 + tx, all = a.out1 ? 2 * a.c : a.c;
   float v = 0.f;
-  for (int64_t r = 0; r < rows; ++r) v += p[r * cols + c];
-  if (accumulate) v += float(out[c]);
-  out[c] = O(v);
+  if (col < all) {
+    const float *p = a.partial + col;
+    int64_t r = ty;
+    for (; r + 3 * LANES < a.rows; r += 4 * LANES) {
+      const float q0 = p[r * a.ld], q1 = p[(r + LANES) * a.ld], q2 = p[(r + 2 * LANES) * a.ld],
+                  q3 = p[(r + 3 * LANES) * a.ld];
+      v += (q0 + q1) + (q2 + q3);
+    }
+    for (; r < a.rows; r += LANES) v += p[r * a.ld];
+  }
+  s[ty][tx] = v;
+  __syncthreads();
+  if (ty != 0 || col >= all) return;
+#pragma unroll
+  for (int i = 1; i < LANES; ++i) v += s[i][tx];
+  O *out = static_cast<O *>(col < a.c ? a.out0 : a.out1);
+  if (!out) return;
+  const int64_t at = col < a.c ? col : col - a.c;
+  if (a.accumulate) v += float(out[at]);
+  out[at] = O(v);
+}
+
+template <class O>
+hipError_t sum_rows(const SumRows &a, hipStream_t stream) {
+  if (!a.out0 && !a.out1) return hipSuccess;
+  const dim3 grid(uint32_t(((a.out1 ? 2 * a.c : a.c) + 63) / 64));
+  if (a.rows > 16)
+    sum_rows_kernel<O, 16><<<grid, dim3(1024), 0, stream>>>(a);
+  else
+    sum_rows_kernel<O, 4><<<grid, dim3(256), 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -122,20 +171,10 @@ hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_sum_rows(const float *partial, int64_t rows, int64_t cols, void *out,
-                           int out_dtype, int accumulate, hipStream_t stream) {
-  const dim3 grid(uint32_t((cols + kThreads - 1) / kThreads)), block(kThreads);
-  switch (out_dtype) {
-    case DIP_F32:
-      sum_rows_kernel<<<grid, block, 0, stream>>>(partial, rows, cols, static_cast<float *>(out), accumulate);
-      break;
-    case DIP_F16:
-      sum_rows_kernel<<<grid, block, 0, stream>>>(partial, rows, cols, static_cast<_Float16 *>(out), accumulate);
-      break;
-    default:
-      sum_rows_kernel<<<grid, block, 0, stream>>>(partial, rows, cols, static_cast<__bf16 *>(out), accumulate);
-  }
-  return hipGetLastError();
+hipError_t launch_sum_rows(const SumRows &a, int out_dtype, hipStream_t stream) {
+  return out_dtype == DIP_F32   ? sum_rows<float>(a, stream)
+         : out_dtype == DIP_F16 ? sum_rows<_Float16>(a, stream)
+                                : sum_rows<__bf16>(a, stream);
 }
 
 }  // namespace dipops

@@ -1,135 +1,809 @@
-// kern_groupnorm.hip -- group norm with an activation over channels-last arrays.
+// kern_groupnorm.hip -- group norm with an activation over channels-last arrays,
+// and its gradients.
+//
+// All of it is bound by memory: x read once and y written once forward, x and dy
+// read and dx written backward, against some 30 operations an element.  Three
+// ways, by the shape (plan below):
+//  rows   one position a sample: a group is one contiguous row, held in registers
+//         from the read to the write, one pass.
+//  block  a workgroup takes a slab of whole groups of one sample and goes over it
+//         twice, the second time out of the caches.
+//  split  a sample's positions are cut into chunks: a pass for the sums of every
+//         channel of a chunk, a small kernel that joins them, a pass that writes.
+// Variances are sums of squares about the mean (rows), or about a value of the
+// channel (block, split), joined through (count, mean, sum of squares about the
+// mean), so that a mean far from zero costs no digits.  Sums are float32, in an
+// order that depends on the shape alone.
+#include <algorithm>
+
 #include "ops_internal.h"
 
 namespace dipops {
 namespace {
 
-constexpr int kThreads = 256;
+// ------------------------------------------------------------ rows
 
-__device__ __forceinline__ float block_sum(float v, float *s) {
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = v;
-  __syncthreads();
-  return (s[0] + s[1]) + (s[2] + s[3]);
+  return v;
+}
+// over the waves of a workgroup; s holds two sets of values in turn, so that one
+// barrier a sum is enough
+template <int THREADS>
+__device__ __forceinline__ float block_sum(float v, float *s, int &turn) {
+  v = wave_sum(v);
+  if constexpr (THREADS > 64) {
+    float *q = s + turn * (THREADS / 64);
+    turn ^= 1;
+    if (threadIdx.x % 64 == 0) q[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) v += q[i];
+  }
+  return v;
 }
 
-// One block a sample and group; statistics in two passes over the data.
 template <class T>
-__global__ __launch_bounds__(kThreads) void norm_kernel(dip_group_norm_args a) {
-  __shared__ float s[4];
-  const int64_t i = blockIdx.x / a.groups;
-  const int g = int(blockIdx.x % a.groups), per = int(a.c / a.groups);
-  const int64_t count = a.s * per;
-  const T *x = static_cast<const T *>(a.x) + i * a.x_sb + int64_t(g) * per;
-  T *y = static_cast<T *>(a.y) + i * a.y_sb + int64_t(g) * per;
-  const T *gamma = static_cast<const T *>(a.gamma), *beta = static_cast<const T *>(a.beta);
-  float v = 0.f;
-  for (int64_t j = threadIdx.x; j < count; j += kThreads) v += float(x[j / per * a.x_ss + j % per]);
-  const float mean = block_sum(v, s) / float(max(count, int64_t(1)));
-  v = 0.f;
-  for (int64_t j = threadIdx.x; j < count; j += kThreads) {
-    const float d = float(x[j / per * a.x_ss + j % per]) - mean;
-    v += d * d;
+struct Affine {
+  const T *gamma, *beta;
+  // of columns c .. c + 7, ones and zeros where there are none
+  __device__ __forceinline__ void get(int64_t c, int left, float (&g)[8], float (&b)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = 1.f, b[i] = 0.f;
+    if (gamma) load8(gamma + c, left, g);
+    if (beta) load8(beta + c, left, b);
   }
-  const float rstd = 1.f / sqrtf(block_sum(v, s) / float(max(count, int64_t(1))) + a.eps);
-  if (threadIdx.x == 0) {
-    if (a.mean) a.mean[blockIdx.x] = mean;
-    if (a.rstd) a.rstd[blockIdx.x] = rstd;
+};
+
+// THREADS a row of `per` channels, NV vectors of eight a thread.
+template <class T, int THREADS, int NV>
+__global__ __launch_bounds__(256) void rows_kernel(dip_group_norm_args a, int64_t rows) {
+  constexpr int kRows = 256 / THREADS;
+  __shared__ float s[2 * 4];
+  int turn = 0;
+  const int t = threadIdx.x % THREADS;
+  const int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / THREADS;
+  if (row >= rows) return;   // whole waves: THREADS is 64, or the workgroup has one row
+  const uint32_t i = uint32_t(row) / uint32_t(a.groups), g = uint32_t(row) % uint32_t(a.groups);
+  const int per = int(a.c / a.groups);
+  const int64_t c0 = int64_t(g) * per;
+  const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c0;
+  T *y = static_cast<T *>(a.y) + i * a.y_sb + c0;
+  float v[NV][8];
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    load8(x + (t + j * THREADS) * 8, per - (t + j * THREADS) * 8, v[j]);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sum += v[j][q];
   }
-  for (int64_t j = threadIdx.x; j < count; j += kThreads) {
-    const int c = int(j % per);
-    float z = (float(x[j / per * a.x_ss + c]) - mean) * rstd;
-    z = z * (gamma ? float(gamma[g * per + c]) : 1.f) + (beta ? float(beta[g * per + c]) : 0.f);
-    y[j / per * a.y_ss + c] = T(act_of(z, a.act));
+  const float inv = 1.f / float(per);
+  const float mean = block_sum<THREADS>(sum, s, turn) * inv;
+  sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float d = v[j][q] - mean;
+      v[j][q] = d;
+      sum += (t + j * THREADS) * 8 + q < per ? d * d : 0.f;
+    }
+  const float rstd = 1.f / sqrtf(block_sum<THREADS>(sum, s, turn) * inv + a.eps);
+  if (t == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  const Affine<T> affine{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (t + j * THREADS) * 8;
+    if (c >= per) continue;
+    float ga[8], be[8];
+    affine.get(c0 + c, per - c, ga, be);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[j][q] = act_of(v[j][q] * rstd * ga[q] + be[q], a.act);
+    store8(y + c, per - c, v[j]);
   }
 }
 
-// One block a sample and group; its channels' sums over positions go to
-// partial[2][b][c] (dgamma's first).
+// A workgroup goes over the samples j, j + gridDim.x, .. of one group, and keeps
+// the sums of dgamma and dbeta of its channels on the way: partial[j][2][c].
+template <class T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void rows_grad_kernel(dip_group_norm_grad_args a, float *partial) {
+  __shared__ float s[2 * 2 * 4];
+  int turn = 0, turn2 = 0;
+  const int t = threadIdx.x, per = int(a.c / a.groups);
+  const uint32_t g = blockIdx.y;
+  const int64_t c0 = int64_t(g) * per;
+  const Affine<T> affine{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)};
+  float sg[NV][8] = {}, sb[NV][8] = {}, ga[NV][8], be[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) affine.get(c0 + (t + j * THREADS) * 8, per - (t + j * THREADS) * 8, ga[j], be[j]);
+  const float inv = 1.f / float(per);
+  for (int64_t i = blockIdx.x; i < a.b; i += gridDim.x) {
+    const float mean = a.mean[i * a.groups + g], rstd = a.rstd[i * a.groups + g];
+    const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c0;
+    const T *dy = static_cast<const T *>(a.dy) + i * a.dy_sb + c0;
+    float xh[NV][8], h[NV][8];
+    float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (t + j * THREADS) * 8;
+      load8(x + c, per - c, xh[j]);
+      load8(dy + c, per - c, h[j]);   // zeros beyond the row
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        xh[j][q] = (xh[j][q] - mean) * rstd;
+        const float v = a.act == DIP_ACT_NONE ? h[j][q] : h[j][q] * act_slope(xh[j][q] * ga[j][q] + be[j][q], a.act);
+        sg[j][q] += v * xh[j][q];
+        sb[j][q] += v;
+        h[j][q] = v * ga[j][q];
+        m1 += h[j][q];
+        m2 += h[j][q] * xh[j][q];
+      }
+    if (!a.dx) continue;
+    m1 = block_sum<THREADS>(m1, s, turn) * inv;
+    m2 = block_sum<THREADS>(m2, s + 2 * 4, turn2) * inv;
+    T *dx = static_cast<T *>(a.dx) + i * a.dx_sb + c0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (t + j * THREADS) * 8;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) h[j][q] = rstd * (h[j][q] - m1 - xh[j][q] * m2);
+      store8(dx + c, per - c, h[j]);
+    }
+  }
+  if (!partial) return;
+  float *p = partial + int64_t(blockIdx.x) * 2 * a.c + c0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (t + j * THREADS) * 8;
+    store8(p + c, per - c, sg[j]);
+    store8(p + a.c + c, per - c, sb[j]);
+  }
+}
+
+// ------------------------------------------------------------ block and split
+
+// How a workgroup's threads lie over a slab: vector vx of eight channels, rows
+// ty, ty + TY, .., TY a power of two.
+struct Lanes {
+  int vx, ty, TY;
+  bool on;
+  __device__ Lanes(int vectors, int lanes_y) {
+    TY = lanes_y;
+    vx = int(threadIdx.x) % vectors;
+    ty = int(threadIdx.x) / vectors;
+    on = ty < TY;
+  }
+};
+
+// Adds two values a channel over the workgroup's rows; every thread then finds
+// the sums of channel c at s[c] and s[half + c], half = vectors * 8 * TY.
+__device__ __forceinline__ void channel_sums(const Lanes &l, int vectors, const float (&a)[8], const float (&b)[8],
+                                             float *s) {
+  const int width = vectors * 8, half = width * l.TY;
+  __syncthreads();
+  if (l.on) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      s[l.ty * width + l.vx * 8 + q] = a[q];
+      s[half + l.ty * width + l.vx * 8 + q] = b[q];
+    }
+  }
+  __syncthreads();
+  for (int h = l.TY / 2; h >= 1; h /= 2) {
+    for (int j = threadIdx.x; j < 2 * h * width; j += blockDim.x) {
+      const int which = j >= h * width, at = (which ? half - h * width : 0) + j;
+      s[at] += s[at + h * width];
+    }
+    __syncthreads();
+  }
+}
+
+// The sums about a channel's own value k: a = sum (x - k), b = sum (x - k)^2,
+// over rows r0 + ty, .. below r1.
 template <class T>
-__global__ __launch_bounds__(kThreads) void norm_grad_kernel(dip_group_norm_grad_args a) {
-  __shared__ float s[4];
-  const int64_t i = blockIdx.x / a.groups;
-  const int g = int(blockIdx.x % a.groups), per = int(a.c / a.groups);
-  const int64_t count = a.s * per;
-  const T *x = static_cast<const T *>(a.x) + i * a.x_sb + int64_t(g) * per;
-  const T *dy = static_cast<const T *>(a.dy) + i * a.dy_sb + int64_t(g) * per;
-  const T *gamma = static_cast<const T *>(a.gamma), *beta = static_cast<const T *>(a.beta);
-  const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
-  float *pg = static_cast<float *>(a.workspace) + i * a.c + int64_t(g) * per;
-  float *pb = pg + a.b * a.c;
-  auto grad = [&](int64_t p, int c, float &xh) {
-    xh = (float(x[p * a.x_ss + c]) - mean) * rstd;
-    const float z = xh * (gamma ? float(gamma[g * per + c]) : 1.f) + (beta ? float(beta[g * per + c]) : 0.f);
-    return float(dy[p * a.dy_ss + c]) * act_slope(z, a.act);
+__device__ __forceinline__ void moments(const T *x, int64_t ss, int left, const Lanes &l, int64_t r0, int64_t r1,
+                                        float (&k)[8], float (&a)[8], float (&b)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) a[q] = b[q] = k[q] = 0.f;
+  if (!l.on || r0 >= r1) return;
+  load8(x + r0 * ss, left, k);
+  int64_t r = r0 + l.ty;
+  for (; r + 3 * l.TY < r1; r += 4 * l.TY) {
+    float v[4][8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load8(x + (r + u * l.TY) * ss, left, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float d = v[u][q] - k[q];
+        a[q] += d;
+        b[q] += d * d;
+      }
+  }
+  for (; r < r1; r += l.TY) {
+    float v[8];
+    load8(x + r * ss, left, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float d = v[q] - k[q];
+      a[q] += d;
+      b[q] += d * d;
+    }
+  }
+}
+
+// a sum of squares that rounding took below zero; NaN stays
+__device__ __forceinline__ float above_zero(float v) { return v < 0.f ? 0.f : v; }
+
+// Eight channels' part in the forward's second pass and in both of the
+// gradient's: z = x scale + shift, xh = (x - mean) rstd.
+struct Channels {
+  float mean[8], rstd[8], gamma[8], beta[8];
+};
+
+template <class T>
+__device__ __forceinline__ void write_rows(const T *x, int64_t x_ss, T *y, int64_t y_ss, int left, const Lanes &l,
+                                           int64_t r0, int64_t r1, const Channels &c, int act) {
+  if (!l.on) return;
+  float scale[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) scale[q] = c.rstd[q] * c.gamma[q];
+  auto one = [&](int64_t r, float(&v)[8]) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = (v[q] - c.mean[q]) * scale[q] + c.beta[q];
+    if (act == DIP_ACT_SILU) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = act_of(v[q], DIP_ACT_SILU);
+    } else if (act != DIP_ACT_NONE) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = act_of(v[q], act);
+    }
+    store8(y + r * y_ss, left, v);
   };
-  float h_sum = 0.f, hx_sum = 0.f;
-  for (int c = 0; c < per; ++c) {
-    float sg = 0.f, sb = 0.f;
-    for (int64_t p = threadIdx.x; p < a.s; p += kThreads) {
-      float xh;
-      const float v = grad(p, c, xh);
-      sg += v * xh;
-      sb += v;
+  int64_t r = r0 + l.ty;
+  for (; r + l.TY < r1; r += 2 * l.TY) {
+    float v[2][8];
+    load8(x + r * x_ss, left, v[0]);
+    load8(x + (r + l.TY) * x_ss, left, v[1]);
+    one(r, v[0]);
+    one(r + l.TY, v[1]);
+  }
+  if (r < r1) {
+    float v[8];
+    load8(x + r * x_ss, left, v);
+    one(r, v);
+  }
+}
+
+// v = dy act'(z) and xh of eight channels of one row
+__device__ __forceinline__ void grad_terms(const Channels &c, int act, float (&xv)[8], float (&dv)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) xv[q] = (xv[q] - c.mean[q]) * c.rstd[q];
+  if (act == DIP_ACT_SILU) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) dv[q] *= act_slope(xv[q] * c.gamma[q] + c.beta[q], DIP_ACT_SILU);
+  } else if (act != DIP_ACT_NONE) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) dv[q] *= act_slope(xv[q] * c.gamma[q] + c.beta[q], act);
+  }
+}
+
+// a = sum v xh, b = sum v over a thread's rows
+template <class T>
+__device__ __forceinline__ void grad_sums(const T *x, int64_t x_ss, const T *dy, int64_t dy_ss, int left,
+                                          const Lanes &l, int64_t r0, int64_t r1, const Channels &c, int act,
+                                          float (&a)[8], float (&b)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) a[q] = b[q] = 0.f;
+  if (!l.on) return;
+  auto add = [&](float(&xv)[8], float(&dv)[8]) {
+    grad_terms(c, act, xv, dv);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      a[q] += dv[q] * xv[q];
+      b[q] += dv[q];
     }
-    sg = block_sum(sg, s);
-    sb = block_sum(sb, s);
-    if (threadIdx.x == 0) {
-      pg[c] = sg;
-      pb[c] = sb;
+  };
+  int64_t r = r0 + l.ty;
+  for (; r + l.TY < r1; r += 2 * l.TY) {
+    float xv[2][8], dv[2][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      load8(x + (r + u * l.TY) * x_ss, left, xv[u]);
+      load8(dy + (r + u * l.TY) * dy_ss, left, dv[u]);
     }
-    const float w = gamma ? float(gamma[g * per + c]) : 1.f;
-    h_sum += sb * w;
-    hx_sum += sg * w;
+    add(xv[0], dv[0]);
+    add(xv[1], dv[1]);
+  }
+  if (r < r1) {
+    float xv[8], dv[8];
+    load8(x + r * x_ss, left, xv);
+    load8(dy + r * dy_ss, left, dv);
+    add(xv, dv);
+  }
+}
+
+// dx = rstd (h - m1 - xh m2), h = v gamma
+template <class T>
+__device__ __forceinline__ void write_grad(const T *x, int64_t x_ss, const T *dy, int64_t dy_ss, T *dx, int64_t dx_ss,
+                                           int left, const Lanes &l, int64_t r0, int64_t r1, const Channels &c,
+                                           const float (&m1)[8], const float (&m2)[8], int act) {
+  if (!l.on) return;
+  auto one = [&](int64_t r, float(&xv)[8], float(&dv)[8]) {
+    grad_terms(c, act, xv, dv);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) dv[q] = c.rstd[q] * (dv[q] * c.gamma[q] - m1[q] - xv[q] * m2[q]);
+    store8(dx + r * dx_ss, left, dv);
+  };
+  int64_t r = r0 + l.ty;
+  for (; r + l.TY < r1; r += 2 * l.TY) {
+    float xv[2][8], dv[2][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      load8(x + (r + u * l.TY) * x_ss, left, xv[u]);
+      load8(dy + (r + u * l.TY) * dy_ss, left, dv[u]);
+    }
+    one(r, xv[0], dv[0]);
+    one(r + l.TY, xv[1], dv[1]);
+  }
+  if (r < r1) {
+    float xv[8], dv[8];
+    load8(x + r * x_ss, left, xv);
+    load8(dy + r * dy_ss, left, dv);
+    one(r, xv, dv);
+  }
+}
+
+// the statistics (or any per-group pair) of eight channels' groups
+__device__ __forceinline__ void of_groups(const float *p, int64_t c, int per, int left, float (&v)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = q < left ? p[uint32_t(c + q) / uint32_t(per)] : 0.f;
+}
+
+// One workgroup: a slab of `groups` whole groups of one sample.
+template <class T>
+__global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int groups, int vectors, int lanes_y) {
+  extern __shared__ float s[];
+  const Lanes l(vectors, lanes_y);
+  const int tiles = (a.groups + groups - 1) / groups;
+  const int per = int(a.c / a.groups), g0 = int(blockIdx.x % tiles) * groups, slab = min(groups, a.groups - g0) * per;
+  const int64_t i = blockIdx.x / tiles, c0 = int64_t(g0) * per, c = c0 + l.vx * 8;
+  const int left = slab - l.vx * 8;
+  const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c;
+  float k[8], u[8], v[8];
+  moments(x, a.x_ss, left, l, 0, a.s, k, u, v);
+  channel_sums(l, vectors, u, v, s);
+  const int width = vectors * 8, half = width * l.TY;
+  // channel c: s[c] its mean, s[half + c] the squares about it
+  const float n = float(max(a.s, int64_t(1)));
+  if (l.on && l.ty == 0) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int at = l.vx * 8 + q;
+      const float d = s[at];
+      s[half + at] = above_zero(s[half + at] - d * (d / n));
+      s[at] = k[q] + d / n;
+    }
+  }
+  __syncthreads();
+  float *stat = s + 2 * half;   // [2][groups]
+  for (int g = threadIdx.x; g < slab / max(per, 1); g += blockDim.x) {
+    float mean = 0.f, m2 = 0.f;
+    for (int j = 0; j < per; ++j) mean += s[g * per + j];
+    mean /= float(per);
+    for (int j = 0; j < per; ++j) {
+      const float d = s[g * per + j] - mean;
+      m2 += s[half + g * per + j] + n * d * d;
+    }
+    const float rstd = 1.f / sqrtf(m2 / (n * float(per)) + a.eps);
+    stat[g] = mean;
+    stat[groups + g] = rstd;
+    if (a.mean) a.mean[i * a.groups + g0 + g] = mean;
+    if (a.rstd) a.rstd[i * a.groups + g0 + g] = rstd;
+  }
+  __syncthreads();
+  if (left <= 0) return;
+  Channels ch;
+  of_groups(stat, l.vx * 8, per, left, ch.mean);
+  of_groups(stat + groups, l.vx * 8, per, left, ch.rstd);
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
+  write_rows(x, a.x_ss, static_cast<T *>(a.y) + i * a.y_sb + c, a.y_ss, left, l, 0, a.s, ch, a.act);
+}
+
+template <class T>
+__global__ __launch_bounds__(512) void block_grad_kernel(dip_group_norm_grad_args a, int groups, int vectors,
+                                                          int lanes_y, float *partial) {
+  extern __shared__ float s[];
+  const Lanes l(vectors, lanes_y);
+  const int tiles = (a.groups + groups - 1) / groups;
+  const int per = int(a.c / a.groups), g0 = int(blockIdx.x % tiles) * groups, slab = min(groups, a.groups - g0) * per;
+  const int64_t i = blockIdx.x / tiles, c0 = int64_t(g0) * per, c = c0 + l.vx * 8;
+  const int left = slab - l.vx * 8;
+  const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c, *dy = static_cast<const T *>(a.dy) + i * a.dy_sb + c;
+  Channels ch;
+  of_groups(a.mean + i * a.groups, c, per, left, ch.mean);
+  of_groups(a.rstd + i * a.groups, c, per, left, ch.rstd);
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
+  float u[8], v[8];
+  grad_sums(x, a.x_ss, dy, a.dy_ss, left, l, 0, a.s, ch, a.act, u, v);
+  channel_sums(l, vectors, u, v, s);
+  const int half = vectors * 8 * l.TY;
+  if (partial) {
+    float *p = partial + i * 2 * a.c + c0;
+    for (int j = threadIdx.x; j < slab; j += blockDim.x) p[j] = s[j], p[a.c + j] = s[half + j];
   }
   if (!a.dx) return;
-  const float h_mean = h_sum / float(count), hx_mean = hx_sum / float(count);
-  T *dx = static_cast<T *>(a.dx) + i * a.dx_sb + int64_t(g) * per;
-  for (int64_t j = threadIdx.x; j < count; j += kThreads) {
-    const int c = int(j % per);
-    float xh;
-    const float h = grad(j / per, c, xh) * (gamma ? float(gamma[g * per + c]) : 1.f);
-    dx[j / per * a.dx_ss + c] = T(rstd * (h - h_mean - xh * hx_mean));
+  const T *gamma = static_cast<const T *>(a.gamma);
+  float *mean = s + 2 * half;   // [2][groups]
+  for (int g = threadIdx.x; g < slab / per; g += blockDim.x) {
+    float m1 = 0.f, m2 = 0.f;
+    for (int j = 0; j < per; ++j) {
+      const float w = gamma ? float(gamma[c0 + g * per + j]) : 1.f;
+      m2 += w * s[g * per + j];
+      m1 += w * s[half + g * per + j];
+    }
+    const float inv = 1.f / (float(a.s) * float(per));
+    mean[g] = m1 * inv;
+    mean[groups + g] = m2 * inv;
+  }
+  __syncthreads();
+  if (left <= 0) return;
+  float m1[8], m2[8];
+  of_groups(mean, l.vx * 8, per, left, m1);
+  of_groups(mean + groups, l.vx * 8, per, left, m2);
+  write_grad(x, a.x_ss, dy, a.dy_ss, static_cast<T *>(a.dx) + i * a.dx_sb + c, a.dx_ss, left, l, 0, a.s, ch, m1, m2,
+             a.act);
+}
+
+// Split: a workgroup a column tile, chunk and sample, 256 threads.
+struct Part {
+  int64_t i, c, left, r0, r1, at;   // sample, channel, rows, index among all chunks
+  __device__ Part(const Lanes &l, int vectors, int tiles, int chunks, int64_t chunk, int64_t all_c, int64_t all_s,
+                  bool backwards) {
+    const uint32_t tile = blockIdx.x % tiles, rest = blockIdx.x / tiles;
+    uint32_t q = rest % chunks;
+    if (backwards) q = chunks - 1 - q;
+    i = rest / chunks;
+    at = i * chunks + q;
+    c = (int64_t(tile) * vectors + l.vx) * 8;
+    left = min(all_c - c, int64_t(8));
+    r0 = chunk * q;
+    r1 = min(r0 + chunk, all_s);
+  }
+};
+
+// A chunk's channels: partial[sample][chunk][2][c], mean and squares about it.
+template <class T>
+__global__ __launch_bounds__(256) void split_sums_kernel(dip_group_norm_args a, int vectors, int lanes_y, int tiles,
+                                                         int chunks, int64_t chunk, float *partial) {
+  extern __shared__ float s[];
+  const Lanes l(vectors, lanes_y);
+  const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, false);
+  const int left = int(w.left);
+  float k[8], u[8], v[8];
+  moments(static_cast<const T *>(a.x) + w.i * a.x_sb + w.c, a.x_ss, left, l, w.r0, w.r1, k, u, v);
+  channel_sums(l, vectors, u, v, s);
+  const int half = vectors * 8 * l.TY;
+  if (!l.on || l.ty != 0) return;
+  const float n = float(w.r1 - w.r0);
+  float *p = partial + w.at * 2 * a.c + w.c;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float d = s[l.vx * 8 + q];
+    u[q] = k[q] + d / n;
+    v[q] = above_zero(s[half + l.vx * 8 + q] - d * (d / n));
+  }
+  store8(p, left, u);
+  store8(p + a.c, left, v);
+}
+
+// One workgroup a sample and group joins its chunks' channels.
+__global__ __launch_bounds__(256) void split_join_kernel(const float *partial, int64_t s_all, int64_t chunk,
+                                                         int chunks, int64_t c, int per, float eps, float *mean,
+                                                         float *rstd, float *stat) {
+  __shared__ float s[2 * 4];
+  int turn = 0;
+  const uint32_t groups = uint32_t(c / per), i = blockIdx.x / groups, g = blockIdx.x % groups;
+  const float *p = partial + int64_t(i) * chunks * 2 * c + int64_t(g) * per;
+  const int all = chunks * per;
+  const float total = float(s_all) * float(per);
+  // every value times its count, about the first chunk's first channel
+  const float k = p[0];
+  float u = 0.f;
+  for (int j = threadIdx.x; j < all; j += 256) {
+    const int q = j / per;
+    u += (p[int64_t(q) * 2 * c + j % per] - k) * float(min(chunk, s_all - chunk * q));
+  }
+  const float m = k + block_sum<256>(u, s, turn) / total;
+  u = 0.f;
+  for (int j = threadIdx.x; j < all; j += 256) {
+    const int q = j / per;
+    const float *v = p + int64_t(q) * 2 * c + j % per;
+    const float d = v[0] - m;
+    u += v[c] + d * d * float(min(chunk, s_all - chunk * q));
+  }
+  const float r = 1.f / sqrtf(block_sum<256>(u, s, turn) / total + eps);
+  if (threadIdx.x == 0) {
+    stat[blockIdx.x] = m;
+    stat[gridDim.x + blockIdx.x] = r;
+    if (mean) mean[blockIdx.x] = m;
+    if (rstd) rstd[blockIdx.x] = r;
   }
 }
 
 template <class T>
-hipError_t norm(const dip_group_norm_args &a, hipStream_t st) {
-  norm_kernel<T><<<dim3(uint32_t(a.b * a.groups)), dim3(kThreads), 0, st>>>(a);
+__global__ __launch_bounds__(256) void split_write_kernel(dip_group_norm_args a, int vectors, int lanes_y, int tiles,
+                                                          int chunks, int64_t chunk, const float *stat) {
+  const Lanes l(vectors, lanes_y);
+  // the chunks read last come first: they may still be in the caches
+  const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, true);
+  const int left = int(w.left), per = int(a.c / a.groups);
+  const int64_t i = w.i, c = w.c;
+  if (left <= 0) return;
+  Channels ch;
+  of_groups(stat + i * a.groups, c, per, left, ch.mean);
+  of_groups(stat + (a.b + i) * a.groups, c, per, left, ch.rstd);
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
+  write_rows(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<T *>(a.y) + i * a.y_sb + c, a.y_ss, left,
+             l, w.r0, w.r1, ch, a.act);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void split_grad_sums_kernel(dip_group_norm_grad_args a, int vectors, int lanes_y, int tiles,
+                                                              int chunks, int64_t chunk, float *partial) {
+  extern __shared__ float s[];
+  const Lanes l(vectors, lanes_y);
+  const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, false);
+  const int left = int(w.left), per = int(a.c / a.groups);
+  const int64_t i = w.i, c = w.c;
+  Channels ch;
+  of_groups(a.mean + i * a.groups, c, per, left, ch.mean);
+  of_groups(a.rstd + i * a.groups, c, per, left, ch.rstd);
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
+  float u[8], v[8];
+  grad_sums(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<const T *>(a.dy) + i * a.dy_sb + c,
+            a.dy_ss, left, l, w.r0, w.r1, ch, a.act, u, v);
+  channel_sums(l, vectors, u, v, s);
+  const int half = vectors * 8 * l.TY;
+  if (!l.on || l.ty != 0) return;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) u[q] = s[l.vx * 8 + q], v[q] = s[half + l.vx * 8 + q];
+  float *p = partial + w.at * 2 * a.c + c;
+  store8(p, left, u);
+  store8(p + a.c, left, v);
+}
+
+// One workgroup a group: the group's means of h and h xh of every sample to
+// mean[2][b][groups], and its channels' dgamma and dbeta over all samples.  A
+// wave takes every fourth channel, its lanes the chunks.
+template <class T>
+__global__ __launch_bounds__(256) void split_grad_join_kernel(const float *partial, int64_t b, int64_t s_all,
+                                                              int chunks, int64_t c, int per, const T *gamma,
+                                                              T *dgamma, T *dbeta, float *mean) {
+  __shared__ float s[2][4];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, groups = int(c / per);
+  const int64_t c0 = int64_t(blockIdx.x) * per;
+  const float inv = 1.f / (float(s_all) * float(per));
+  for (int64_t i = 0; i < b; ++i) {
+    float m1 = 0.f, m2 = 0.f;
+    for (int j = wave; j < per; j += 4) {
+      float u = 0.f, v = 0.f;
+      for (int q = lane; q < chunks; q += 64) {
+        const float *p = partial + (i * chunks + q) * 2 * c + c0 + j;
+        u += p[0];
+        v += p[c];
+      }
+      const float w = gamma ? float(gamma[c0 + j]) : 1.f;
+      m2 += w * wave_sum(u);
+      m1 += w * wave_sum(v);
+    }
+    if (lane == 0) s[0][wave] = m1, s[1][wave] = m2;
+    __syncthreads();
+    if (threadIdx.x < 2) {
+      const float *p = s[threadIdx.x];
+      mean[(threadIdx.x * b + i) * groups + blockIdx.x] = ((p[0] + p[1]) + (p[2] + p[3])) * inv;
+    }
+    __syncthreads();
+  }
+  for (int j = wave; j < per; j += 4) {
+    float u = 0.f, v = 0.f;
+    for (int64_t q = lane; q < b * chunks; q += 64) {
+      const float *p = partial + q * 2 * c + c0 + j;
+      u += p[0];
+      v += p[c];
+    }
+    u = wave_sum(u);
+    v = wave_sum(v);
+    if (lane == 0) {
+      if (dgamma) dgamma[c0 + j] = T(u);
+      if (dbeta) dbeta[c0 + j] = T(v);
+    }
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void split_grad_write_kernel(dip_group_norm_grad_args a, int vectors, int lanes_y, int tiles,
+                                                               int chunks, int64_t chunk, const float *mean) {
+  const Lanes l(vectors, lanes_y);
+  const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, true);
+  const int left = int(w.left), per = int(a.c / a.groups);
+  const int64_t i = w.i, c = w.c;
+  if (left <= 0) return;
+  Channels ch;
+  of_groups(a.mean + i * a.groups, c, per, left, ch.mean);
+  of_groups(a.rstd + i * a.groups, c, per, left, ch.rstd);
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
+  float m1[8], m2[8];
+  of_groups(mean + i * a.groups, c, per, left, m1);
+  of_groups(mean + (a.b + i) * a.groups, c, per, left, m2);
+  write_grad(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<const T *>(a.dy) + i * a.dy_sb + c,
+             a.dy_ss, static_cast<T *>(a.dx) + i * a.dx_sb + c, a.dx_ss, left, l, w.r0, w.r1, ch, m1, m2, a.act);
+}
+
+// ------------------------------------------------------------ plans
+
+enum Way { kRows, kBlock, kSplit };
+struct Plan {
+  Way way = kRows;
+  int groups = 1, vectors = 1, lanes_y = 1, threads = 256, tiles = 1;   // block: groups a slab
+  int64_t chunk = 0, chunks = 1;                                       // split
+  int64_t row_blocks = 1;                                              // rows' gradient
+  size_t lds = 0;
+  int64_t partial = 0, stat = 0;   // floats
+  int64_t bytes() const { return up16(partial * 4) + up16(stat * 4); }
+};
+
+int pow2_at_most(int64_t n) {
+  int p = 1;
+  while (2 * p <= n) p *= 2;
+  return p;
+}
+
+constexpr int kRowMost = 16384;      // channels a row held in registers
+constexpr int kSlabMost = 4096;      // channels a slab, eight a thread
+
+Plan plan(int64_t b, int64_t s, int64_t c, int groups, bool grad) {
+  Plan p;
+  const int64_t per = c / groups;
+  if (s == 1 && per <= kRowMost && groups < 65536) {
+    p.way = kRows;
+    p.row_blocks = std::max<int64_t>(1, std::min<int64_t>(b, std::max<int64_t>(1, 512 / groups)));
+    p.partial = grad ? p.row_blocks * 2 * c : 0;
+    return p;
+  }
+  // a slab of at least 128 bytes of a row, and beyond that as many groups as
+  // still leave workgroups for the whole card
+  int64_t slab = std::max<int64_t>(1, std::min<int64_t>(groups, (64 + per - 1) / std::max<int64_t>(per, 1)));
+  while (slab * 2 <= groups && slab * 2 * per <= 512 && b * ((groups + slab * 2 - 1) / (slab * 2)) >= 1024) slab *= 2;
+  const int64_t blocks = b * ((groups + slab - 1) / slab);
+  if (slab * per <= kSlabMost && (s * slab * per <= 32768 || blocks >= 512)) {
+    p.way = kBlock;
+    p.groups = int(slab);
+    p.vectors = int((slab * per + 7) / 8);
+    p.threads = s * p.vectors > 256 ? 512 : 256;
+    p.lanes_y = pow2_at_most(std::min<int64_t>(std::max<int64_t>(s, 1), p.threads / p.vectors));
+    p.tiles = int((groups + slab - 1) / slab);
+    p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4 + size_t(2) * slab * 4;
+    p.partial = grad ? b * 2 * c : 0;
+    return p;
+  }
+  p.way = kSplit;
+  const int64_t cv = (c + 7) / 8;
+  p.tiles = int((cv + 255) / 256);
+  p.vectors = int((cv + p.tiles - 1) / p.tiles);
+  p.lanes_y = pow2_at_most(256 / p.vectors);
+  // chunks for about eight workgroups a CU, of at least eight rows a thread
+  const int64_t most = std::max<int64_t>(1, s / (int64_t(p.lanes_y) * 8));
+  p.chunks = std::max<int64_t>(1, std::min<int64_t>(most, 2048 / std::max<int64_t>(1, b * p.tiles)));
+  p.chunk = (s + p.chunks - 1) / p.chunks;
+  p.chunks = (s + p.chunk - 1) / p.chunk;
+  p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4;
+  p.partial = b * p.chunks * 2 * c;
+  p.stat = 2 * b * groups;
+  return p;
+}
+
+template <class T>
+hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
+  const Plan p = plan(a.b, a.s, a.c, a.groups, false);
+  const int64_t per = a.c / a.groups, rows = a.b * a.groups;
+  if (p.way == kRows) {
+    if (per <= 512)
+      rows_kernel<T, 64, 1><<<dim3(uint32_t((rows + 3) / 4)), dim3(256), 0, st>>>(a, rows);
+    else if (per <= 1024)
+      rows_kernel<T, 64, 2><<<dim3(uint32_t((rows + 3) / 4)), dim3(256), 0, st>>>(a, rows);
+    else if (per <= 2048)
+      rows_kernel<T, 256, 1><<<dim3(uint32_t(rows)), dim3(256), 0, st>>>(a, rows);
+    else if (per <= 4096)
+      rows_kernel<T, 256, 2><<<dim3(uint32_t(rows)), dim3(256), 0, st>>>(a, rows);
+    else
+      rows_kernel<T, 256, 8><<<dim3(uint32_t(rows)), dim3(256), 0, st>>>(a, rows);
+    return hipGetLastError();
+  }
+  if (p.way == kBlock) {
+    block_kernel<T><<<dim3(uint32_t(p.tiles * a.b)), dim3(p.threads), p.lds, st>>>(a, p.groups, p.vectors,
+                                                                                      p.lanes_y);
+    return hipGetLastError();
+  }
+  float *partial = static_cast<float *>(a.workspace);
+  float *stat = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + up16(p.partial * 4));
+  const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
+  split_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, partial);
+  split_join_kernel<<<dim3(uint32_t(rows)), dim3(256), 0, st>>>(partial, a.s, p.chunk, int(p.chunks), a.c, int(per),
+                                                               a.eps, a.mean, a.rstd, stat);
+  split_write_kernel<T><<<grid, dim3(256), 0, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, stat);
   return hipGetLastError();
 }
+
 template <class T>
-hipError_t norm_grad(const dip_group_norm_grad_args &a, hipStream_t st) {
-  norm_grad_kernel<T><<<dim3(uint32_t(a.b * a.groups)), dim3(kThreads), 0, st>>>(a);
-  return hipGetLastError();
+hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
+  const Plan p = plan(a.b, a.s, a.c, a.groups, true);
+  const int64_t per = a.c / a.groups;
+  float *partial = static_cast<float *>(a.workspace);
+  float *sums = a.dgamma || a.dbeta ? partial : nullptr;
+  if (p.way == kSplit) {
+    float *mean = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + up16(p.partial * 4));
+    const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
+    split_grad_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, partial);
+    split_grad_join_kernel<T><<<dim3(uint32_t(a.groups)), dim3(256), 0, st>>>(
+        partial, a.b, a.s, int(p.chunks), a.c, int(per), static_cast<const T *>(a.gamma), static_cast<T *>(a.dgamma),
+        static_cast<T *>(a.dbeta), mean);
+    if (a.dx) split_grad_write_kernel<T><<<grid, dim3(256), 0, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, mean);
+    return hipGetLastError();
+  }
+  int64_t rows = a.b;
+  if (p.way == kRows) {
+    rows = p.row_blocks;
+    const dim3 grid(uint32_t(p.row_blocks), uint32_t(a.groups));
+    if (per <= 512)
+      rows_grad_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, sums);
+    else if (per <= 2048)
+      rows_grad_kernel<T, 256, 1><<<grid, dim3(256), 0, st>>>(a, sums);
+    else if (per <= 4096)
+      rows_grad_kernel<T, 256, 2><<<grid, dim3(256), 0, st>>>(a, sums);
+    else if (per <= 8192)
+      rows_grad_kernel<T, 256, 4><<<grid, dim3(256), 0, st>>>(a, sums);
+    else
+      rows_grad_kernel<T, 256, 8><<<grid, dim3(256), 0, st>>>(a, sums);
+  } else {
+    block_grad_kernel<T><<<dim3(uint32_t(p.tiles * a.b)), dim3(p.threads), p.lds, st>>>(
+        a, p.groups, p.vectors, p.lanes_y, sums);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !sums) return e;
+  return launch_sum_rows(SumRows{partial, rows, 2 * a.c, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
 }
 
 }  // namespace
 
-int64_t group_norm_workspace(const dip_group_norm_args &) { return 0; }
-int64_t group_norm_grad_workspace(const dip_group_norm_grad_args &a) { return up16(2 * a.b * a.c * 4); }
+int64_t group_norm_workspace(const dip_group_norm_args &a) {
+  return a.b > 0 && a.c > 0 ? plan(a.b, a.s, a.c, a.groups, false).bytes() : 0;
+}
+int64_t group_norm_grad_workspace(const dip_group_norm_grad_args &a) {
+  return a.b > 0 && a.c > 0 && a.s > 0 ? plan(a.b, a.s, a.c, a.groups, true).bytes() : 0;
+}
 
 hipError_t launch_group_norm(const dip_group_norm_args &a, hipStream_t st) {
-  return a.dtype == DIP_F32 ? norm<float>(a, st) : a.dtype == DIP_F16 ? norm<_Float16>(a, st) : norm<__bf16>(a, st);
+  return a.dtype == DIP_F32   ? forward<float>(a, st)
+         : a.dtype == DIP_F16 ? forward<_Float16>(a, st)
+                              : forward<__bf16>(a, st);
 }
 
 hipError_t launch_group_norm_grad(const dip_group_norm_grad_args &a, hipStream_t st) {
-  if (a.b > 0 && a.s > 0) {
-    const hipError_t e = a.dtype == DIP_F32   ? norm_grad<float>(a, st)
-                         : a.dtype == DIP_F16 ? norm_grad<_Float16>(a, st)
-                                              : norm_grad<__bf16>(a, st);
-    if (e != hipSuccess) return e;
-  }
-  const float *p = static_cast<const float *>(a.workspace);
-  const int64_t rows = a.s > 0 ? a.b : 0;
-  for (int j = 0; j < 2; ++j) {
-    void *out = j ? a.dbeta : a.dgamma;
-    if (!out) continue;
-    const hipError_t e = launch_sum_rows(p + j * a.b * a.c, rows, a.c, out, a.dtype, 0, st);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  if (a.b == 0 || a.s == 0)   // sums over nothing
+    return launch_sum_rows(SumRows{nullptr, 0, 0, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
+  return a.dtype == DIP_F32   ? backward<float>(a, st)
+         : a.dtype == DIP_F16 ? backward<_Float16>(a, st)
+                              : backward<__bf16>(a, st);
 }
 
 }  // namespace dipops

@@ -386,11 +386,12 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   // code; the others go eight columns by eight.
   constexpr int P = FN / 2;
   const int64_t col0 = n0 + wn + 8 * (lane / 16);
-  const bool whole = e.fast && m0 + wm + 16 * FM <= m && n0 + wn + 16 * FN <= n;
+  const bool whole = !e.out_f32 && !e.accumulate && m0 + wm + 16 * FM <= m && n0 + wn + 16 * FN <= n;
+  typedef typename Any8<T>::type VA;   // rows of any alignment
   V bias[P];
   if (KIND == kForward && whole && e.bias) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) bias[p] = reinterpret_cast<const V *>(static_cast<const T *>(e.bias) + col0)[4 * p];
+    for (int p = 0; p < P; ++p) bias[p] = reinterpret_cast<const VA *>(static_cast<const T *>(e.bias) + col0)[4 * p];
   }
 #pragma unroll 1
   for (int i = 0; i < FM; ++i) {
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
       if constexpr (KIND == kForward) {
         if (e.bias) each<P>([&](int p, int q) { v[p][q] += float(bias[p][q]); });
         if (e.pre) {
-          V *o = reinterpret_cast<V *>(static_cast<T *>(e.pre) + row * e.ldp + col0);
+          VA *o = reinterpret_cast<VA *>(static_cast<T *>(e.pre) + row * e.ldp + col0);
 #pragma unroll
           for (int p = 0; p < P; ++p) o[4 * p] = round8<T>(v[p]);
         }
@@ -420,14 +421,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
           for (int p = 0; p < P; ++p) drop8(e.drop, uint32_t(col0 >> 3) + 4 * p, uint32_t(row), v[p]);
         }
         if (e.residual) {
-          const V *o = reinterpret_cast<const V *>(static_cast<const T *>(e.residual) + row * e.ldr + col0);
+          const VA *o = reinterpret_cast<const VA *>(static_cast<const T *>(e.residual) + row * e.ldr + col0);
           V r[P];
 #pragma unroll
           for (int p = 0; p < P; ++p) r[p] = o[4 * p];
           each<P>([&](int p, int q) { v[p][q] += float(r[p][q]); });
         }
       }
-      V *o = reinterpret_cast<V *>(static_cast<T *>(e.out) + row * e.ldo + col0);
+      VA *o = reinterpret_cast<VA *>(static_cast<T *>(e.out) + row * e.ldo + col0);
 #pragma unroll
       for (int p = 0; p < P; ++p) o[4 * p] = round8<T>(v[p]);
     } else if (row < m) {
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
         const int64_t col = col0 + 32 * p;
         if (col >= n) continue;
         if constexpr (KIND == kPartial)
-          store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, true, v[p]);
+          store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, v[p]);
         else
           finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v[p]);
       }
@@ -452,10 +453,10 @@ __global__ __launch_bounds__(256) void join_kernel(int64_t m, int64_t n, Epilogu
   if (i >= all) return;
   const int64_t row = i / per, col = i % per * 8;
   float v[8];
-  load8(split.partial + row * split.n8 + col, 8, true, v);
+  load8(split.partial + row * split.n8 + col, 8, v);
   for (int s = 1; s < splits; ++s) {
     float q[8];
-    load8(split.partial + (int64_t(s) * m + row) * split.n8 + col, 8, true, q);
+    load8(split.partial + (int64_t(s) * m + row) * split.n8 + col, 8, q);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += q[j];
   }
@@ -490,18 +491,19 @@ hipError_t pick(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand
   }
 }
 
-// Copies rows to where the products can take them: 16-byte aligned, the stride
-// a multiple of 8, zeros in the columns up to it.
+// Copies one or two arrays to where the products can take them: 16-byte aligned,
+// the stride a multiple of 8, zeros in the columns up to it.  One launch for both.
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(const T *p, int64_t rows, int64_t cols, int64_t ld, T *out,
-                                                   int64_t ldo) {
-  const int64_t per = ldo / 8;
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= rows * per) return;
-  const int64_t row = i / per, col = i % per * 8;
+__global__ __launch_bounds__(256) void pack_kernel(PackJob a, PackJob b, uint32_t blocks_a) {
+  const bool second = blockIdx.x >= blocks_a;
+  const PackJob &j = second ? b : a;
+  const uint32_t per = uint32_t(j.ldo / 8);
+  const int64_t i = int64_t(blockIdx.x - (second ? blocks_a : 0)) * 256 + threadIdx.x;
+  if (i >= j.rows * per) return;
+  const int64_t row = i / per, col = (i - row * per) * 8;
   float v[8];
-  load8(p + row * ld + col, int(max(int64_t(0), min(int64_t(8), cols - col))), false, v);
-  store8(out + row * ldo + col, 8, true, v);
+  load8(static_cast<const T *>(j.p) + row * j.ld + col, int(min(int64_t(8), j.cols - col)), v);
+  store8(static_cast<T *>(j.out) + row * j.ldo + col, 8, v);
 }
 
 }  // namespace
@@ -557,15 +559,13 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
   return pick<_Float16, true, true>(m, n, k, a, b, e, plan, partial, stream);
 }
 
-hipError_t launch_pack(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld, void *out, int64_t ldo,
-                       hipStream_t stream) {
-  const dim3 grid(uint32_t((rows * (ldo / 8) + 255) / 256));
+hipError_t launch_pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t stream) {
+  const int64_t na = (a.rows * (a.ldo / 8) + 255) / 256, nb = (b.rows * (b.ldo / 8) + 255) / 256;
+  const dim3 grid(uint32_t(na + nb));
   if (dtype == DIP_BF16)
-    pack_kernel<<<grid, dim3(256), 0, stream>>>(static_cast<const __bf16 *>(p), rows, cols, ld,
-                                               static_cast<__bf16 *>(out), ldo);
+    pack_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, b, uint32_t(na));
   else
-    pack_kernel<<<grid, dim3(256), 0, stream>>>(static_cast<const _Float16 *>(p), rows, cols, ld,
-                                               static_cast<_Float16 *>(out), ldo);
+    pack_kernel<_Float16><<<grid, dim3(256), 0, stream>>>(a, b, uint32_t(na));
   return hipGetLastError();
 }
 

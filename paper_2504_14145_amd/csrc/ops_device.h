@@ -43,18 +43,24 @@ __device__ __forceinline__ void mfma16(f16x8 a, f16x8 b, f32x4 &c) {
 __device__ __forceinline__ void products_wait() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 __device__ __forceinline__ void products_done(f32x4 &a, f32x4 &b) { asm volatile("" : "+a"(a), "+a"(b)); }
 
-// Eight consecutive elements.  `vec`: their address is a multiple of 16 bytes
-// (wave-uniform by construction: it is a property of the array's base and
-// stride); else, or with fewer than 8 columns left, element by element.
+// Eight consecutive elements from any address aligned to its element (the
+// hardware takes vector accesses at such addresses, and a row of odd length
+// costs an extra cache line, not eight loads); `left` of them exist, the others
+// read as zero and are not written.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 template <class T>
-__device__ __forceinline__ void load8(const T *p, int left, bool vec, float (&v)[8]) {
-  if (vec && left >= 8) {
+struct Any8 {
+  typedef typename Vec8<T>::type type __attribute__((aligned(2)));
+};
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int left, float (&v)[8]) {
+  if (left >= 8) {
     if constexpr (sizeof(T) == 2) {
-      const typename Vec8<T>::type t = *reinterpret_cast<const typename Vec8<T>::type *>(p);
+      const typename Vec8<T>::type t = *reinterpret_cast<const typename Any8<T>::type *>(p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = float(t[i]);
     } else {
-      const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+      const f32x4 a = reinterpret_cast<const f32x4_any *>(p)[0], b = reinterpret_cast<const f32x4_any *>(p)[1];
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
     }
@@ -71,16 +77,16 @@ __device__ __forceinline__ typename Vec8<T>::type round8(const float (&v)[8]) {
   return t;
 }
 template <class T>
-__device__ __forceinline__ void store8(T *p, int left, bool vec, const float (&v)[8]) {
-  if (vec && left >= 8) {
+__device__ __forceinline__ void store8(T *p, int left, const float (&v)[8]) {
+  if (left >= 8) {
     if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<typename Vec8<T>::type *>(p) = round8<T>(v);
+      *reinterpret_cast<typename Any8<T>::type *>(p) = round8<T>(v);
     } else {
       f32x4 a, b;
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[i] = v[i], b[i] = v[4 + i];
-      reinterpret_cast<f32x4 *>(p)[0] = a;
-      reinterpret_cast<f32x4 *>(p)[1] = b;
+      reinterpret_cast<f32x4_any *>(p)[0] = a;
+      reinterpret_cast<f32x4_any *>(p)[1] = b;
     }
   } else {
 #pragma unroll
@@ -175,9 +181,7 @@ struct Epilogue {
   int64_t ldr, ldo, ldp;
   Drop drop;
   int32_t act;
-  uint8_t vec_bias, vec_res, vec_out, vec_pre;   // 16-byte aligned rows
   uint8_t out_f32, accumulate;
-  uint8_t fast;   // every array aligned, a plain output of the operands' type
 };
 
 // Eight consecutive columns of one row; `left`: columns up to the matrix's end.
@@ -186,11 +190,11 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t row, int64_t 
                                         float (&v)[8]) {
   if (e.bias) {
     float b[8];
-    load8(static_cast<const T *>(e.bias) + col, left, e.vec_bias, b);
+    load8(static_cast<const T *>(e.bias) + col, left, b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += b[i];
   }
-  if (e.pre) store8(static_cast<T *>(e.pre) + row * e.ldp + col, left, e.vec_pre, v);
+  if (e.pre) store8(static_cast<T *>(e.pre) + row * e.ldp + col, left, v);
   if (e.act != DIP_ACT_NONE) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = act_of(v[i], e.act);
@@ -198,7 +202,7 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t row, int64_t 
   if (e.drop.drop_of) drop8(e.drop, uint32_t(col >> 3), uint32_t(row), v);
   if (e.residual) {
     float r[8];
-    load8(static_cast<const T *>(e.residual) + row * e.ldr + col, left, e.vec_res, r);
+    load8(static_cast<const T *>(e.residual) + row * e.ldr + col, left, r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += r[i];
   }
@@ -206,20 +210,20 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t row, int64_t 
     float *o = static_cast<float *>(e.out) + row * e.ldo + col;
     if (e.accumulate) {
       float r[8];
-      load8(o, left, e.vec_out, r);
+      load8(o, left, r);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
-    store8(o, left, e.vec_out, v);
+    store8(o, left, v);
   } else {
     T *o = static_cast<T *>(e.out) + row * e.ldo + col;
     if (e.accumulate) {
       float r[8];
-      load8(o, left, e.vec_out, r);
+      load8(o, left, r);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
-    store8(o, left, e.vec_out, v);
+    store8(o, left, v);
   }
 }
 

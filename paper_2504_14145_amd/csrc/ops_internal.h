@@ -31,9 +31,14 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
                        hipStream_t stream);
 // rows x cols from p to out (16-byte aligned, stride ldo a multiple of 8), zeros
-// in columns cols .. ldo - 1
-hipError_t launch_pack(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld, void *out,
-                       int64_t ldo, hipStream_t stream);
+// in columns cols .. ldo - 1; no rows: nothing
+struct PackJob {
+  const void *p = nullptr;
+  int64_t rows = 0, cols = 0, ld = 0;
+  void *out = nullptr;
+  int64_t ldo = 8;
+};
+hipError_t launch_pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t stream);
 
 // g = D(dy) act'(pre) to out (ld a multiple of 8, padding columns zero; null:
 // not wanted), and its column sums before rounding to partial[row_chunks][n]
@@ -44,7 +49,6 @@ struct GradIn {
   int64_t ldy, ldp;
   Drop drop;
   int32_t act;
-  uint8_t vec_dy, vec_pre;
   void *out;
   int64_t ldo;
   float *partial;
@@ -52,9 +56,16 @@ struct GradIn {
 };
 int32_t grad_row_chunks(int64_t m, int64_t n);
 hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream);
-// out[c] (+)= sum over the rows of partial[rows][cols], in row order
-hipError_t launch_sum_rows(const float *partial, int64_t rows, int64_t cols, void *out,
-                           int out_dtype, int accumulate, hipStream_t stream);
+// out0[j] (+)= the sum over the rows of partial[rows][ld] of column j, and out1[j]
+// of column c + j, j < c, in an order that depends on the sizes alone; either may
+// be null.
+struct SumRows {
+  const float *partial;
+  int64_t rows, ld, c;
+  void *out0, *out1;
+  int accumulate;
+};
+hipError_t launch_sum_rows(const SumRows &s, int out_dtype, hipStream_t stream);
 
 hipError_t launch_dropout_add(int dtype, int64_t m, int64_t n, const void *x, int64_t ldx,
                               const void *residual, int64_t ldr, const Drop &drop, void *y,
