@@ -1,6 +1,7 @@
 // kern_elementwise.hip -- dropout, the gradient before the matrix products, and
 // sums over rows.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops_internal.h"
 
@@ -75,22 +76,41 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   const int left = int(max(int64_t(0), min(int64_t(8), g.n - col)));
   float sum[8] = {};
   if (left > 0) {
-    for (int64_t row = r0 + ty; row < r1; row += 8) {
-      float v[8], z[8];
-      load8(static_cast<const T *>(g.dy) + row * g.ldy + col, left, v);
-      if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row), v);
-      if (g.pre) {
-        load8(static_cast<const T *>(g.pre) + row * g.ldp + col, left, z);
+    const T *dy = static_cast<const T *>(g.dy) + col, *pre = static_cast<const T *>(g.pre) + col;
+    // U rows at a time, their loads first
+    auto rows = [&](int64_t row, auto u_) {
+      constexpr int U = decltype(u_)::value;
+      float v[U][8], z[U][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= act_slope(z[j], g.act);
+      for (int u = 0; u < U; ++u) load8(dy + (row + 8 * u) * g.ldy, left, v[u]);
+      if (g.pre) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load8(pre + (row + 8 * u) * g.ldp, left, z[u]);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j >= left) v[j] = 0.f;
+      for (int u = 0; u < U; ++u) {
+        if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row + 8 * u), v[u]);
+        if (g.act == DIP_ACT_GELU) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += v[j];
-      if (g.out) store8(static_cast<T *>(g.out) + row * g.ldo + col, 8, v);
-    }
+          for (int j = 0; j < 8; ++j) v[u][j] *= act_slope(z[u][j], DIP_ACT_GELU);
+        } else if (g.act == DIP_ACT_SILU) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[u][j] *= act_slope(z[u][j], DIP_ACT_SILU);
+        } else if (g.act == DIP_ACT_RELU) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[u][j] *= act_slope(z[u][j], DIP_ACT_RELU);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j >= left) v[u][j] = 0.f;
+          sum[j] += v[u][j];
+        }
+        if (g.out) store8(static_cast<T *>(g.out) + (row + 8 * u) * g.ldo + col, 8, v[u]);
+      }
+    };
+    int64_t row = r0 + ty;
+    for (; row + 24 < r1; row += 32) rows(row, std::integral_constant<int, 4>{});
+    for (; row < r1; row += 8) rows(row, std::integral_constant<int, 1>{});
   }
   if (!g.partial) return;
 #pragma unroll

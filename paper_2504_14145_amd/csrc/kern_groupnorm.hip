@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void rows_kernel(dip_group_norm_args a, int64_
 // the sums of dgamma and dbeta of its channels on the way: partial[j][2][c].
 template <class T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void rows_grad_kernel(dip_group_norm_grad_args a, float *partial) {
-  __shared__ float s[2 * 2 * 4];
+  __shared__ float s[2 * 2 * THREADS / 64];
   int turn = 0, turn2 = 0;
   const int t = threadIdx.x, per = int(a.c / a.groups);
   const uint32_t g = blockIdx.y;
@@ -122,33 +122,39 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(dip_group_norm_grad_
 #pragma unroll
   for (int j = 0; j < NV; ++j) affine.get(c0 + (t + j * THREADS) * 8, per - (t + j * THREADS) * 8, ga[j], be[j]);
   const float inv = 1.f / float(per);
-  for (int64_t i = blockIdx.x; i < a.b; i += gridDim.x) {
-    const float mean = a.mean[i * a.groups + g], rstd = a.rstd[i * a.groups + g];
+  // the next sample's row is asked for before this one's sums are waited for
+  float xn[NV][8], dn[NV][8];
+  auto fetch = [&](int64_t i) __attribute__((always_inline)) {
     const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c0;
     const T *dy = static_cast<const T *>(a.dy) + i * a.dy_sb + c0;
-    float xh[NV][8], h[NV][8];
-    float m1 = 0.f, m2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (t + j * THREADS) * 8;
-      load8(x + c, per - c, xh[j]);
-      load8(dy + c, per - c, h[j]);   // zeros beyond the row
+      load8(x + c, per - c, xn[j]);
+      load8(dy + c, per - c, dn[j]);   // zeros beyond the row
     }
+  };
+  if (int64_t(blockIdx.x) < a.b) fetch(blockIdx.x);
+  for (int64_t i = blockIdx.x; i < a.b; i += gridDim.x) {
+    const float mean = a.mean[i * a.groups + g], rstd = a.rstd[i * a.groups + g];
+    float xh[NV][8], h[NV][8];
+    float m1 = 0.f, m2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        xh[j][q] = (xh[j][q] - mean) * rstd;
-        const float v = a.act == DIP_ACT_NONE ? h[j][q] : h[j][q] * act_slope(xh[j][q] * ga[j][q] + be[j][q], a.act);
+        xh[j][q] = (xn[j][q] - mean) * rstd;
+        const float v = a.act == DIP_ACT_NONE ? dn[j][q] : dn[j][q] * act_slope(xh[j][q] * ga[j][q] + be[j][q], a.act);
         sg[j][q] += v * xh[j][q];
         sb[j][q] += v;
         h[j][q] = v * ga[j][q];
         m1 += h[j][q];
         m2 += h[j][q] * xh[j][q];
       }
+    if (i + gridDim.x < a.b) fetch(i + gridDim.x);
     if (!a.dx) continue;
     m1 = block_sum<THREADS>(m1, s, turn) * inv;
-    m2 = block_sum<THREADS>(m2, s + 2 * 4, turn2) * inv;
+    m2 = block_sum<THREADS>(m2, s + 2 * THREADS / 64, turn2) * inv;
     T *dx = static_cast<T *>(a.dx) + i * a.dx_sb + c0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -379,6 +385,8 @@ __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int g
   const int64_t i = blockIdx.x / tiles, c0 = int64_t(g0) * per, c = c0 + l.vx * 8;
   const int left = slab - l.vx * 8;
   const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c;
+  Channels ch;
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
   float k[8], u[8], v[8];
   moments(x, a.x_ss, left, l, 0, a.s, k, u, v);
   channel_sums(l, vectors, u, v, s);
@@ -412,10 +420,8 @@ __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int g
   }
   __syncthreads();
   if (left <= 0) return;
-  Channels ch;
   of_groups(stat, l.vx * 8, per, left, ch.mean);
   of_groups(stat + groups, l.vx * 8, per, left, ch.rstd);
-  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
   write_rows(x, a.x_ss, static_cast<T *>(a.y) + i * a.y_sb + c, a.y_ss, left, l, 0, a.s, ch, a.act);
 }
 
@@ -506,6 +512,19 @@ __global__ __launch_bounds__(256) void split_sums_kernel(dip_group_norm_args a, 
   store8(p + a.c, left, v);
 }
 
+// A workgroup's threads over [chunks][per] values of one sample and group, whole
+// runs of channels side by side: f(chunk, channel), eight of a thread's at once.
+template <class F>
+__device__ __forceinline__ void over_chunks(int chunks, int per, F &&f) {
+  const int side = min(per, 256), rows = 256 / side;
+  const int tx = threadIdx.x % side, ty = threadIdx.x / side;
+  if (ty >= rows) return;
+  for (int j = tx; j < per; j += side) {
+#pragma unroll 8
+    for (int q = ty; q < chunks; q += rows) f(q, j);
+  }
+}
+
 // One workgroup a sample and group joins its chunks' channels.
 __global__ __launch_bounds__(256) void split_join_kernel(const float *partial, int64_t s_all, int64_t chunk,
                                                          int chunks, int64_t c, int per, float eps, float *mean,
@@ -514,23 +533,21 @@ __global__ __launch_bounds__(256) void split_join_kernel(const float *partial, i
   int turn = 0;
   const uint32_t groups = uint32_t(c / per), i = blockIdx.x / groups, g = blockIdx.x % groups;
   const float *p = partial + int64_t(i) * chunks * 2 * c + int64_t(g) * per;
-  const int all = chunks * per;
-  const float total = float(s_all) * float(per);
+  const float total = float(s_all) * float(per), full = float(chunk);
+  const float rest = float(s_all - chunk * (chunks - 1));   // rows of the last chunk
   // every value times its count, about the first chunk's first channel
   const float k = p[0];
   float u = 0.f;
-  for (int j = threadIdx.x; j < all; j += 256) {
-    const int q = j / per;
-    u += (p[int64_t(q) * 2 * c + j % per] - k) * float(min(chunk, s_all - chunk * q));
-  }
+  over_chunks(chunks, per, [&](int q, int j) {
+    u += (p[int64_t(q) * 2 * c + j] - k) * (q + 1 < chunks ? full : rest);
+  });
   const float m = k + block_sum<256>(u, s, turn) / total;
   u = 0.f;
-  for (int j = threadIdx.x; j < all; j += 256) {
-    const int q = j / per;
-    const float *v = p + int64_t(q) * 2 * c + j % per;
+  over_chunks(chunks, per, [&](int q, int j) {
+    const float *v = p + int64_t(q) * 2 * c + j;
     const float d = v[0] - m;
-    u += v[c] + d * d * float(min(chunk, s_all - chunk * q));
-  }
+    u += v[c] + d * d * (q + 1 < chunks ? full : rest);
+  });
   const float r = 1.f / sqrtf(block_sum<256>(u, s, turn) / total + eps);
   if (threadIdx.x == 0) {
     stat[blockIdx.x] = m;
@@ -582,51 +599,55 @@ __global__ __launch_bounds__(256) void split_grad_sums_kernel(dip_group_norm_gra
   store8(p + a.c, left, v);
 }
 
-// One workgroup a group: the group's means of h and h xh of every sample to
-// mean[2][b][groups], and its channels' dgamma and dbeta over all samples.  A
-// wave takes every fourth channel, its lanes the chunks.
+// One workgroup a sample and group: its channels' sums over the chunks to
+// sums[sample][2][c], and the group's means of h and h xh to mean[2][b][groups].
 template <class T>
-__global__ __launch_bounds__(256) void split_grad_join_kernel(const float *partial, int64_t b, int64_t s_all,
-                                                              int chunks, int64_t c, int per, const T *gamma,
-                                                              T *dgamma, T *dbeta, float *mean) {
-  __shared__ float s[2][4];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, groups = int(c / per);
-  const int64_t c0 = int64_t(blockIdx.x) * per;
-  const float inv = 1.f / (float(s_all) * float(per));
-  for (int64_t i = 0; i < b; ++i) {
-    float m1 = 0.f, m2 = 0.f;
-    for (int j = wave; j < per; j += 4) {
-      float u = 0.f, v = 0.f;
-      for (int q = lane; q < chunks; q += 64) {
-        const float *p = partial + (i * chunks + q) * 2 * c + c0 + j;
-        u += p[0];
-        v += p[c];
+__global__ __launch_bounds__(256) void split_grad_join_kernel(const float *partial, int64_t s_all, int chunks,
+                                                              int64_t c, int per, const T *gamma, float *sums,
+                                                              float *mean) {
+  __shared__ float s[2][256];
+  __shared__ float sw[2 * 2 * 4];
+  int turn = 0, turn2 = 0;
+  const uint32_t groups = uint32_t(c / per), i = blockIdx.x / groups, g = blockIdx.x % groups;
+  const int64_t c0 = int64_t(g) * per;
+  const float *p = partial + int64_t(i) * chunks * 2 * c + c0;
+  const int side = min(per, 256), rows = 256 / side;
+  const int tx = threadIdx.x % side, ty = threadIdx.x / side;
+  float m1 = 0.f, m2 = 0.f;
+  for (int j0 = 0; j0 < per; j0 += side) {
+    const int j = j0 + tx;
+    float u = 0.f, v = 0.f;
+    if (ty < rows && j < per) {
+#pragma unroll 8
+      for (int q = ty; q < chunks; q += rows) {
+        u += p[int64_t(q) * 2 * c + j];
+        v += p[int64_t(q) * 2 * c + c + j];
+      }
+    }
+    __syncthreads();
+    s[0][threadIdx.x] = u;
+    s[1][threadIdx.x] = v;
+    __syncthreads();
+    if (ty == 0 && j < per) {
+      for (int r = 1; r < rows; ++r) {
+        u += s[0][r * side + tx];
+        v += s[1][r * side + tx];
+      }
+      if (sums) {
+        sums[int64_t(i) * 2 * c + c0 + j] = u;
+        sums[int64_t(i) * 2 * c + c + c0 + j] = v;
       }
       const float w = gamma ? float(gamma[c0 + j]) : 1.f;
-      m2 += w * wave_sum(u);
-      m1 += w * wave_sum(v);
+      m2 += w * u;
+      m1 += w * v;
     }
-    if (lane == 0) s[0][wave] = m1, s[1][wave] = m2;
-    __syncthreads();
-    if (threadIdx.x < 2) {
-      const float *p = s[threadIdx.x];
-      mean[(threadIdx.x * b + i) * groups + blockIdx.x] = ((p[0] + p[1]) + (p[2] + p[3])) * inv;
-    }
-    __syncthreads();
   }
-  for (int j = wave; j < per; j += 4) {
-    float u = 0.f, v = 0.f;
-    for (int64_t q = lane; q < b * chunks; q += 64) {
-      const float *p = partial + q * 2 * c + c0 + j;
-      u += p[0];
-      v += p[c];
-    }
-    u = wave_sum(u);
-    v = wave_sum(v);
-    if (lane == 0) {
-      if (dgamma) dgamma[c0 + j] = T(u);
-      if (dbeta) dbeta[c0 + j] = T(v);
-    }
+  const float inv = 1.f / (float(s_all) * float(per));
+  m1 = block_sum<256>(m1, sw, turn) * inv;
+  m2 = block_sum<256>(m2, sw + 2 * 4, turn2) * inv;
+  if (threadIdx.x == 0) {
+    mean[blockIdx.x] = m1;
+    mean[gridDim.x + blockIdx.x] = m2;
   }
 }
 
@@ -658,8 +679,10 @@ struct Plan {
   int64_t chunk = 0, chunks = 1;                                       // split
   int64_t row_blocks = 1;                                              // rows' gradient
   size_t lds = 0;
-  int64_t partial = 0, stat = 0;   // floats
-  int64_t bytes() const { return up16(partial * 4) + up16(stat * 4); }
+  int64_t partial = 0, stat = 0, sums = 0;   // floats
+  int64_t stat_at() const { return up16(partial * 4); }
+  int64_t sums_at() const { return stat_at() + up16(stat * 4); }
+  int64_t bytes() const { return sums_at() + up16(sums * 4); }
 };
 
 int pow2_at_most(int64_t n) {
@@ -701,14 +724,15 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, bool grad) {
   p.tiles = int((cv + 255) / 256);
   p.vectors = int((cv + p.tiles - 1) / p.tiles);
   p.lanes_y = pow2_at_most(256 / p.vectors);
-  // chunks for about eight workgroups a CU, of at least eight rows a thread
-  const int64_t most = std::max<int64_t>(1, s / (int64_t(p.lanes_y) * 8));
-  p.chunks = std::max<int64_t>(1, std::min<int64_t>(most, 2048 / std::max<int64_t>(1, b * p.tiles)));
+  // chunks for about four workgroups a CU, of at least two rows a thread
+  const int64_t most = std::max<int64_t>(1, s / (int64_t(p.lanes_y) * 2));
+  p.chunks = std::max<int64_t>(1, std::min<int64_t>(most, 1024 / std::max<int64_t>(1, b * p.tiles)));
   p.chunk = (s + p.chunks - 1) / p.chunks;
   p.chunks = (s + p.chunk - 1) / p.chunk;
   p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4;
   p.partial = b * p.chunks * 2 * c;
   p.stat = 2 * b * groups;
+  p.sums = grad ? b * 2 * c : 0;
   return p;
 }
 
@@ -735,7 +759,7 @@ hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
     return hipGetLastError();
   }
   float *partial = static_cast<float *>(a.workspace);
-  float *stat = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + up16(p.partial * 4));
+  float *stat = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
   const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
   split_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, partial);
   split_join_kernel<<<dim3(uint32_t(rows)), dim3(256), 0, st>>>(partial, a.s, p.chunk, int(p.chunks), a.c, int(per),
@@ -751,14 +775,16 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
   float *partial = static_cast<float *>(a.workspace);
   float *sums = a.dgamma || a.dbeta ? partial : nullptr;
   if (p.way == kSplit) {
-    float *mean = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + up16(p.partial * 4));
+    float *mean = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
     const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
     split_grad_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, partial);
-    split_grad_join_kernel<T><<<dim3(uint32_t(a.groups)), dim3(256), 0, st>>>(
-        partial, a.b, a.s, int(p.chunks), a.c, int(per), static_cast<const T *>(a.gamma), static_cast<T *>(a.dgamma),
-        static_cast<T *>(a.dbeta), mean);
+    if (sums) sums = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.sums_at());
+    split_grad_join_kernel<T><<<dim3(uint32_t(a.b * a.groups)), dim3(256), 0, st>>>(
+        partial, a.s, int(p.chunks), a.c, int(per), static_cast<const T *>(a.gamma), sums, mean);
     if (a.dx) split_grad_write_kernel<T><<<grid, dim3(256), 0, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, mean);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !sums) return e;
+    return launch_sum_rows(SumRows{sums, a.b, 2 * a.c, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
   }
   int64_t rows = a.b;
   if (p.way == kRows) {
@@ -769,11 +795,11 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
     else if (per <= 2048)
       rows_grad_kernel<T, 256, 1><<<grid, dim3(256), 0, st>>>(a, sums);
     else if (per <= 4096)
-      rows_grad_kernel<T, 256, 2><<<grid, dim3(256), 0, st>>>(a, sums);
+      rows_grad_kernel<T, 512, 1><<<grid, dim3(512), 0, st>>>(a, sums);
     else if (per <= 8192)
-      rows_grad_kernel<T, 256, 4><<<grid, dim3(256), 0, st>>>(a, sums);
+      rows_grad_kernel<T, 512, 2><<<grid, dim3(512), 0, st>>>(a, sums);
     else
-      rows_grad_kernel<T, 256, 8><<<grid, dim3(256), 0, st>>>(a, sums);
+      rows_grad_kernel<T, 512, 4><<<grid, dim3(512), 0, st>>>(a, sums);
   } else {
     block_grad_kernel<T><<<dim3(uint32_t(p.tiles * a.b)), dim3(p.threads), p.lds, st>>>(
         a, p.groups, p.vectors, p.lanes_y, sums);

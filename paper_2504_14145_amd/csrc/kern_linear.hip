@@ -393,6 +393,15 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
     for (int p = 0; p < P; ++p) bias[p] = reinterpret_cast<const VA *>(static_cast<const T *>(e.bias) + col0)[4 * p];
   }
+  // the residual's rows are asked for one round ahead
+  V r[P];
+  auto residual = [&](int i) __attribute__((always_inline)) {
+    const VA *o = reinterpret_cast<const VA *>(static_cast<const T *>(e.residual) +
+                                               (m0 + wm + 16 * i + lane % 16) * e.ldr + col0);
+#pragma unroll
+    for (int p = 0; p < P; ++p) r[p] = o[4 * p];
+  };
+  if (KIND == kForward && whole && e.residual) residual(0);
 #pragma unroll 1
   for (int i = 0; i < FM; ++i) {
     float v[P][8];
@@ -421,11 +430,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
           for (int p = 0; p < P; ++p) drop8(e.drop, uint32_t(col0 >> 3) + 4 * p, uint32_t(row), v[p]);
         }
         if (e.residual) {
-          const VA *o = reinterpret_cast<const VA *>(static_cast<const T *>(e.residual) + row * e.ldr + col0);
-          V r[P];
-#pragma unroll
-          for (int p = 0; p < P; ++p) r[p] = o[4 * p];
           each<P>([&](int p, int q) { v[p][q] += float(r[p][q]); });
+          if (i + 1 < FM) residual(i + 1);
         }
       }
       VA *o = reinterpret_cast<VA *>(static_cast<T *>(e.out) + row * e.ldo + col0);
@@ -523,7 +529,7 @@ GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k) {
     int64_t side, slots;
     double step_us, fixed_us;
   };
-  constexpr Shape shapes[] = {{256, 256, 1.35, 6.0}, {128, 512, 0.75, 4.0}, {128, 256, 0.45, 3.5}};
+  constexpr Shape shapes[] = {{256, 256, 1.35, 8.0}, {128, 512, 0.75, 4.0}, {128, 256, 0.45, 3.5}};
   const int64_t steps = (k + kStep - 1) / kStep;
   GemmPlan best;
   double least = 0;

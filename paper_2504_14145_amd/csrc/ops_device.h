@@ -97,20 +97,27 @@ __device__ __forceinline__ void store8(T *p, int left, const float (&v)[8]) {
 
 // ------------------------------------------------------------ activations
 
-// 1 / (1 + exp(-z)) with the hardware's exponential and reciprocal: within 1e-6
-// of the value for the z at which an output of it is not rounded to 0 or 1.
-__device__ __forceinline__ float logistic(float z) {
-  return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+// 1 / (1 + 2^t) with the hardware's exponential and reciprocal: within 1e-6 of
+// the value for the t at which an output of it is not rounded to 0 or 1.
+__device__ __forceinline__ float logistic2(float t) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t));
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGeluA = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGeluC = 0.044715f;
+
+// the logistic function's argument of each, times -log2 e: z, and 2 u of GELU
+__device__ __forceinline__ float silu_arg(float z) { return -kLog2e * z; }
+__device__ __forceinline__ float gelu_arg(float z) {
+  return z * (z * z * (-2.f * kLog2e * kGeluA * kGeluC) - 2.f * kLog2e * kGeluA);
+}
 
 __device__ __forceinline__ float act_of(float z, int act) {
   switch (act) {
     case DIP_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-    case DIP_ACT_SILU: return z * logistic(z);
-    case DIP_ACT_GELU: return z * logistic(2.f * kGeluA * z * (1.f + kGeluC * z * z));
+    case DIP_ACT_SILU: return z * logistic2(silu_arg(z));
+    case DIP_ACT_GELU: return z * logistic2(gelu_arg(z));
     default: return z;
   }
 }
@@ -118,13 +125,13 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   switch (act) {
     case DIP_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
     case DIP_ACT_SILU: {
-      const float e = logistic(z);
+      const float e = logistic2(silu_arg(z));
       return e * (1.f + z * (1.f - e));
     }
     case DIP_ACT_GELU: {
       if (fabsf(z) > 12.f) return z > 0.f ? 1.f : 0.f;   // e is 0 or 1 there, z^2 may overflow
-      const float e = logistic(2.f * kGeluA * z * (1.f + kGeluC * z * z));
-      return e * (1.f + z * (1.f - e) * 2.f * kGeluA * (1.f + 3.f * kGeluC * z * z));
+      const float e = logistic2(gelu_arg(z));
+      return e * (1.f + z * (1.f - e) * (2.f * kGeluA + 6.f * kGeluA * kGeluC * z * z));
     }
     default: return 1.f;
   }

@@ -13,7 +13,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import DipSimError, _check, load
+from . import E_CAPACITY, _check, load
 
 F32, F16, BF16 = 0, 1, 2
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
@@ -81,12 +81,13 @@ class _GroupNormGrad(ctypes.Structure):
 
 _lib = None
 _torch = None
+_raw_stream = None   # device index -> handle of torch's current stream
 _types = {}
 
 
 def _load():
     """The library with the operators' signatures, and torch."""
-    global _lib, _torch
+    global _lib, _torch, _raw_stream
     if _lib is None:
         import torch
         lib = load()
@@ -101,6 +102,8 @@ def _load():
                                         ctypes.POINTER(Dropout), _vp, _i64, _vp]
         lib.dip_dropout_add.restype = ctypes.c_int
         _types.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda index: torch.cuda.current_stream(index).cuda_stream)
         _torch, _lib = torch, lib
     return _lib
 
@@ -114,64 +117,85 @@ def _need(ok: bool, what: str):
 
 
 def _act(name) -> int:
-    _need(name in ACTS, f"unknown activation {name!r}: one of {', '.join(ACTS)}")
-    return ACTS[name]
+    code = ACTS.get(name)
+    if code is None:
+        raise ValueError(f"unknown activation {name!r}: one of {', '.join(ACTS)}")
+    return code
+
+
+def _refuse(t, shape, dtype, device, name):
+    if not isinstance(t, _torch.Tensor):
+        raise ValueError(f"{name}: want a tensor, got {type(t).__name__}")
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name}: want {tuple(shape)} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    raise ValueError(f"{name}: the last dimension has to be contiguous")
+
+
+_NONE = (None, 0)
 
 
 def _matrix(t, shape, dtype, device, name):
-    """A [rows, cols] tensor as (address, leading stride)."""
-    _need(t.shape == shape and t.dtype == dtype and t.device == device,
-          f"{name}: want {tuple(shape)} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    ld, one = t.stride()
-    _need(one == 1 or shape[1] <= 1, f"{name}: the last dimension has to be contiguous")
+    """A [rows, cols] tensor as (address, leading stride); (None, 0) for None."""
+    if t is None:
+        return _NONE
+    try:
+        ld, one = t.stride()
+        ok = t.shape == shape and t.dtype is dtype and t.device == device and (one == 1 or shape[1] <= 1)
+    except (AttributeError, ValueError):
+        ok = False
+    if not ok:
+        _refuse(t, shape, dtype, device, name)
     return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
 
 
 def _vector(t, n, dtype, device, name):
     if t is None:
         return None
-    _need(t.shape == (n,) and t.dtype == dtype and t.device == device and t.is_contiguous(),
-          f"{name}: want a contiguous ({n},) {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if not (t.shape == (n,) and t.dtype is dtype and t.device == device and t.is_contiguous()):
+        _refuse(t, (n,), dtype, device, name)
     return t.data_ptr()
 
 
 def _type(t, name):
-    _need(t.is_cuda, f"{name}: want a device tensor, got {t.device}")
+    _need(isinstance(t, _torch.Tensor) and t.is_cuda, f"{name}: want a device tensor")
     code = _types.get(t.dtype)
-    _need(code is not None, f"{name}: {t.dtype} is not float32, float16 or bfloat16")
+    if code is None:
+        raise ValueError(f"{name}: {t.dtype} is not float32, float16 or bfloat16")
     return code
 
 
 def _call(name, a, device, stream, used):
-    """Workspace, launch on the tensors' device, and its check."""
-    lib = _load()
-    with _torch.cuda.device(device):
-        need = getattr(lib, name + "_workspace")(ctypes.byref(a))
-        if need < 0:
-            raise DipSimError(int(need), name)
-        s, other = _stream(stream, device)
-        if need:
-            ws = _torch.empty(need, dtype=_torch.uint8, device=device)
-            a.workspace, a.workspace_bytes = ws.data_ptr(), need
-            used = used + (ws,)
-        _check(getattr(lib, name)(ctypes.byref(a), s), name)
-    _keep(other, used)
+    """Launch on the tensors' device, with a workspace where one is needed."""
+    if device.index != _torch.cuda.current_device():
+        with _torch.cuda.device(device):
+            return _call(name, a, device, stream, used)
+    run = getattr(_lib, name)
+    handle, other = _stream(stream, device)
+    code = run(ctypes.byref(a), handle)
+    if code == E_CAPACITY:
+        need = getattr(_lib, name + "_workspace")(ctypes.byref(a))
+        ws = _torch.empty(need, dtype=_torch.uint8, device=device)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), need
+        used = (*used, ws)
+        code = run(ctypes.byref(a), handle)
+    if code:
+        _check(code, name)
+    if other is not None:
+        _keep(other, used)
 
 
 def _stream(stream, device):
     """(its handle, the stream itself where it is not the current one)"""
-    current = _torch.cuda.current_stream(device)
+    current = _raw_stream(device.index)
     if stream is None:
-        return current.cuda_stream, None
+        return current, None
     handle = getattr(stream, "cuda_stream", stream)
-    return handle, None if handle == current.cuda_stream else stream
+    return handle, None if handle == current else stream
 
 
 def _keep(stream, tensors):
     """Memory that torch's allocator gave to the current stream and that another
     one works on is not given out again before that one has passed."""
-    if stream is None:
-        return
     if not isinstance(stream, _torch.cuda.Stream):
         stream = _torch.cuda.ExternalStream(stream)
     for t in tensors:
@@ -193,10 +217,10 @@ def linear(x, w, bias=None, act="none", dropout=None, residual=None, pre=None, o
         out = _torch.empty((m, n), dtype=dt, device=dev)
     a = _Linear(m, n, k, code, _act(act), *_matrix(x, (m, k), dt, dev, "x"),
                 *_matrix(w, (n, k), dt, dev, "w"), _vector(bias, n, dt, dev, "bias"),
-                *(_matrix(residual, (m, n), dt, dev, "residual") if residual is not None else (None, 0)),
+                *_matrix(residual, (m, n), dt, dev, "residual"),
                 dropout if dropout is not None else _NO_DROP,
                 *_matrix(out, (m, n), dt, dev, "out"),
-                *(_matrix(pre, (m, n), dt, dev, "pre") if pre is not None else (None, 0)), None, 0)
+                *_matrix(pre, (m, n), dt, dev, "pre"), None, 0)
     _call("dip_linear", a, dev, stream, (x, w, bias, residual, pre, out))
     return out
 
@@ -227,10 +251,10 @@ def linear_backward(dy, x, w, act="none", dropout=None, pre=None, bias=True, nee
     dx, dw, db = dx if need_dx else None, dw if need_dw else None, db if bias else None
     a = _LinearGrad(m, n, k, code, _act(act), *_matrix(dy, (m, n), dt, dev, "dy"),
                     *_matrix(x, (m, k), dt, dev, "x"), *_matrix(w, (n, k), dt, dev, "w"),
-                    *(_matrix(pre, (m, n), dt, dev, "pre") if act != "none" else (None, 0)),
+                    *_matrix(pre if act != "none" else None, (m, n), dt, dev, "pre"),
                     dropout if dropout is not None else _NO_DROP,
-                    *(_matrix(dx, (m, k), dt, dev, "dx") if dx is not None else (None, 0)),
-                    *(_matrix(dw, (n, k), gt, dev, "dw") if dw is not None else (None, 0)),
+                    *_matrix(dx, (m, k), dt, dev, "dx"),
+                    *_matrix(dw, (n, k), gt, dev, "dw"),
                     _vector(db, n, gt, dev, "db"), _types[gt], int(bool(accumulate)), None, 0)
     _call("dip_linear_grad", a, dev, stream, (dy, x, w, pre, dx, dw, db))
     return dx, dw, db
@@ -246,22 +270,31 @@ def dropout_add(x, dropout, residual=None, out=None, stream=None):
     if out is None:
         out = _torch.empty((m, n), dtype=dt, device=dev)
     px, ldx = _matrix(x, (m, n), dt, dev, "x")
-    pr, ldr = _matrix(residual, (m, n), dt, dev, "residual") if residual is not None else (None, 0)
+    pr, ldr = _matrix(residual, (m, n), dt, dev, "residual")
     py, ldy = _matrix(out, (m, n), dt, dev, "out")
-    with _torch.cuda.device(dev):
-        s, other = _stream(stream, dev)
-        _check(_lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, ctypes.byref(dropout), py, ldy, s),
-               "dip_dropout_add")
-    _keep(other, (x, residual, out))
+    if dev.index != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return dropout_add(x, dropout, residual, out, stream)
+    handle, other = _stream(stream, dev)
+    code = _lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, ctypes.byref(dropout), py, ldy, handle)
+    if code:
+        _check(code, "dip_dropout_add")
+    if other is not None:
+        _keep(other, (x, residual, out))
     return out
 
 
 def _rows(t, shape, dtype, device, name):
     """A [b, s, c] tensor as (address, sample stride, position stride)."""
-    _need(t.shape == shape and t.dtype == dtype and t.device == device,
-          f"{name}: want {tuple(shape)} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    sb, ss, one = t.stride()
-    _need(one == 1 or shape[2] <= 1, f"{name}: the last dimension has to be contiguous")
+    if t is None:
+        return None, 0, 0
+    try:
+        sb, ss, one = t.stride()
+        ok = t.shape == shape and t.dtype is dtype and t.device == device and (one == 1 or shape[2] <= 1)
+    except (AttributeError, ValueError):
+        ok = False
+    if not ok:
+        _refuse(t, shape, dtype, device, name)
     return t.data_ptr(), sb, ss
 
 
@@ -295,6 +328,7 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
     _load()
     code, dt, dev = _type(dy, "dy"), dy.dtype, dy.device
     _need(dy.dim() == 3, "dy is [samples, positions, channels]")
+    _need(mean is not None and rstd is not None, "mean and rstd (the forward's) are needed")
     b, s, c = dy.shape
     f32 = _torch.float32
     _need(1 <= groups < 1 << 31, f"{groups} groups")
@@ -308,7 +342,7 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
                        _vector(beta, c, dt, dev, "beta"),
                        _vector(mean.view(-1), b * groups, f32, dev, "mean"),
                        _vector(rstd.view(-1), b * groups, f32, dev, "rstd"),
-                       *(_rows(dx, (b, s, c), dt, dev, "dx") if dx is not None else (None, 0, 0)),
+                       *_rows(dx, (b, s, c), dt, dev, "dx"),
                        dgamma.data_ptr() if dgamma is not None else None,
                        dbeta.data_ptr() if dbeta is not None else None, None, 0)
     _call("dip_group_norm_grad", a, dev, stream, (dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta))
