@@ -121,7 +121,7 @@ struct LinearPlan {
 };
 LinearPlan plan_linear(const dip_linear_args *a) {
   LinearPlan p;
-  if (a->m == 0 || a->n == 0) return p;
+  if (a->m == 0 || a->n == 0 || a->m <= kThinRows) return p;
   Space s;
   p.gemm = plan_gemm(a->m, a->n, a->k);
   if (!direct(a->x, a->ldx, a->k, true)) p.x_at = s.take(a->m * up8(a->k) * 2);
@@ -236,11 +236,6 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
   if (a->m == 0 || a->n == 0) return DIP_OK;
   const hipStream_t st = hipStream_t(stream);
-  char *ws = static_cast<char *>(a->workspace);
-  PackJob px, pw;
-  const Operand x = place(a->x, a->m, a->k, a->ldx, false, ws, p.x_at, &px);
-  const Operand w = place(a->w, a->n, a->k, a->ldw, false, ws, p.w_at, &pw);
-  OPS_CHECK(pack(a->dtype, px, pw, st));
   Epilogue e{};
   e.bias = a->bias;
   e.residual = a->residual;
@@ -251,6 +246,13 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   e.ldp = a->ldp;
   e.drop = make_drop(a->drop);
   e.act = a->act;
+  if (a->m <= kThinRows)
+    return hip_code(launch_thin(a->dtype, a->m, a->n, a->k, a->x, a->ldx, a->w, a->ldw, e, st));
+  char *ws = static_cast<char *>(a->workspace);
+  PackJob px, pw;
+  const Operand x = place(a->x, a->m, a->k, a->ldx, false, ws, p.x_at, &px);
+  const Operand w = place(a->w, a->n, a->k, a->ldw, false, ws, p.w_at, &pw);
+  OPS_CHECK(pack(a->dtype, px, pw, st));
   return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm,
                               reinterpret_cast<float *>(ws + p.partial_at), st));
 }

@@ -29,17 +29,17 @@ __device__ __forceinline__ i32x4 descriptor(const void *p, uint32_t bytes) {
   return d;
 }
 
-// 16 bytes a lane from the buffer straight to LDS: lds_at(to, OFF), then, after
-// at least one other instruction, load_lds(d, offset) loads to to + OFF + 16 lane.
-// Written out, because for the builtin the compiler waits for all loads before
-// any LDS read that follows; the waits below are this file's own.  No register
-// receives the data, and the offset is read when the instruction issues.
+// 16 bytes a lane from the buffer straight to LDS: lds_at(to, OFF), then
+// load_lds(d, offset) loads to to + OFF + 16 lane.  Written out, because for the
+// builtin the compiler waits for all loads before any LDS read that follows; the
+// waits below are this file's own.  No register receives the data, the offset is
+// read when the instruction issues, and the no-op is the wait that a new M0 needs.
 template <int OFF>
 __device__ __forceinline__ void lds_at(uint32_t to) {
   asm volatile("s_add_u32 m0, %0, %1" : : "s"(to), "n"(OFF) : "scc", "memory");
 }
 __device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t offset) {
-  asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(d) : "memory");
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(d) : "memory");
 }
 
 // Where a row's 16-byte chunks sit in LDS when the contraction runs along rows:
@@ -312,7 +312,6 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
       sb.begin(lds_b + p * StageB::kBytes, present(left - p), wave);
       unrolled<p + 1 < R ? kLoads : kFirst>([&](auto j_) __attribute__((always_inline)) {
         aim(j_);
-        asm volatile("s_nop 0");
         load(j_);
       });
     });
@@ -361,25 +360,20 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
             if constexpr (at < FN) w[ahead ? 0 : 1][at] = rb.read(at, ahead ? 0 : 1);
           } else {
             aim(std::integral_constant<int, d0 + o - 1 - n_w>{});
-            if constexpr (o + 1 < o1) {   // the product lies between the last one's halves
-              asm volatile("s_nop 0");
-              load(std::integral_constant<int, d0 + o - 1 - n_w>{});
-            }
+            load(std::integral_constant<int, d0 + o - 1 - n_w>{});
           }
         });
         mfma16(w[s / FM][j], x[s % X], acc[s % FM][j]);
-        if constexpr (o1 > o0 && o1 - 1 > n_w) load(std::integral_constant<int, d0 + o1 - 2 - n_w>{});
         __builtin_amdgcn_sched_barrier(0);
       });
     });
   }
   // the loads after the last tile write zeros to LDS: they end before the wave
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  products_wait();
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int p = 0; p < FN / 2; ++p) products_done(acc[i][2 * p], acc[i][2 * p + 1]);
+    for (int p = 0; p < FN / 2; ++p) in_accumulators(acc[i][2 * p], acc[i][2 * p + 1]);
   // One copy of the epilogue, looped over the rows of fragments: the loop picks
   // its fragments by uniform branches, since registers have no index.  A wave
   // whose part lies inside aligned arrays takes a row at a time through straight

@@ -28,20 +28,16 @@ struct Vec8<_Float16> {
 
 // c[i][j] += sum_k a[i][k] b[j][k], 16 x 16 x 32: lane l holds row l % 16 and
 // k = 8 (l / 16) .. + 7 of either operand, and c's column l % 16, rows
-// 4 (l / 16) .. + 3.  Written out so that c stays in accumulation registers: with
-// 256 of them a lane the compiler moves them back and forth.  Whoever reads c
-// next calls products_done on it first.
+// 4 (l / 16) .. + 3.
 __device__ __forceinline__ void mfma16(bf16x8 a, bf16x8 b, f32x4 &c) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ void mfma16(f16x8 a, f16x8 b, f32x4 &c) {
-  asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-// A product's result may be read some cycles after its issue at the earliest:
-// the first call waits longer than the slowest takes, and all of them tie the
-// reads that follow to places after it.
-__device__ __forceinline__ void products_wait() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
-__device__ __forceinline__ void products_done(f32x4 &a, f32x4 &b) { asm volatile("" : "+a"(a), "+a"(b)); }
+// Keeps a result in accumulation registers up to here: with 256 of them a lane
+// the compiler otherwise moves them back and forth.
+__device__ __forceinline__ void in_accumulators(f32x4 &a, f32x4 &b) { asm volatile("" : "+a"(a), "+a"(b)); }
 
 // Eight consecutive elements from any address aligned to its element (the
 // hardware takes vector accesses at such addresses, and a row of odd length

@@ -30,6 +30,11 @@ GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k);   // by sizes alone
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
                        hipStream_t stream);
+// The same for at most kThinRows rows of an x that is read where it is, as w is:
+// any alignment, no workspace.
+constexpr int64_t kThinRows = 64;
+hipError_t launch_thin(int dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w,
+                       int64_t ldw, const Epilogue &e, hipStream_t stream);
 // rows x cols from p to out (16-byte aligned, stride ldo a multiple of 8), zeros
 // in columns cols .. ldo - 1; no rows: nothing
 struct PackJob {
