@@ -121,7 +121,7 @@ struct LinearPlan {
 };
 LinearPlan plan_linear(const dip_linear_args *a) {
   LinearPlan p;
-  if (a->m == 0 || a->n == 0 || a->m <= kThinRows) return p;
+  if (a->m == 0 || a->n == 0 || thin(a->m, a->n, a->k)) return p;
   Space s;
   p.gemm = plan_gemm(a->m, a->n, a->k);
   if (!direct(a->x, a->ldx, a->k, true)) p.x_at = s.take(a->m * up8(a->k) * 2);
@@ -246,7 +246,7 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   e.ldp = a->ldp;
   e.drop = make_drop(a->drop);
   e.act = a->act;
-  if (a->m <= kThinRows)
+  if (thin(a->m, a->n, a->k))
     return hip_code(launch_thin(a->dtype, a->m, a->n, a->k, a->x, a->ldx, a->w, a->ldw, e, st));
   char *ws = static_cast<char *>(a->workspace);
   PackJob px, pw;

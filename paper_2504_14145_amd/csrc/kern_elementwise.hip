@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
       }
     };
     int64_t row = r0 + ty;
-    for (; row + 24 < r1; row += 32) rows(row, std::integral_constant<int, 4>{});
+    for (; row + 8 < r1; row += 16) rows(row, std::integral_constant<int, 2>{});
     for (; row < r1; row += 8) rows(row, std::integral_constant<int, 1>{});
   }
   if (!g.partial) return;
@@ -179,7 +179,7 @@ hipError_t launch_dropout_add(int dtype, int64_t m, int64_t n, const void *x, in
 
 int32_t grad_row_chunks(int64_t m, int64_t n) {
   const int64_t cols = (n + 255) / 256;
-  return int32_t(std::max<int64_t>(1, std::min<int64_t>((m + 31) / 32, 2048 / cols)));
+  return int32_t(std::max<int64_t>(1, std::min<int64_t>((m + 15) / 16, 2048 / cols)));
 }
 
 hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream) {

@@ -235,8 +235,9 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
   tn = in / high;
 }
 
-// what a workgroup does with its tile
-constexpr int kForward = 0, kGradient = 1, kPartial = 2;
+// what a workgroup does with its tile: the epilogue, a plain output of the
+// operands' type, one of either type or added to, a part of a split
+constexpr int kForward = 0, kGradient = 1, kGradientAny = 2, kPartial = 3;
 
 // out tile BM x BN by WM x WN waves.
 template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R, int KIND>
@@ -370,78 +371,94 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   }
   // the loads after the last tile write zeros to LDS: they end before the wave
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  products_wait();
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int p = 0; p < FN / 2; ++p) in_accumulators(acc[i][2 * p], acc[i][2 * p + 1]);
-  // One copy of the epilogue, looped over the rows of fragments: the loop picks
-  // its fragments by uniform branches, since registers have no index.  A wave
-  // whose part lies inside aligned arrays takes a row at a time through straight
-  // code; the others go eight columns by eight.
+  // A wave takes a row of fragments at a time, all of a row's loads ahead of their
+  // use: it has the SIMD to itself, so nothing else covers them.  Of a long
+  // epilogue there is one copy, looped over the rows: the loop picks its fragments
+  // by uniform branches, since registers have no index.
   constexpr int P = FN / 2;
-  const int64_t col0 = n0 + wn + 8 * (lane / 16);
-  const bool whole = !e.out_f32 && !e.accumulate && m0 + wm + 16 * FM <= m && n0 + wn + 16 * FN <= n;
-  typedef typename Any8<T>::type VA;   // rows of any alignment
-  V bias[P];
-  if (KIND == kForward && whole && e.bias) {
+  const int64_t col0 = n0 + wn + 8 * (lane / 16), row0 = m0 + wm + lane % 16;
+  int cols[P];   // columns of each eight that exist
 #pragma unroll
-    for (int p = 0; p < P; ++p) bias[p] = reinterpret_cast<const VA *>(static_cast<const T *>(e.bias) + col0)[4 * p];
+  for (int p = 0; p < P; ++p) cols[p] = int(max(int64_t(0), min(int64_t(8), n - col0 - 32 * p)));
+  V bias[P], r[P];
+  if (KIND == kForward && e.bias) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) bias[p] = take8(static_cast<const T *>(e.bias) + col0 + 32 * p, cols[p]);
   }
   // the residual's rows are asked for one round ahead
-  V r[P];
-  auto residual = [&](int i) __attribute__((always_inline)) {
-    const VA *o = reinterpret_cast<const VA *>(static_cast<const T *>(e.residual) +
-                                               (m0 + wm + 16 * i + lane % 16) * e.ldr + col0);
+  auto residual = [&](int64_t row) __attribute__((always_inline)) {
+    const T *q = static_cast<const T *>(e.residual) + row * e.ldr + col0;
 #pragma unroll
-    for (int p = 0; p < P; ++p) r[p] = o[4 * p];
+    for (int p = 0; p < P; ++p) r[p] = take8(q + 32 * p, row < m ? cols[p] : 0);
   };
-  if (KIND == kForward && whole && e.residual) residual(0);
-#pragma unroll 1
-  for (int i = 0; i < FM; ++i) {
-    float v[P][8];
-    unrolled<FM>([&](auto i_) __attribute__((always_inline)) {
-      if (i == decltype(i_)::value) {
+  if (KIND == kForward && e.residual) residual(row0);
+  auto finish = [&](int i, float(&v)[P][8]) __attribute__((always_inline)) {
+    const int64_t row = row0 + 16 * i;
+    auto store = [&](auto *base, int64_t ld) __attribute__((always_inline)) {
+      auto *q = base + row * ld + col0;
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+      for (int p = 0; p < P; ++p) store8(q + 32 * p, row < m ? cols[p] : 0, v[p]);
+    };
+    if constexpr (KIND == kPartial) {
+      // rows of the partial product are padded to eight columns
+      float *q = split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col0;
 #pragma unroll
-          for (int q = 0; q < 8; ++q) v[p][q] = acc[decltype(i_)::value][2 * p + q / 4][q % 4];
+      for (int p = 0; p < P; ++p)
+        if (row < m && cols[p] > 0) store8(q + 32 * p, 8, v[p]);
+      return;
+    }
+    if constexpr (KIND == kForward) {
+      if (e.bias) each<P>([&](int p, int q) { v[p][q] += float(bias[p][q]); });
+      if (e.pre) store(static_cast<T *>(e.pre), e.ldp);
+      if (e.act == DIP_ACT_SILU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_SILU); });
+      else if (e.act == DIP_ACT_GELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_GELU); });
+      else if (e.act == DIP_ACT_RELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_RELU); });
+      if (e.drop.drop_of) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) drop8(e.drop, uint32_t(col0 >> 3) + 4 * p, uint32_t(row), v[p]);
       }
-    });
-    const int64_t row = m0 + wm + 16 * i + lane % 16;
-    if (KIND != kPartial && whole) {
-      if constexpr (KIND == kForward) {
-        if (e.bias) each<P>([&](int p, int q) { v[p][q] += float(bias[p][q]); });
-        if (e.pre) {
-          VA *o = reinterpret_cast<VA *>(static_cast<T *>(e.pre) + row * e.ldp + col0);
-#pragma unroll
-          for (int p = 0; p < P; ++p) o[4 * p] = round8<T>(v[p]);
-        }
-        if (e.act == DIP_ACT_SILU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_SILU); });
-        else if (e.act == DIP_ACT_GELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_GELU); });
-        else if (e.act == DIP_ACT_RELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_RELU); });
-        if (e.drop.drop_of) {
-#pragma unroll
-          for (int p = 0; p < P; ++p) drop8(e.drop, uint32_t(col0 >> 3) + 4 * p, uint32_t(row), v[p]);
-        }
-        if (e.residual) {
-          each<P>([&](int p, int q) { v[p][q] += float(r[p][q]); });
-          if (i + 1 < FM) residual(i + 1);
-        }
-      }
-      VA *o = reinterpret_cast<VA *>(static_cast<T *>(e.out) + row * e.ldo + col0);
-#pragma unroll
-      for (int p = 0; p < P; ++p) o[4 * p] = round8<T>(v[p]);
-    } else if (row < m) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int64_t col = col0 + 32 * p;
-        if (col >= n) continue;
-        if constexpr (KIND == kPartial)
-          store8(split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col, 8, v[p]);
-        else
-          finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v[p]);
+      if (e.residual) {
+        each<P>([&](int p, int q) { v[p][q] += float(r[p][q]); });
+        if (i + 1 < FM) residual(row + 16);
       }
     }
+    if constexpr (KIND == kGradientAny) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        if (row < m && cols[p] > 0) finish8<T>(e, row, col0 + 32 * p, cols[p], v[p]);
+    } else {
+      store(static_cast<T *>(e.out), e.ldo);
+    }
+  };
+  auto fragments = [&](auto i_, float(&v)[P][8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[p][q] = acc[decltype(i_)::value][2 * p + q / 4][q % 4];
+  };
+  if constexpr (KIND == kForward || KIND == kGradientAny) {
+#pragma unroll 1
+    for (int i = 0; i < FM; ++i) {
+      // read by instructions written out: the compiler would make one array
+      // indexed by i of the branches, and put it into memory
+      float v[P][8];
+      unrolled<FM>([&](auto i_) __attribute__((always_inline)) {
+        if (i == decltype(i_)::value)
+          each<P>([&](int p, int q) { v[p][q] = from_accumulator(acc[decltype(i_)::value][2 * p + q / 4][q % 4]); });
+      });
+      finish(i, v);
+    }
+  } else {
+    unrolled<FM>([&](auto i_) __attribute__((always_inline)) {
+      float v[P][8];
+      fragments(i_, v);
+      finish(decltype(i_)::value, v);
+    });
   }
 }
 
@@ -470,7 +487,10 @@ hipError_t run(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand 
   const dim3 block(64 * WM * WN);
   Split s{partial, plan.steps, (n + 7) / 8 * 8};
   if (plan.splits <= 1) {
-    gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, B_K ? kGradient : kForward><<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
+    auto go = [&](auto kernel) { kernel<<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s); };
+    if constexpr (!B_K) go(gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, kForward>);
+    else if (e.out_f32 || e.accumulate) go(gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, kGradientAny>);
+    else go(gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, kGradient>);
     return hipGetLastError();
   }
   gemm_kernel<T, A_K, B_K, BM, BN, WM, WN, R, kPartial>

@@ -102,8 +102,7 @@ hipError_t run(int m, int64_t n, int64_t k, const void *x, int64_t ldx, const vo
                                                    ldw, e);
   };
   if (m <= 16) two ? go(thin_kernel<T, 1, 2, 8>) : go(thin_kernel<T, 1, 1, 8>);
-  else if (m <= 32) two ? go(thin_kernel<T, 2, 2, 8>) : go(thin_kernel<T, 2, 1, 8>);
-  else two ? go(thin_kernel<T, 4, 2, 4>) : go(thin_kernel<T, 4, 1, 4>);
+  else two ? go(thin_kernel<T, 2, 2, 8>) : go(thin_kernel<T, 2, 1, 8>);
   return hipGetLastError();
 }
 

@@ -35,6 +35,14 @@ __device__ __forceinline__ void mfma16(bf16x8 a, bf16x8 b, f32x4 &c) {
 __device__ __forceinline__ void mfma16(f16x8 a, f16x8 b, f32x4 &c) {
   c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
+// A product's result may be read some cycles after its issue at the earliest; this
+// waits longer than the slowest takes, for reads that the compiler does not place.
+__device__ __forceinline__ void products_wait() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+__device__ __forceinline__ float from_accumulator(float a) {
+  float v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+  return v;
+}
 // Keeps a result in accumulation registers up to here: with 256 of them a lane
 // the compiler otherwise moves them back and forth.
 __device__ __forceinline__ void in_accumulators(f32x4 &a, f32x4 &b) { asm volatile("" : "+a"(a), "+a"(b)); }
@@ -64,6 +72,15 @@ __device__ __forceinline__ void load8(const T *p, int left, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < left ? float(p[i]) : 0.f;
   }
+}
+// The same as one vector of 2-byte elements.
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type take8(const T *p, int left) {
+  if (left >= 8) return *reinterpret_cast<const typename Any8<T>::type *>(p);
+  typename Vec8<T>::type t;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = i < left ? p[i] : T(0.f);
+  return t;
 }
 template <class T>
 __device__ __forceinline__ typename Vec8<T>::type round8(const float (&v)[8]) {

@@ -30,9 +30,12 @@ GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k);   // by sizes alone
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
                        hipStream_t stream);
-// The same for at most kThinRows rows of an x that is read where it is, as w is:
-// any alignment, no workspace.
-constexpr int64_t kThinRows = 64;
+// The same for few rows of an x that is read where it is, as w is: any alignment,
+// no workspace.  Every 16 or 32 rows of w read x again, from the caches, so it
+// pays for up to 16 rows, and up to 32 where w is small: 32 rows, k 4096 x n 3584
+// 13 us against 17 by tiles, 4096 x 14336 37 against 35, 14336 x 4096 49 against
+// 29; 16 rows 9.8, 32 and 33.
+inline bool thin(int64_t m, int64_t n, int64_t k) { return m <= 16 || (m <= 32 && n * k <= (int64_t(1) << 25)); }
 hipError_t launch_thin(int dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w,
                        int64_t ldw, const Epilogue &e, hipStream_t stream);
 // rows x cols from p to out (16-byte aligned, stride ldo a multiple of 8), zeros
