@@ -123,7 +123,7 @@ LinearPlan plan_linear(const dip_linear_args *a) {
   LinearPlan p;
   if (a->m == 0 || a->n == 0 || thin(a->m, a->n, a->k)) return p;
   Space s;
-  p.gemm = plan_gemm(a->m, a->n, a->k);
+  p.gemm = plan_gemm(a->m, a->n, a->k, true);
   if (!direct(a->x, a->ldx, a->k, true)) p.x_at = s.take(a->m * up8(a->k) * 2);
   if (!direct(a->w, a->ldw, a->k, true)) p.w_at = s.take(a->n * up8(a->k) * 2);
   p.partial_at = s.take(p.gemm.bytes);
@@ -152,12 +152,12 @@ GradPlan plan_grad(const dip_linear_grad_args *a) {
   int64_t partial = 0;
   if (a->dx && a->k > 0) {
     if (!direct(a->w, a->ldw, a->k, false)) p.w_at = s.take(a->n * up8(a->k) * 2);
-    p.dx = plan_gemm(a->m, a->k, a->n);
+    p.dx = plan_gemm(a->m, a->k, a->n, true);
     partial = p.dx.bytes;
   }
   if (a->dw && a->k > 0) {
     if (!direct(a->x, a->ldx, a->k, false)) p.x_at = s.take(a->m * up8(a->k) * 2);
-    p.dw = plan_gemm(a->n, a->k, a->m);
+    p.dw = plan_gemm(a->n, a->k, a->m, false);
     partial = partial > p.dw.bytes ? partial : p.dw.bytes;
   }
   p.partial_at = s.take(partial);   // the two products run one after the other

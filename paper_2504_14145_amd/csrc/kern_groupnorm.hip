@@ -694,7 +694,7 @@ int pow2_at_most(int64_t n) {
 constexpr int kRowMost = 16384;      // channels a row held in registers
 constexpr int kSlabMost = 4096;      // channels a slab, eight a thread
 
-Plan plan(int64_t b, int64_t s, int64_t c, int groups, bool grad) {
+Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   Plan p;
   const int64_t per = c / groups;
   if (s == 1 && per <= kRowMost && groups < 65536) {
@@ -703,9 +703,10 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, bool grad) {
     p.partial = grad ? p.row_blocks * 2 * c : 0;
     return p;
   }
-  // a slab of at least 128 bytes of a row, and beyond that as many groups as
-  // still leave workgroups for the whole card
-  int64_t slab = std::max<int64_t>(1, std::min<int64_t>(groups, (64 + per - 1) / std::max<int64_t>(per, 1)));
+  // a slab of at least 128 bytes of a row (64 where samples are few), and beyond
+  // that as many groups as still leave workgroups for the whole card
+  const int64_t least = (b * c * elem >= 128 * 256 ? 128 : 64) / elem;
+  int64_t slab = std::max<int64_t>(1, std::min<int64_t>(groups, (least + per - 1) / std::max<int64_t>(per, 1)));
   while (slab * 2 <= groups && slab * 2 * per <= 512 && b * ((groups + slab * 2 - 1) / (slab * 2)) >= 1024) slab *= 2;
   const int64_t blocks = b * ((groups + slab - 1) / slab);
   if (slab * per <= kSlabMost && (s * slab * per <= 32768 || blocks >= 512)) {
@@ -738,7 +739,7 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, bool grad) {
 
 template <class T>
 hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
-  const Plan p = plan(a.b, a.s, a.c, a.groups, false);
+  const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false);
   const int64_t per = a.c / a.groups, rows = a.b * a.groups;
   if (p.way == kRows) {
     if (per <= 512)
@@ -770,7 +771,7 @@ hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
 
 template <class T>
 hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
-  const Plan p = plan(a.b, a.s, a.c, a.groups, true);
+  const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, true);
   const int64_t per = a.c / a.groups;
   float *partial = static_cast<float *>(a.workspace);
   float *sums = a.dgamma || a.dbeta ? partial : nullptr;
@@ -812,10 +813,10 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
 }  // namespace
 
 int64_t group_norm_workspace(const dip_group_norm_args &a) {
-  return a.b > 0 && a.c > 0 ? plan(a.b, a.s, a.c, a.groups, false).bytes() : 0;
+  return a.b > 0 && a.c > 0 ? plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false).bytes() : 0;
 }
 int64_t group_norm_grad_workspace(const dip_group_norm_grad_args &a) {
-  return a.b > 0 && a.c > 0 && a.s > 0 ? plan(a.b, a.s, a.c, a.groups, true).bytes() : 0;
+  return a.b > 0 && a.c > 0 && a.s > 0 ? plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, true).bytes() : 0;
 }
 
 hipError_t launch_group_norm(const dip_group_norm_args &a, hipStream_t st) {

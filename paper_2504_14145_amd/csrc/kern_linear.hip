@@ -385,18 +385,25 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   int cols[P];   // columns of each eight that exist
 #pragma unroll
   for (int p = 0; p < P; ++p) cols[p] = int(max(int64_t(0), min(int64_t(8), n - col0 - 32 * p)));
-  V bias[P], r[P];
+  V bias[P];
   if (KIND == kForward && e.bias) {
 #pragma unroll
     for (int p = 0; p < P; ++p) bias[p] = take8(static_cast<const T *>(e.bias) + col0 + 32 * p, cols[p]);
   }
-  // the residual's rows are asked for one round ahead
-  auto residual = [&](int64_t row) __attribute__((always_inline)) {
+  // the residual's rows are asked for all at once where there are few, else one
+  // round ahead
+  constexpr int kRows = FM <= 4 ? FM : 1;
+  V r[kRows][P];
+  auto residual = [&](int at, int i) __attribute__((always_inline)) {
+    const int64_t row = row0 + 16 * i;
     const T *q = static_cast<const T *>(e.residual) + row * e.ldr + col0;
 #pragma unroll
-    for (int p = 0; p < P; ++p) r[p] = take8(q + 32 * p, row < m ? cols[p] : 0);
+    for (int p = 0; p < P; ++p) r[at][p] = take8(q + 32 * p, row < m ? cols[p] : 0);
   };
-  if (KIND == kForward && e.residual) residual(row0);
+  if (KIND == kForward && e.residual) {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) residual(i, i);
+  }
   auto finish = [&](int i, float(&v)[P][8]) __attribute__((always_inline)) {
     const int64_t row = row0 + 16 * i;
     auto store = [&](auto *base, int64_t ld) __attribute__((always_inline)) {
@@ -423,8 +430,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
         for (int p = 0; p < P; ++p) drop8(e.drop, uint32_t(col0 >> 3) + 4 * p, uint32_t(row), v[p]);
       }
       if (e.residual) {
-        each<P>([&](int p, int q) { v[p][q] += float(r[p][q]); });
-        if (i + 1 < FM) residual(row + 16);
+        each<P>([&](int p, int q) { v[p][q] += float(r[i % kRows][p][q]); });
+        if (kRows < FM && i + 1 < FM) residual(0, i + 1);
       }
     }
     if constexpr (KIND == kGradientAny) {
@@ -441,7 +448,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[p][q] = acc[decltype(i_)::value][2 * p + q / 4][q % 4];
   };
-  if constexpr (KIND == kForward || KIND == kGradientAny) {
+  if constexpr ((KIND == kForward && kRows < FM) || KIND == kGradientAny) {
 #pragma unroll 1
     for (int i = 0; i < FM; ++i) {
       // read by instructions written out: the compiler would make one array
@@ -507,6 +514,8 @@ hipError_t pick(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand
   switch (plan.tile) {
     case 0: return run<T, A_K, B_K, 256, 256, 2, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
     case 1: return run<T, A_K, B_K, 128, 128, 2, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
+    case 3:
+      if constexpr (!A_K) return run<T, A_K, B_K, 192, 128, 2, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
     default: return run<T, A_K, B_K, 128, 128, 2, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
   }
 }
@@ -529,27 +538,30 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJob a, PackJob b, uint32_
 }  // namespace
 
 // The tile and the number of splits of the contraction with the least expected
-// time.  Three shapes: 256 x 256, one workgroup a CU, reaches the highest rate;
-// 128 x 128 with two workgroups a CU fills the card with a quarter of the output;
-// 128 x 128 with a longer ring of loads, one workgroup a CU, hides the latency of
-// memory better where that suffices.  Microseconds a step and a workgroup's start
-// and end as measured in bf16 (2048^3: 45 / 28 / 21 us; 4096^3: 94 / 110 / 136;
-// 1152 x 1792 x 3840: 42 / 26 / 35; 149 x 4096 x 14336: 81 / 49 / 33).  A split
+// time.  256 x 256, one workgroup a CU, reaches the highest rate; 128 x 128 with
+// two workgroups a CU fills the card with a quarter of the output; 128 x 128 and
+// 192 x 128 with a longer ring of loads, one workgroup a CU, hide the latency of
+// memory better where they suffice (192 only for rows of a that lie along the
+// contraction: the other layout's loads do not divide by it).  Microseconds a step
+// and a workgroup's start and end as measured in bf16, in that order: 2048^3 44 /
+// 28 / 20 / 25 us; 1500 x 3584 x 3584 71 / 46 / 55 / 39; 1152 x 1792 x 3840 43 / 26
+// / 33 / 23; 149 x 4096 x 14336 81 / 49 / 32 / 41; 4096^3 94 / 110 / 136 / -.  A split
 // costs its partial products' way through the caches: 65,536 x 3584 x 2560's
 // weight gradient takes 1328 us whole, 932 in 7 parts; 1152 x 1792 x 3840 26 whole,
 // 40 in 2.
-GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k) {
+GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows) {
   struct Shape {
-    int64_t side, slots;
+    int64_t bm, bn, slots;
     double step_us, fixed_us;
   };
-  constexpr Shape shapes[] = {{256, 256, 1.35, 8.0}, {128, 512, 0.75, 4.0}, {128, 256, 0.45, 3.5}};
+  constexpr Shape shapes[] = {
+      {256, 256, 256, 1.35, 8.0}, {128, 128, 512, 0.78, 4.0}, {128, 128, 256, 0.45, 3.5}, {192, 128, 256, 0.62, 4.5}};
   const int64_t steps = (k + kStep - 1) / kStep;
   GemmPlan best;
   double least = 0;
-  for (int tile = 0; tile < 3; ++tile) {
+  for (int tile = 0; tile < (a_rows ? 4 : 3); ++tile) {
     const Shape &s = shapes[tile];
-    const int64_t tiles = ((m + s.side - 1) / s.side) * ((n + s.side - 1) / s.side);
+    const int64_t tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
     for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * 2 <= steps); ++splits) {
       const int64_t each = (steps + splits - 1) / splits;
       if (splits > 1 && (steps + each - 1) / each != splits) continue;
