@@ -19,8 +19,8 @@
  * Conventions of all calls
  *  - Matrices are row-major with a leading stride in elements; the last
  *    dimension is contiguous.  Pointers are device pointers aligned to their
- *    element; 16-byte aligned rows run at full speed, others through a copy or
- *    element by element.
+ *    element; 16-byte aligned rows run at full speed, others cost the products a
+ *    copy into the workspace and the other operators little.
  *  - Sums, statistics and everything between inputs and outputs are held in
  *    float32; an output is rounded once (to nearest even), save where a comment
  *    below says otherwise.
@@ -35,9 +35,10 @@
  *    the host before anything is launched: DIP_E_INVAL (null or misaligned
  *    pointers, negative sizes, strides below the row, unknown type or
  *    activation, overlapping shapes), DIP_E_RANGE (sizes beyond the kernels'
- *    index range), DIP_E_UNSUPPORTED (float32 in dip_linear), DIP_E_CAPACITY
- *    (workspace too small), DIP_E_HIP.  Sizes of zero are legal: nothing is
- *    read, sums over nothing are zero.
+ *    index range: 2^31 rows, 2^22 columns and strides of a matrix),
+ *    DIP_E_UNSUPPORTED (float32 in dip_linear), DIP_E_CAPACITY (workspace too
+ *    small; nothing has been done), DIP_E_HIP.  Sizes of zero are legal: nothing
+ *    is read, sums over nothing are zero.
  */
 #ifndef DIP_OPS_H
 #define DIP_OPS_H

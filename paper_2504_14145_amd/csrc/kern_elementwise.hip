@@ -23,7 +23,8 @@ struct Divide {
 
 // Bound by memory while a counter's 128 bits serve eight elements: its twenty
 // 32 x 32 products take 320 cycles a wave, less than the wave's 24 bytes a lane
-// take to come and go.  Eight columns of a row a thread.
+// take to come and go.  Eight columns of a row a thread.  65,536 x 3584 bf16 with a
+// residual 240 us (5.9 TB/s), without 146 (6.4).
 template <class T, bool RESIDUAL>
 __global__ __launch_bounds__(kThreads) void dropout_add_kernel(uint32_t items, uint32_t row0, Divide per, int64_t n,
                                                                const T *x, int64_t ldx, const T *r, int64_t ldr,
@@ -64,8 +65,11 @@ hipError_t dropout_add(int64_t m, int64_t n, const void *x, int64_t ldx, const v
   return hipSuccess;
 }
 
-// A block takes 256 columns (32 threads of eight) of one chunk of rows, eight
-// rows at a time, and adds its eight row lanes at the end.
+// g = D(dy) act'(pre) and its column sums: bound by memory, dy and pre read and g
+// written once.  A block takes 256 columns (32 threads of eight) of one chunk of
+// rows, sixteen rows at a time, and adds its eight row lanes at the end; the
+// chunks' sums are added in their order by sum_rows_kernel.  65,536 x 2560 with
+// GELU 217 us (4.6 TB/s; the slope's arithmetic is the rest).
 template <class T>
 __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   __shared__ float s[8][256 + 8];

@@ -1,4 +1,21 @@
-// kern_linear.hip -- matrix products of the stage operators.
+// kern_linear.hip -- matrix products of the stage operators: out[m][n] =
+// epilogue(sum_k a(m, k) b(n, k)), for dip_linear (x w^T) and its gradients (g w,
+// g^T x), each operand lying along the contraction or across it.
+//
+// Bound by the matrix instructions where m, n and k are large, by the latency of
+// memory where few tiles are, by memory where one side is short.  A large tile is
+// 256 x 256 by four waves of 128 x 128, which reads least from LDS a product (with
+// eight waves of 128 x 64 the LDS, reads and incoming tiles together, is as busy as
+// the matrix units); an operand's tiles go from memory to LDS without passing
+// registers, and across-lying ones are read through the transposing LDS read, so
+// that no weight or activation is ever transposed in memory.  The product is taken
+// as b a^T: a lane then holds eight consecutive columns of a row of the output,
+// which its epilogue (bias, activation, eight dropout draws of one counter,
+// residual) and its 16-byte stores want.
+// bf16, 8192^3: 1.43 to 1.5 PFLOP/s forward, 1.46 to 1.51 and 1.44 to 1.5 for the
+// gradients of x and w, the card's clock falling under the load; 65,536 x 3584 x
+// 2560: 1.32, 1.33, 1.26.  Of a step's 2500 cycles 2048 are products, 280 waits at
+// the two barriers; a tile's start and end take another 20,000.
 #include <algorithm>
 #include <type_traits>
 #include <utility>

@@ -5,6 +5,8 @@
 // fragments of w and x straight into registers, eight of each at once, so that all
 // of a wave's loads are on their way before the first product, and at any
 // alignment.  The eight partial results meet in LDS: one launch, no workspace.
+// bf16, one row: 4096 x 3584 7.7 us a call (3.8 TB/s of w), 4096 x 14336 27 us
+// (4.4 TB/s); by tiles, split 16 ways and joined, the first took 14.
 #include "ops_internal.h"
 
 namespace dipops {

@@ -12,6 +12,7 @@ no call records an autograd graph.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from . import E_CAPACITY, _check, load
 
@@ -79,24 +80,36 @@ class _GroupNormGrad(ctypes.Structure):
                 ("dbeta", _vp), ("workspace", _vp), ("workspace_bytes", _i64)]
 
 
+# A call's arguments go to the library as the bytes of its struct, in one step.
+_CODES = {_i64: "q", _i32: "i", ctypes.c_float: "f", _vp: "Q", Dropout: "QQII"}
+
+
+def _packer(cls):
+    return struct.Struct("@" + "".join(_CODES[t] for _, t in cls._fields_)).pack
+
+
+_pack_linear, _pack_linear_grad = _packer(_Linear), _packer(_LinearGrad)
+_pack_norm, _pack_norm_grad = _packer(_GroupNorm), _packer(_GroupNormGrad)
+_WORKSPACE = struct.Struct("@Qq")   # every struct's last two members
+
 _lib = None
 _torch = None
+_empty = None
 _raw_stream = None   # device index -> handle of torch's current stream
+_device = None       # () -> index of the current device
 _types = {}
 
 
 def _load():
     """The library with the operators' signatures, and torch."""
-    global _lib, _torch, _raw_stream
+    global _lib, _torch, _empty, _raw_stream, _device
     if _lib is None:
         import torch
         lib = load()
-        for name, args in (("dip_linear", _Linear), ("dip_linear_grad", _LinearGrad),
-                           ("dip_group_norm", _GroupNorm),
-                           ("dip_group_norm_grad", _GroupNormGrad)):
-            getattr(lib, name).argtypes = [ctypes.POINTER(args), _vp]
+        for name in ("dip_linear", "dip_linear_grad", "dip_group_norm", "dip_group_norm_grad"):
+            getattr(lib, name).argtypes = [_vp, _vp]
             getattr(lib, name).restype = ctypes.c_int
-            getattr(lib, name + "_workspace").argtypes = [ctypes.POINTER(args)]
+            getattr(lib, name + "_workspace").argtypes = [_vp]
             getattr(lib, name + "_workspace").restype = _i64
         lib.dip_dropout_add.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _i64,
                                         ctypes.POINTER(Dropout), _vp, _i64, _vp]
@@ -104,11 +117,12 @@ def _load():
         _types.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                               lambda index: torch.cuda.current_stream(index).cuda_stream)
-        _torch, _lib = torch, lib
+        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _torch, _empty, _lib = torch, torch.empty, lib
     return _lib
 
 
-_NO_DROP = Dropout(0.0, 0)
+_NO_DROP = (0, 0, 0, 0)
 
 
 def _need(ok: bool, what: str):
@@ -123,70 +137,92 @@ def _act(name) -> int:
     return code
 
 
-def _refuse(t, shape, dtype, device, name):
+def _drop(d):
+    return _NO_DROP if d is None else (d.seed, d.offset, d.row0, d.drop_of)
+
+
+def _refuse(t, shape, dtype, index, name):
     if not isinstance(t, _torch.Tensor):
         raise ValueError(f"{name}: want a tensor, got {type(t).__name__}")
-    if t.shape != shape or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name}: want {tuple(shape)} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{name}: want {tuple(shape)} {dtype} on cuda:{index}, "
+                         f"got {tuple(t.shape)} {t.dtype} on {t.device}")
     raise ValueError(f"{name}: the last dimension has to be contiguous")
 
 
-_NONE = (None, 0)
+_NONE, _NONE3 = (0, 0), (0, 0, 0)
 
 
-def _matrix(t, shape, dtype, device, name):
-    """A [rows, cols] tensor as (address, leading stride); (None, 0) for None."""
+def _matrix(t, shape, dtype, index, name):
+    """A [rows, cols] tensor as (address, leading stride); zeros for None."""
     if t is None:
         return _NONE
     try:
         ld, one = t.stride()
-        ok = t.shape == shape and t.dtype is dtype and t.device == device and (one == 1 or shape[1] <= 1)
+        if t.shape == shape and t.dtype is dtype and t.get_device() == index and (one == 1 or shape[1] <= 1):
+            return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
     except (AttributeError, ValueError):
-        ok = False
-    if not ok:
-        _refuse(t, shape, dtype, device, name)
-    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
+        pass
+    _refuse(t, shape, dtype, index, name)
 
 
-def _vector(t, n, dtype, device, name):
+def _rows(t, shape, dtype, index, name):
+    """A [b, s, c] tensor as (address, sample stride, position stride)."""
     if t is None:
-        return None
-    if not (t.shape == (n,) and t.dtype is dtype and t.device == device and t.is_contiguous()):
-        _refuse(t, (n,), dtype, device, name)
-    return t.data_ptr()
+        return _NONE3
+    try:
+        sb, ss, one = t.stride()
+        if t.shape == shape and t.dtype is dtype and t.get_device() == index and (one == 1 or shape[2] <= 1):
+            return t.data_ptr(), sb, ss
+    except (AttributeError, ValueError):
+        pass
+    _refuse(t, shape, dtype, index, name)
+
+
+def _whole(t, shape, dtype, index, name):
+    """The address of a contiguous tensor; zero for None."""
+    if t is None:
+        return 0
+    if isinstance(t, _torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == index \
+            and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(t, shape, dtype, index, name)
 
 
 def _type(t, name):
-    _need(isinstance(t, _torch.Tensor) and t.is_cuda, f"{name}: want a device tensor")
-    code = _types.get(t.dtype)
+    """(code, dtype, device index) of an operator's first tensor."""
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: want a device tensor")
+    dtype = t.dtype
+    code = _types.get(dtype)
     if code is None:
-        raise ValueError(f"{name}: {t.dtype} is not float32, float16 or bfloat16")
-    return code
+        raise ValueError(f"{name}: {dtype} is not float32, float16 or bfloat16")
+    return code, dtype, t.get_device()
 
 
-def _call(name, a, device, stream, used):
+def _call(name, args, index, stream, used):
     """Launch on the tensors' device, with a workspace where one is needed."""
-    if device.index != _torch.cuda.current_device():
-        with _torch.cuda.device(device):
-            return _call(name, a, device, stream, used)
+    if index != _device():
+        with _torch.cuda.device(index):
+            return _call(name, args, index, stream, used)
     run = getattr(_lib, name)
-    handle, other = _stream(stream, device)
-    code = run(ctypes.byref(a), handle)
+    handle, other = _stream(stream, index)
+    code = run(args, handle)
     if code == E_CAPACITY:
-        need = getattr(_lib, name + "_workspace")(ctypes.byref(a))
-        ws = _torch.empty(need, dtype=_torch.uint8, device=device)
-        a.workspace, a.workspace_bytes = ws.data_ptr(), need
+        need = getattr(_lib, name + "_workspace")(args)
+        ws = _empty(need, dtype=_torch.uint8, device=used[0].device)
+        args = args[:-_WORKSPACE.size] + _WORKSPACE.pack(ws.data_ptr(), need)
         used = (*used, ws)
-        code = run(ctypes.byref(a), handle)
+        code = run(args, handle)
     if code:
         _check(code, name)
     if other is not None:
         _keep(other, used)
 
 
-def _stream(stream, device):
+def _stream(stream, index):
     """(its handle, the stream itself where it is not the current one)"""
-    current = _raw_stream(device.index)
+    current = _raw_stream(index)
     if stream is None:
         return current, None
     handle = getattr(stream, "cuda_stream", stream)
@@ -209,19 +245,20 @@ def linear(x, w, bias=None, act="none", dropout=None, residual=None, pre=None, o
     and the result [m, n]; float16 or bfloat16, summed in float32.  ``pre``, if
     given, receives ``x w^T + bias``, which linear_backward needs when there is an
     activation.  A result allocated here belongs to torch's current stream."""
-    _load()
-    code, dt, dev = _type(x, "x"), x.dtype, x.device
+    if _lib is None:
+        _load()
+    code, dt, dev = _type(x, "x")
     _need(x.dim() == 2 and w.dim() == 2, "x and w are matrices")
-    (m, k), n = x.shape, w.shape[0]
+    m, k = x.shape
+    n = w.shape[0]
     if out is None:
-        out = _torch.empty((m, n), dtype=dt, device=dev)
-    a = _Linear(m, n, k, code, _act(act), *_matrix(x, (m, k), dt, dev, "x"),
-                *_matrix(w, (n, k), dt, dev, "w"), _vector(bias, n, dt, dev, "bias"),
-                *_matrix(residual, (m, n), dt, dev, "residual"),
-                dropout if dropout is not None else _NO_DROP,
-                *_matrix(out, (m, n), dt, dev, "out"),
-                *_matrix(pre, (m, n), dt, dev, "pre"), None, 0)
-    _call("dip_linear", a, dev, stream, (x, w, bias, residual, pre, out))
+        out = x.new_empty((m, n))
+    args = _pack_linear(m, n, k, code, _act(act), *_matrix(x, (m, k), dt, dev, "x"),
+                        *_matrix(w, (n, k), dt, dev, "w"), _whole(bias, (n,), dt, dev, "bias"),
+                        *_matrix(residual, (m, n), dt, dev, "residual"), *_drop(dropout),
+                        *_matrix(out, (m, n), dt, dev, "out"), *_matrix(pre, (m, n), dt, dev, "pre"),
+                        0, 0)
+    _call("dip_linear", args, dev, stream, (x, w, bias, residual, pre, out))
     return out
 
 
@@ -231,52 +268,59 @@ def linear_backward(dy, x, w, act="none", dropout=None, pre=None, bias=True, nee
     None for those not asked for.  ``dx``, ``dw`` and ``db`` may be given; dw and
     db may then be float32, and with ``accumulate`` they are added to.  The
     residual's gradient is dy."""
-    _load()
-    code, dt, dev = _type(dy, "dy"), dy.dtype, dy.device
+    if _lib is None:
+        _load()
+    code, dt, dev = _type(dy, "dy")
     _need(dy.dim() == 2 and x.dim() == 2 and w.dim() == 2, "dy, x and w are matrices")
-    (m, n), k = dy.shape, x.shape[1]
+    m, n = dy.shape
+    k = x.shape[1]
     _need(act == "none" or pre is not None, f"{act}: pre (the forward's) is needed")
-    given = [t for t in (dw, db) if t is not None]
-    _need(not accumulate or (not need_dw or dw is not None) and (not bias or db is not None),
-          "accumulate: dw and db have to be given")
-    gt = given[0].dtype if given else dt
-    _need(all(t.dtype == gt for t in given) and gt in (dt, _torch.float32),
+    if accumulate:
+        _need((not need_dw or dw is not None) and (not bias or db is not None),
+              "accumulate: dw and db have to be given")
+    gt = dw.dtype if dw is not None else db.dtype if db is not None else dt
+    _need((gt is dt or gt is _torch.float32) and (db is None or db.dtype is gt),
           "dw and db are both of dy's type or both float32")
-    if need_dx and dx is None:
-        dx = _torch.empty((m, k), dtype=dt, device=dev)
-    if need_dw and dw is None:
-        dw = _torch.empty((n, k), dtype=gt, device=dev)
-    if bias and db is None:
-        db = _torch.empty((n,), dtype=gt, device=dev)
-    dx, dw, db = dx if need_dx else None, dw if need_dw else None, db if bias else None
-    a = _LinearGrad(m, n, k, code, _act(act), *_matrix(dy, (m, n), dt, dev, "dy"),
-                    *_matrix(x, (m, k), dt, dev, "x"), *_matrix(w, (n, k), dt, dev, "w"),
-                    *_matrix(pre if act != "none" else None, (m, n), dt, dev, "pre"),
-                    dropout if dropout is not None else _NO_DROP,
-                    *_matrix(dx, (m, k), dt, dev, "dx"),
-                    *_matrix(dw, (n, k), gt, dev, "dw"),
-                    _vector(db, n, gt, dev, "db"), _types[gt], int(bool(accumulate)), None, 0)
-    _call("dip_linear_grad", a, dev, stream, (dy, x, w, pre, dx, dw, db))
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = dy.new_empty((m, k))
+    if not need_dw:
+        dw = None
+    elif dw is None:
+        dw = dy.new_empty((n, k), dtype=gt)
+    if not bias:
+        db = None
+    elif db is None:
+        db = dy.new_empty((n,), dtype=gt)
+    args = _pack_linear_grad(m, n, k, code, _act(act), *_matrix(dy, (m, n), dt, dev, "dy"),
+                             *_matrix(x, (m, k), dt, dev, "x"), *_matrix(w, (n, k), dt, dev, "w"),
+                             *_matrix(pre if act != "none" else None, (m, n), dt, dev, "pre"),
+                             *_drop(dropout), *_matrix(dx, (m, k), dt, dev, "dx"),
+                             *_matrix(dw, (n, k), gt, dev, "dw"), _whole(db, (n,), gt, dev, "db"),
+                             _types[gt], int(bool(accumulate)), 0, 0)
+    _call("dip_linear_grad", args, dev, stream, (dy, x, w, pre, dx, dw, db))
     return dx, dw, db
 
 
 def dropout_add(x, dropout, residual=None, out=None, stream=None):
     """``residual + D(x)`` for x [m, n]; ``dropout_add(dy, dropout)`` is the
     gradient of x."""
-    _load()
-    code, dt, dev = _type(x, "x"), x.dtype, x.device
+    if _lib is None:
+        _load()
+    code, dt, dev = _type(x, "x")
     _need(x.dim() == 2, "x is a matrix")
-    m, n = x.shape
+    shape = m, n = x.shape
     if out is None:
-        out = _torch.empty((m, n), dtype=dt, device=dev)
-    px, ldx = _matrix(x, (m, n), dt, dev, "x")
-    pr, ldr = _matrix(residual, (m, n), dt, dev, "residual")
-    py, ldy = _matrix(out, (m, n), dt, dev, "out")
-    if dev.index != _torch.cuda.current_device():
+        out = x.new_empty(shape)
+    px, ldx = _matrix(x, shape, dt, dev, "x")
+    pr, ldr = _matrix(residual, shape, dt, dev, "residual")
+    py, ldy = _matrix(out, shape, dt, dev, "out")
+    if dev != _device():
         with _torch.cuda.device(dev):
             return dropout_add(x, dropout, residual, out, stream)
     handle, other = _stream(stream, dev)
-    code = _lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, ctypes.byref(dropout), py, ldy, handle)
+    code = _lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, dropout, py, ldy, handle)
     if code:
         _check(code, "dip_dropout_add")
     if other is not None:
@@ -284,40 +328,29 @@ def dropout_add(x, dropout, residual=None, out=None, stream=None):
     return out
 
 
-def _rows(t, shape, dtype, device, name):
-    """A [b, s, c] tensor as (address, sample stride, position stride)."""
-    if t is None:
-        return None, 0, 0
-    try:
-        sb, ss, one = t.stride()
-        ok = t.shape == shape and t.dtype is dtype and t.device == device and (one == 1 or shape[2] <= 1)
-    except (AttributeError, ValueError):
-        ok = False
-    if not ok:
-        _refuse(t, shape, dtype, device, name)
-    return t.data_ptr(), sb, ss
-
-
 def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None, mean=None,
                rstd=None, stream=None):
     """(y, mean, rstd): group norm of x [b, s, c] (channels last) and its
     activation; float32 statistics [b, groups] for group_norm_backward.  One
     position and one group a sample make it a layer norm of the rows."""
-    _load()
-    code, dt, dev = _type(x, "x"), x.dtype, x.device
+    if _lib is None:
+        _load()
+    code, dt, dev = _type(x, "x")
     _need(x.dim() == 3, "x is [samples, positions, channels]")
-    b, s, c = x.shape
-    out = _torch.empty((b, s, c), dtype=dt, device=dev) if out is None else out
     _need(1 <= groups < 1 << 31, f"{groups} groups")
-    mean, rstd = (t if t is not None else _torch.empty((b, groups), dtype=_torch.float32, device=dev)
-                  for t in (mean, rstd))
-    f32 = _torch.float32
-    a = _GroupNorm(b, s, c, groups, code, _act(act), eps, *_rows(x, (b, s, c), dt, dev, "x"),
-                   _vector(gamma, c, dt, dev, "gamma"), _vector(beta, c, dt, dev, "beta"),
-                   *_rows(out, (b, s, c), dt, dev, "out"),
-                   _vector(mean.view(-1), b * groups, f32, dev, "mean"),
-                   _vector(rstd.view(-1), b * groups, f32, dev, "rstd"), None, 0)
-    _call("dip_group_norm", a, dev, stream, (x, gamma, beta, out, mean, rstd))
+    shape = b, s, c = x.shape
+    f32, stats = _torch.float32, (b, groups)
+    if out is None:
+        out = x.new_empty(shape)
+    if mean is None:
+        mean = x.new_empty(stats, dtype=f32)
+    if rstd is None:
+        rstd = x.new_empty(stats, dtype=f32)
+    args = _pack_norm(b, s, c, groups, code, _act(act), eps, *_rows(x, shape, dt, dev, "x"),
+                      _whole(gamma, (c,), dt, dev, "gamma"), _whole(beta, (c,), dt, dev, "beta"),
+                      *_rows(out, shape, dt, dev, "out"), _whole(mean, stats, f32, dev, "mean"),
+                      _whole(rstd, stats, f32, dev, "rstd"), 0, 0)
+    _call("dip_group_norm", args, dev, stream, (x, gamma, beta, out, mean, rstd))
     return out, mean, rstd
 
 
@@ -325,25 +358,25 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
                         need_dparam=True, dx=None, stream=None):
     """Gradients (dx, dgamma, dbeta) of group_norm; dgamma and dbeta are None
     without ``need_dparam`` or where gamma and beta are None."""
-    _load()
-    code, dt, dev = _type(dy, "dy"), dy.dtype, dy.device
+    if _lib is None:
+        _load()
+    code, dt, dev = _type(dy, "dy")
     _need(dy.dim() == 3, "dy is [samples, positions, channels]")
-    _need(mean is not None and rstd is not None, "mean and rstd (the forward's) are needed")
-    b, s, c = dy.shape
-    f32 = _torch.float32
     _need(1 <= groups < 1 << 31, f"{groups} groups")
-    if need_dx and dx is None:
-        dx = _torch.empty((b, s, c), dtype=dt, device=dev)
-    dx = dx if need_dx else None
-    dgamma = _torch.empty((c,), dtype=dt, device=dev) if need_dparam and gamma is not None else None
-    dbeta = _torch.empty((c,), dtype=dt, device=dev) if need_dparam and beta is not None else None
-    a = _GroupNormGrad(b, s, c, groups, code, _act(act), *_rows(dy, (b, s, c), dt, dev, "dy"),
-                       *_rows(x, (b, s, c), dt, dev, "x"), _vector(gamma, c, dt, dev, "gamma"),
-                       _vector(beta, c, dt, dev, "beta"),
-                       _vector(mean.view(-1), b * groups, f32, dev, "mean"),
-                       _vector(rstd.view(-1), b * groups, f32, dev, "rstd"),
-                       *_rows(dx, (b, s, c), dt, dev, "dx"),
-                       dgamma.data_ptr() if dgamma is not None else None,
-                       dbeta.data_ptr() if dbeta is not None else None, None, 0)
-    _call("dip_group_norm_grad", a, dev, stream, (dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta))
+    _need(mean is not None and rstd is not None, "mean and rstd (the forward's) are needed")
+    shape = b, s, c = dy.shape
+    f32, stats = _torch.float32, (b, groups)
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = dy.new_empty(shape)
+    dgamma = dy.new_empty((c,)) if need_dparam and gamma is not None else None
+    dbeta = dy.new_empty((c,)) if need_dparam and beta is not None else None
+    args = _pack_norm_grad(b, s, c, groups, code, _act(act), *_rows(dy, shape, dt, dev, "dy"),
+                           *_rows(x, shape, dt, dev, "x"), _whole(gamma, (c,), dt, dev, "gamma"),
+                           _whole(beta, (c,), dt, dev, "beta"), _whole(mean, stats, f32, dev, "mean"),
+                           _whole(rstd, stats, f32, dev, "rstd"), *_rows(dx, shape, dt, dev, "dx"),
+                           dgamma.data_ptr() if dgamma is not None else 0,
+                           dbeta.data_ptr() if dbeta is not None else 0, 0, 0)
+    _call("dip_group_norm_grad", args, dev, stream, (dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta))
     return dx, dgamma, dbeta
