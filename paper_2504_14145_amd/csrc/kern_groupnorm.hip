@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256) void split_sums_kernel(dip_group_norm_args a, 
   channel_sums(l, vectors, u, v, s);
   const int half = vectors * 8 * l.TY;
   if (!l.on || l.ty != 0) return;
-  const float n = float(w.r1 - w.r0);
+  const float n = float(max(w.r1 - w.r0, int64_t(1)));
   float *p = partial + w.at * 2 * a.c + w.c;
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(256) void split_join_kernel(const float *partial, i
   int turn = 0;
   const uint32_t groups = uint32_t(c / per), i = blockIdx.x / groups, g = blockIdx.x % groups;
   const float *p = partial + int64_t(i) * chunks * 2 * c + int64_t(g) * per;
-  const float total = float(s_all) * float(per), full = float(chunk);
+  const float total = float(max(s_all, int64_t(1))) * float(per), full = float(chunk);
   const float rest = float(s_all - chunk * (chunks - 1));   // rows of the last chunk
   // every value times its count, about the first chunk's first channel
   const float k = p[0];
@@ -732,8 +732,8 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   // chunks for about four workgroups a CU, of at least two rows a thread
   const int64_t most = std::max<int64_t>(1, s / (int64_t(p.lanes_y) * 2));
   p.chunks = std::max<int64_t>(1, std::min<int64_t>(most, 1024 / std::max<int64_t>(1, b * p.tiles)));
-  p.chunk = (s + p.chunks - 1) / p.chunks;
-  p.chunks = (s + p.chunk - 1) / p.chunk;
+  p.chunk = std::max<int64_t>(1, (s + p.chunks - 1) / p.chunks);   // no positions: one empty chunk
+  p.chunks = std::max<int64_t>(1, (s + p.chunk - 1) / p.chunk);
   p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4;
   p.partial = b * p.chunks * 2 * c;
   p.stat = 2 * b * groups;
