@@ -5,19 +5,25 @@
 // read and dx written backward, against some 30 operations an element.  Three
 // ways, by the shape (plan below):
 //  rows   one position a sample: a group is one contiguous row, held in registers
-//         from the read to the write, one pass.
-//  block  a workgroup takes a slab of whole groups of one sample and goes over it
-//         twice, the second time out of the caches.
+//         from the read to the write, one pass.  Up to 512 channels a wave or part
+//         of one takes a row (narrow), beyond that a workgroup.
+//  block  a workgroup takes a slab of whole groups of one sample, and holds the first
+//         four rows of every thread from the sums to the write; what is beyond them
+//         it reads a second time, out of the caches.
 //  split  a sample's positions are cut into chunks: a pass for the sums of every
 //         channel of a chunk, a small kernel that joins them, a pass that writes.
 // Variances are sums of squares about the mean (rows), or about a value of the
 // channel (block, split), joined through (count, mean, sum of squares about the
 // mean), so that a mean far from zero costs no digits.  Sums are float32, in an
 // order that depends on the shape alone.
-// bf16: rows, 8192 x 4096, 28 us forward (4.8 TB/s) and 50 for the gradient (4.0);
-// split, four samples of 16,384 x 512 with SiLU, 16 + 5 + 25 us forward and 32 + 5
-// + 37 + 4 for the gradient, whose passes over x and dy run at 4.2 and 5.5 TB/s;
-// block, 64 x 320, 8 us, a chain of latencies.
+// bf16: rows, 8192 x 4096, 27 us forward (4.9 TB/s) and 44 for the gradient (4.6);
+// 55,388 x 249 in fp16 with GELU, odd rows, 19 (2.8 TB/s) and 33 (2.5), where one wave
+// a row and 512 at once, element by element at the row's end, took 360 together;
+// split, four samples of 16,384 x 512 with SiLU, 16 + 5 + 24 us forward and 30 + 5
+// + 36 + 4 for the gradient, whose passes over x and dy run at 4.5 and 5.6 TB/s;
+// block, 64 x 320, 7 us, three samples of 577 x 120 in fp32 10 and 12: a chain of
+// latencies (both passes from memory and every channel's sum over 256 rows by a tree
+// took 8, 13 and 18).
 #include <algorithm>
 
 #include "ops_internal.h"
@@ -27,16 +33,18 @@ namespace {
 
 // ------------------------------------------------------------ rows
 
+// over the LANES lanes of a wave that share threadIdx.x / LANES
+template <int LANES = 64>
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  for (int d = 1; d < LANES; d *= 2) v += __shfl_xor(v, d);
   return v;
 }
 // over the waves of a workgroup; s holds two sets of values in turn, so that one
 // barrier a sum is enough
 template <int THREADS>
 __device__ __forceinline__ float block_sum(float v, float *s, int &turn) {
-  v = wave_sum(v);
+  v = wave_sum<(THREADS < 64 ? THREADS : 64)>(v);
   if constexpr (THREADS > 64) {
     float *q = s + turn * (THREADS / 64);
     turn ^= 1;
@@ -61,7 +69,71 @@ struct Affine {
   }
 };
 
+// Eight elements as they lie in memory, held from their load to their use.
+template <class T>
+struct Held {
+  typename Vec8<T>::type t;
+  __device__ __forceinline__ void get(const T *p, int left) { t = take8(p, left); }
+  __device__ __forceinline__ void to(float (&v)[8]) const {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = float(t[q]);
+  }
+};
+template <>
+struct Held<float> {
+  float t[8];
+  __device__ __forceinline__ void get(const float *p, int left) { load8(p, left, t); }
+  __device__ __forceinline__ void to(float (&v)[8]) const {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = t[q];
+  }
+};
+// Eight channels from c on of a run of n.  Where the run ends inside them the eight
+// that end with it are taken, so that all lanes read whole vectors (element by
+// element the odd lane costs a chain of loads); the first `skip` of those belong to
+// the lane before.  A run below eight: its `left` channels.
+struct Eight {
+  int at, skip, left;
+  __device__ __forceinline__ Eight(int c, int n)
+      : at(max(0, min(c, n - 8))), skip(min(c - at, 8)), left(min(8, n - at)) {}
+  __device__ __forceinline__ bool own(int q) const { return q >= skip && q < left; }
+};
+
 // THREADS a row of `per` channels, NV vectors of eight a thread.
+// Up to 512 channels: as many lanes as a row has vectors, to the next power of two.
+template <class T, int LANES>
+__global__ __launch_bounds__(256) void narrow_kernel(dip_group_norm_args a, int64_t rows) {
+  const int64_t row = int64_t(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  if (row >= rows) return;   // all lanes of a row
+  const uint32_t i = uint32_t(row) / uint32_t(a.groups), g = uint32_t(row) % uint32_t(a.groups);
+  const int per = int(a.c) / a.groups, t = threadIdx.x % LANES;
+  const Eight e(t * 8, per);
+  const int64_t c = int64_t(g) * per + e.at;
+  float v[8], ga[8], be[8];
+  load8(static_cast<const T *>(a.x) + i * a.x_sb + c, e.left, v);
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, e.left, ga, be);
+  const float inv = 1.f / float(per);
+  float sum = 0.f;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) sum += e.own(q) ? v[q] : 0.f;
+  const float mean = wave_sum<LANES>(sum) * inv;
+  sum = 0.f;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    v[q] -= mean;
+    sum += e.own(q) ? v[q] * v[q] : 0.f;
+  }
+  const float rstd = 1.f / sqrtf(wave_sum<LANES>(sum) * inv + a.eps);
+  if (t == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  if (t * 8 >= per) return;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = act_of(v[q] * rstd * ga[q] + be[q], a.act);
+  store8(static_cast<T *>(a.y) + i * a.y_sb + c, e.left, v);   // the skipped ones: what their own lane writes
+}
+
 template <class T, int THREADS, int NV>
 __global__ __launch_bounds__(256) void rows_kernel(dip_group_norm_args a, int64_t rows) {
   constexpr int kRows = 256 / THREADS;
@@ -69,9 +141,9 @@ __global__ __launch_bounds__(256) void rows_kernel(dip_group_norm_args a, int64_
   int turn = 0;
   const int t = threadIdx.x % THREADS;
   const int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / THREADS;
-  if (row >= rows) return;   // whole waves: THREADS is 64, or the workgroup has one row
+  if (row >= rows) return;   // all threads of a row
   const uint32_t i = uint32_t(row) / uint32_t(a.groups), g = uint32_t(row) % uint32_t(a.groups);
-  const int per = int(a.c / a.groups);
+  const int per = int(a.c) / a.groups;
   const int64_t c0 = int64_t(g) * per;
   const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c0;
   T *y = static_cast<T *>(a.y) + i * a.y_sb + c0;
@@ -118,7 +190,7 @@ template <class T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void rows_grad_kernel(dip_group_norm_grad_args a, float *partial) {
   __shared__ float s[2 * 2 * THREADS / 64];
   int turn = 0, turn2 = 0;
-  const int t = threadIdx.x, per = int(a.c / a.groups);
+  const int t = threadIdx.x, per = int(a.c) / a.groups;
   const uint32_t g = blockIdx.y;
   const int64_t c0 = int64_t(g) * per;
   const Affine<T> affine{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)};
@@ -127,15 +199,15 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(dip_group_norm_grad_
   for (int j = 0; j < NV; ++j) affine.get(c0 + (t + j * THREADS) * 8, per - (t + j * THREADS) * 8, ga[j], be[j]);
   const float inv = 1.f / float(per);
   // the next sample's row is asked for before this one's sums are waited for
-  float xn[NV][8], dn[NV][8];
+  Held<T> xn[NV], dn[NV];
   auto fetch = [&](int64_t i) __attribute__((always_inline)) {
     const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c0;
     const T *dy = static_cast<const T *>(a.dy) + i * a.dy_sb + c0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (t + j * THREADS) * 8;
-      load8(x + c, per - c, xn[j]);
-      load8(dy + c, per - c, dn[j]);   // zeros beyond the row
+      xn[j].get(x + c, per - c);
+      dn[j].get(dy + c, per - c);   // zeros beyond the row
     }
   };
   if (int64_t(blockIdx.x) < a.b) fetch(blockIdx.x);
@@ -144,17 +216,20 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(dip_group_norm_grad_
     float xh[NV][8], h[NV][8];
     float m1 = 0.f, m2 = 0.f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      xn[j].to(xh[j]);
+      dn[j].to(h[j]);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        xh[j][q] = (xn[j][q] - mean) * rstd;
-        const float v = a.act == DIP_ACT_NONE ? dn[j][q] : dn[j][q] * act_slope(xh[j][q] * ga[j][q] + be[j][q], a.act);
+        xh[j][q] = (xh[j][q] - mean) * rstd;
+        const float v = a.act == DIP_ACT_NONE ? h[j][q] : h[j][q] * act_slope(xh[j][q] * ga[j][q] + be[j][q], a.act);
         sg[j][q] += v * xh[j][q];
         sb[j][q] += v;
         h[j][q] = v * ga[j][q];
         m1 += h[j][q];
         m2 += h[j][q] * xh[j][q];
       }
+    }
     if (i + gridDim.x < a.b) fetch(i + gridDim.x);
     if (!a.dx) continue;
     m1 = block_sum<THREADS>(m1, s, turn) * inv;
@@ -193,39 +268,43 @@ struct Lanes {
   }
 };
 
-// Adds two values a channel over the workgroup's rows; every thread then finds
-// the sums of channel c at s[c] and s[half + c], half = vectors * 8 * TY.
-__device__ __forceinline__ void channel_sums(const Lanes &l, int vectors, const float (&a)[8], const float (&b)[8],
-                                             float *s) {
-  const int width = vectors * 8, half = width * l.TY;
-  __syncthreads();
-  if (l.on) {
+// Adds two values a channel over the workgroup's TY rows of `width` channels; every
+// thread then finds the sums of channel c at s[c] and s[half + c], half = width TY.
+// s is not in use before.  A thread adds up to sixteen rows, as many threads as
+// that takes side by side, and a second step their sums.
+__device__ __forceinline__ void channel_sums(int width, int ty, int TY, bool on, int at, int skip, const float (&a)[8],
+                                             const float (&b)[8], float *s) {
+  const int half = width * TY;
+  if (on) {
+    float *p = s + ty * width + at;
+    if (skip == 0) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      s[l.ty * width + l.vx * 8 + q] = a[q];
-      s[half + l.ty * width + l.vx * 8 + q] = b[q];
+      for (int q = 0; q < 8; ++q) p[q] = a[q], p[half + q] = b[q];
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (q >= skip) p[q] = a[q], p[half + q] = b[q];
     }
   }
   __syncthreads();
-  for (int h = l.TY / 2; h >= 1; h /= 2) {
-    for (int j = threadIdx.x; j < 2 * h * width; j += blockDim.x) {
-      const int which = j >= h * width, at = (which ? half - h * width : 0) + j;
-      s[at] += s[at + h * width];
+  for (int rows = TY; rows > 1;) {
+    const int parts = rows / min(rows, 16), step = parts * width;
+    for (int j = threadIdx.x; j < 2 * step; j += blockDim.x) {
+      float *p = s + (j >= step ? half + j - step : j), v = p[0];
+#pragma unroll 8
+      for (int r = step; r < rows * width; r += step) v += p[r];
+      p[0] = v;   // row j / width of the half: no other thread of the step reads it
     }
     __syncthreads();
+    rows = parts;
   }
 }
 
-// The sums about a channel's own value k: a = sum (x - k), b = sum (x - k)^2,
-// over rows r0 + ty, .. below r1.
+// The sums about a channel's own value k: a += sum (x - k), b += sum (x - k)^2,
+// over rows r, r + TY, .. below r1.
 template <class T>
-__device__ __forceinline__ void moments(const T *x, int64_t ss, int left, const Lanes &l, int64_t r0, int64_t r1,
-                                        float (&k)[8], float (&a)[8], float (&b)[8]) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) a[q] = b[q] = k[q] = 0.f;
-  if (!l.on || r0 >= r1) return;
-  load8(x + r0 * ss, left, k);
-  int64_t r = r0 + l.ty;
+__device__ __forceinline__ void moments(const T *x, int64_t ss, int left, const Lanes &l, int64_t r, int64_t r1,
+                                        const float (&k)[8], float (&a)[8], float (&b)[8]) {
   for (; r + 3 * l.TY < r1; r += 4 * l.TY) {
     float v[4][8];
 #pragma unroll
@@ -261,25 +340,24 @@ struct Channels {
 };
 
 template <class T>
+__device__ __forceinline__ void write_row(T *y, int left, const Channels &c, int act, float (&v)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = (v[q] - c.mean[q]) * (c.rstd[q] * c.gamma[q]) + c.beta[q];
+  if (act == DIP_ACT_SILU) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = act_of(v[q], DIP_ACT_SILU);
+  } else if (act != DIP_ACT_NONE) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = act_of(v[q], act);
+  }
+  store8(y, left, v);
+}
+
+template <class T>
 __device__ __forceinline__ void write_rows(const T *x, int64_t x_ss, T *y, int64_t y_ss, int left, const Lanes &l,
-                                           int64_t r0, int64_t r1, const Channels &c, int act) {
+                                           int64_t r, int64_t r1, const Channels &c, int act) {
   if (!l.on) return;
-  float scale[8];
-#pragma unroll
-  for (int q = 0; q < 8; ++q) scale[q] = c.rstd[q] * c.gamma[q];
-  auto one = [&](int64_t r, float(&v)[8]) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = (v[q] - c.mean[q]) * scale[q] + c.beta[q];
-    if (act == DIP_ACT_SILU) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = act_of(v[q], DIP_ACT_SILU);
-    } else if (act != DIP_ACT_NONE) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = act_of(v[q], act);
-    }
-    store8(y + r * y_ss, left, v);
-  };
-  int64_t r = r0 + l.ty;
+  auto one = [&](int64_t r, float(&v)[8]) { write_row(y + r * y_ss, left, c, act, v); };
   for (; r + l.TY < r1; r += 2 * l.TY) {
     float v[2][8];
     load8(x + r * x_ss, left, v[0]);
@@ -307,23 +385,23 @@ __device__ __forceinline__ void grad_terms(const Channels &c, int act, float (&x
   }
 }
 
-// a = sum v xh, b = sum v over a thread's rows
+// a += v xh, b += v
+__device__ __forceinline__ void add_grad(const Channels &c, int act, float (&xv)[8], float (&dv)[8], float (&a)[8],
+                                         float (&b)[8]) {
+  grad_terms(c, act, xv, dv);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    a[q] += dv[q] * xv[q];
+    b[q] += dv[q];
+  }
+}
+// the same over rows r, r + TY, .. below r1
 template <class T>
 __device__ __forceinline__ void grad_sums(const T *x, int64_t x_ss, const T *dy, int64_t dy_ss, int left,
-                                          const Lanes &l, int64_t r0, int64_t r1, const Channels &c, int act,
+                                          const Lanes &l, int64_t r, int64_t r1, const Channels &c, int act,
                                           float (&a)[8], float (&b)[8]) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) a[q] = b[q] = 0.f;
   if (!l.on) return;
-  auto add = [&](float(&xv)[8], float(&dv)[8]) {
-    grad_terms(c, act, xv, dv);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      a[q] += dv[q] * xv[q];
-      b[q] += dv[q];
-    }
-  };
-  int64_t r = r0 + l.ty;
+  auto add = [&](float(&xv)[8], float(&dv)[8]) { add_grad(c, act, xv, dv, a, b); };
   for (; r + l.TY < r1; r += 2 * l.TY) {
     float xv[2][8], dv[2][8];
 #pragma unroll
@@ -344,17 +422,21 @@ __device__ __forceinline__ void grad_sums(const T *x, int64_t x_ss, const T *dy,
 
 // dx = rstd (h - m1 - xh m2), h = v gamma
 template <class T>
+__device__ __forceinline__ void write_grad_row(T *dx, int left, const Channels &c, const float (&m1)[8],
+                                               const float (&m2)[8], int act, float (&xv)[8], float (&dv)[8]) {
+  grad_terms(c, act, xv, dv);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) dv[q] = c.rstd[q] * (dv[q] * c.gamma[q] - m1[q] - xv[q] * m2[q]);
+  store8(dx, left, dv);
+}
+template <class T>
 __device__ __forceinline__ void write_grad(const T *x, int64_t x_ss, const T *dy, int64_t dy_ss, T *dx, int64_t dx_ss,
-                                           int left, const Lanes &l, int64_t r0, int64_t r1, const Channels &c,
+                                           int left, const Lanes &l, int64_t r, int64_t r1, const Channels &c,
                                            const float (&m1)[8], const float (&m2)[8], int act) {
   if (!l.on) return;
   auto one = [&](int64_t r, float(&xv)[8], float(&dv)[8]) {
-    grad_terms(c, act, xv, dv);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) dv[q] = c.rstd[q] * (dv[q] * c.gamma[q] - m1[q] - xv[q] * m2[q]);
-    store8(dx + r * dx_ss, left, dv);
+    write_grad_row(dx + r * dx_ss, left, c, m1, m2, act, xv, dv);
   };
-  int64_t r = r0 + l.ty;
   for (; r + l.TY < r1; r += 2 * l.TY) {
     float xv[2][8], dv[2][8];
 #pragma unroll
@@ -373,108 +455,259 @@ __device__ __forceinline__ void write_grad(const T *x, int64_t x_ss, const T *dy
   }
 }
 
-// two values a group (statistics or means), for the groups of eight channels
+// two values a group (statistics or means), for the groups of eight channels from
+// c on; those beyond `left` (at least one) get the last one's
 __device__ __forceinline__ void of_groups(const float *p, const float *r, int64_t c, int per, int left, float (&u)[8],
                                           float (&v)[8]) {
   uint32_t g = uint32_t(c) / uint32_t(per), rest = uint32_t(c) - g * per;   // c < 2^22
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
-    u[q] = q < left ? p[g] : 0.f;
-    v[q] = q < left ? r[g] : 0.f;
-    if (++rest == uint32_t(per)) rest = 0, ++g;
+    u[q] = p[g];
+    v[q] = r[g];
+    if (q + 1 < left && ++rest == uint32_t(per)) rest = 0, ++g;
   }
+}
+
+constexpr int kHeld = 4;   // a thread's rows that a slab reads once
+
+// Lanes for the channels of one group, a power of two, so that each adds up about
+// four of them.
+__device__ __forceinline__ int group_lanes(int per) {
+  int n = 1;
+  while (n < 64 && n * 4 < per) n *= 2;
+  return n;
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int d = 1; d < lanes; d *= 2) v += __shfl_xor(v, d);
+  return v;
 }
 
 // One workgroup: a slab of `groups` whole groups of one sample.
 template <class T>
 __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int groups, int vectors, int lanes_y) {
   extern __shared__ float s[];
-  const Lanes l(vectors, lanes_y);
+  Lanes l(vectors, lanes_y);
   const int tiles = (a.groups + groups - 1) / groups;
-  const int per = int(a.c / a.groups), g0 = int(blockIdx.x % tiles) * groups, slab = min(groups, a.groups - g0) * per;
-  const int64_t i = blockIdx.x / tiles, c0 = int64_t(g0) * per, c = c0 + l.vx * 8;
-  const int left = slab - l.vx * 8;
+  const int per = int(a.c) / a.groups, g0 = int(blockIdx.x % tiles) * groups, count = min(groups, a.groups - g0);
+  const int slab = count * per;
+  const int64_t i = blockIdx.x / tiles;
+  const Eight e(l.vx * 8, slab);
+  const int64_t c = int64_t(g0) * per + e.at;
+  l.on = l.on && l.vx * 8 < slab;
   const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c;
   Channels ch;
-  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
-  float k[8], u[8], v[8];
-  moments(x, a.x_ss, left, l, 0, a.s, k, u, v);
-  channel_sums(l, vectors, u, v, s);
+  float k[8] = {}, u[8] = {}, v[8] = {};
+  Held<T> held[kHeld];
+  if (l.on && a.s > 0) {
+    load8(x, e.left, k);
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) held[j].get(x + min(int64_t(l.ty) + j * l.TY, a.s - 1) * a.x_ss, e.left);
+    Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, e.left, ch.gamma, ch.beta);
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      float w[8];
+      held[j].to(w);
+      if (l.ty + j * l.TY < a.s) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const float d = w[q] - k[q];
+          u[q] += d;
+          v[q] += d * d;
+        }
+      }
+    }
+    moments(x, a.x_ss, e.left, l, l.ty + int64_t(kHeld) * l.TY, a.s, k, u, v);
+  }
   const int width = vectors * 8, half = width * l.TY;
+  channel_sums(width, l.ty, l.TY, l.on, e.at, e.skip, u, v, s);
   // channel c: s[c] its mean, s[half + c] the squares about it
   const float n = float(max(a.s, int64_t(1)));
   if (l.on && l.ty == 0) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const int at = l.vx * 8 + q;
-      const float d = s[at];
-      s[half + at] = above_zero(s[half + at] - d * (d / n));
-      s[at] = k[q] + d / n;
+      if (!e.own(q)) continue;
+      const float d = s[e.at + q];
+      s[half + e.at + q] = above_zero(s[half + e.at + q] - d * (d / n));
+      s[e.at + q] = k[q] + d / n;
     }
   }
   __syncthreads();
   float *stat = s + 2 * half;   // [2][groups]
-  for (int g = threadIdx.x; g < slab / max(per, 1); g += blockDim.x) {
+  const int lanes = group_lanes(per), t = threadIdx.x % lanes, at_once = blockDim.x / lanes;
+  for (int b = 0; b < count; b += at_once) {
+    const int g = b + threadIdx.x / lanes;
+    const float *m = s + min(g, count - 1) * per;
     float mean = 0.f, m2 = 0.f;
-    for (int j = 0; j < per; ++j) mean += s[g * per + j];
-    mean /= float(per);
-    for (int j = 0; j < per; ++j) {
-      const float d = s[g * per + j] - mean;
-      m2 += s[half + g * per + j] + n * d * d;
+#pragma unroll 4
+    for (int j = t; j < per; j += lanes) mean += m[j];
+    mean = lanes_sum(mean, lanes) / float(per);
+#pragma unroll 4
+    for (int j = t; j < per; j += lanes) {
+      const float d = m[j] - mean;
+      m2 += m[half + j] + n * d * d;
     }
-    const float rstd = 1.f / sqrtf(m2 / (n * float(per)) + a.eps);
-    stat[g] = mean;
-    stat[groups + g] = rstd;
-    if (a.mean) a.mean[i * a.groups + g0 + g] = mean;
-    if (a.rstd) a.rstd[i * a.groups + g0 + g] = rstd;
+    const float rstd = 1.f / sqrtf(lanes_sum(m2, lanes) / (n * float(per)) + a.eps);
+    if (t == 0 && g < count) {
+      stat[g] = mean;
+      stat[groups + g] = rstd;
+      if (a.mean) a.mean[i * a.groups + g0 + g] = mean;
+      if (a.rstd) a.rstd[i * a.groups + g0 + g] = rstd;
+    }
   }
   __syncthreads();
-  if (left <= 0) return;
-  of_groups(stat, stat + groups, l.vx * 8, per, left, ch.mean, ch.rstd);
-  write_rows(x, a.x_ss, static_cast<T *>(a.y) + i * a.y_sb + c, a.y_ss, left, l, 0, a.s, ch, a.act);
+  if (!l.on || a.s == 0) return;
+  of_groups(stat, stat + groups, e.at, per, e.left, ch.mean, ch.rstd);
+  T *y = static_cast<T *>(a.y) + i * a.y_sb + c;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int64_t r = l.ty + j * l.TY;
+    float w[8];
+    held[j].to(w);
+    if (r < a.s) write_row(y + r * a.y_ss, e.left, ch, a.act, w);
+  }
+  write_rows(x, a.x_ss, y, a.y_ss, e.left, l, l.ty + int64_t(kHeld) * l.TY, a.s, ch, a.act);
+}
+
+// Sums of dgamma and dbeta of a workgroup's channels: to partial[at][2][c], or, of
+// the only workgroup that has these channels, to the gradients themselves.
+template <class T>
+__device__ __forceinline__ void put_sums(const dip_group_norm_grad_args &a, float *partial, int64_t at, int64_t c0,
+                                         int n, const float *s, int half) {
+  T *dgamma = static_cast<T *>(a.dgamma), *dbeta = static_cast<T *>(a.dbeta);
+  float *p = partial + at * 2 * a.c + c0;
+  for (int j = threadIdx.x; j < n; j += blockDim.x) {
+    if (partial) {
+      p[j] = s[j], p[a.c + j] = s[half + j];
+    } else {
+      if (dgamma) dgamma[c0 + j] = T(s[j]);
+      if (dbeta) dbeta[c0 + j] = T(s[half + j]);
+    }
+  }
 }
 
 template <class T>
 __global__ __launch_bounds__(512) void block_grad_kernel(dip_group_norm_grad_args a, int groups, int vectors,
                                                           int lanes_y, float *partial) {
   extern __shared__ float s[];
-  const Lanes l(vectors, lanes_y);
+  Lanes l(vectors, lanes_y);
   const int tiles = (a.groups + groups - 1) / groups;
-  const int per = int(a.c / a.groups), g0 = int(blockIdx.x % tiles) * groups, slab = min(groups, a.groups - g0) * per;
-  const int64_t i = blockIdx.x / tiles, c0 = int64_t(g0) * per, c = c0 + l.vx * 8;
-  const int left = slab - l.vx * 8;
+  const int per = int(a.c) / a.groups, g0 = int(blockIdx.x % tiles) * groups, count = min(groups, a.groups - g0);
+  const int slab = count * per;
+  const int64_t i = blockIdx.x / tiles, c0 = int64_t(g0) * per;
+  const Eight e(l.vx * 8, slab);
+  const int64_t c = c0 + e.at;
+  l.on = l.on && l.vx * 8 < slab;
   const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c, *dy = static_cast<const T *>(a.dy) + i * a.dy_sb + c;
   Channels ch;
-  of_groups(a.mean + i * a.groups, a.rstd + i * a.groups, c, per, left, ch.mean, ch.rstd);
-  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
-  float u[8], v[8];
-  grad_sums(x, a.x_ss, dy, a.dy_ss, left, l, 0, a.s, ch, a.act, u, v);
-  channel_sums(l, vectors, u, v, s);
-  const int half = vectors * 8 * l.TY;
-  if (partial) {
-    float *p = partial + i * 2 * a.c + c0;
-    for (int j = threadIdx.x; j < slab; j += blockDim.x) p[j] = s[j], p[a.c + j] = s[half + j];
+  float u[8] = {}, v[8] = {};
+  Held<T> hx[kHeld], hd[kHeld];
+  if (l.on) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int64_t r = min(int64_t(l.ty) + j * l.TY, a.s - 1);
+      hx[j].get(x + r * a.x_ss, e.left);
+      hd[j].get(dy + r * a.dy_ss, e.left);
+    }
+    of_groups(a.mean + i * a.groups, a.rstd + i * a.groups, c, per, e.left, ch.mean, ch.rstd);
+    Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, e.left, ch.gamma, ch.beta);
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      float xv[8], dv[8];
+      hx[j].to(xv);
+      hd[j].to(dv);
+      if (l.ty + j * l.TY < a.s) add_grad(ch, a.act, xv, dv, u, v);
+    }
   }
+  grad_sums(x, a.x_ss, dy, a.dy_ss, e.left, l, l.ty + int64_t(kHeld) * l.TY, a.s, ch, a.act, u, v);
+  const int width = vectors * 8, half = width * l.TY;
+  channel_sums(width, l.ty, l.TY, l.on, e.at, e.skip, u, v, s);
+  if (partial || a.b == 1) put_sums<T>(a, partial, i, c0, slab, s, half);
   if (!a.dx) return;
   const T *gamma = static_cast<const T *>(a.gamma);
   float *mean = s + 2 * half;   // [2][groups]
-  for (int g = threadIdx.x; g < slab / per; g += blockDim.x) {
+  const int lanes = group_lanes(per), t = threadIdx.x % lanes, at_once = blockDim.x / lanes;
+  for (int b = 0; b < count; b += at_once) {
+    const int g = b + threadIdx.x / lanes, first = min(g, count - 1) * per;
     float m1 = 0.f, m2 = 0.f;
-    for (int j = 0; j < per; ++j) {
-      const float w = gamma ? float(gamma[c0 + g * per + j]) : 1.f;
-      m2 += w * s[g * per + j];
-      m1 += w * s[half + g * per + j];
+#pragma unroll 4
+    for (int j = t; j < per; j += lanes) {
+      const float w = gamma ? float(gamma[c0 + first + j]) : 1.f;
+      m2 += w * s[first + j];
+      m1 += w * s[half + first + j];
     }
     const float inv = 1.f / (float(a.s) * float(per));
-    mean[g] = m1 * inv;
-    mean[groups + g] = m2 * inv;
+    m1 = lanes_sum(m1, lanes) * inv;
+    m2 = lanes_sum(m2, lanes) * inv;
+    if (t == 0 && g < count) mean[g] = m1, mean[groups + g] = m2;
   }
   __syncthreads();
-  if (left <= 0) return;
+  if (!l.on) return;
   float m1[8], m2[8];
-  of_groups(mean, mean + groups, l.vx * 8, per, left, m1, m2);
-  write_grad(x, a.x_ss, dy, a.dy_ss, static_cast<T *>(a.dx) + i * a.dx_sb + c, a.dx_ss, left, l, 0, a.s, ch, m1, m2,
-             a.act);
+  of_groups(mean, mean + groups, e.at, per, e.left, m1, m2);
+  T *dx = static_cast<T *>(a.dx) + i * a.dx_sb + c;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int64_t r = l.ty + j * l.TY;
+    float xv[8], dv[8];
+    hx[j].to(xv);
+    hd[j].to(dv);
+    if (r < a.s) write_grad_row(dx + r * a.dx_ss, e.left, ch, m1, m2, a.act, xv, dv);
+  }
+  write_grad(x, a.x_ss, dy, a.dy_ss, dx, a.dx_ss, e.left, l, l.ty + int64_t(kHeld) * l.TY, a.s, ch, m1, m2, a.act);
+}
+
+// The gradient of rows of up to 512 channels (one position a sample), LANES lanes a
+// row and 256 / LANES rows at once; dgamma and dbeta as in rows_grad_kernel.
+template <class T, int LANES>
+__global__ __launch_bounds__(256) void narrow_grad_kernel(dip_group_norm_grad_args a, float *partial) {
+  constexpr int kRows = 256 / LANES;
+  __shared__ float s[2 * 256 * 8];
+  const int t = threadIdx.x % LANES, ty = threadIdx.x / LANES, per = int(a.c) / a.groups;
+  const uint32_t g = blockIdx.y;
+  const int64_t c0 = int64_t(g) * per;
+  const Eight e(t * 8, per);
+  const bool on = t * 8 < per;
+  const T *x = static_cast<const T *>(a.x) + c0 + e.at, *dy = static_cast<const T *>(a.dy) + c0 + e.at;
+  const int64_t first = int64_t(blockIdx.x) * kRows + ty, step = int64_t(gridDim.x) * kRows;
+  Held<T> xn, dn;
+  float mean = 0.f, rstd = 0.f;
+  // the next row is asked for before this one's sums are waited for
+  auto fetch = [&](int64_t i) __attribute__((always_inline)) {
+    xn.get(x + i * a.x_sb, e.left);
+    dn.get(dy + i * a.dy_sb, e.left);
+    mean = a.mean[i * a.groups + g];
+    rstd = a.rstd[i * a.groups + g];
+  };
+  if (first < a.b) fetch(first);
+  float ga[8], be[8], sg[8] = {}, sb[8] = {};
+  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c0 + e.at, e.left, ga, be);
+  const float inv = 1.f / float(per);
+  for (int64_t i = first; i < a.b; i += step) {   // all lanes of a row
+    float xh[8], h[8], m1 = 0.f, m2 = 0.f;
+    const float r = rstd;
+    xn.to(xh);
+    dn.to(h);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      xh[q] = (xh[q] - mean) * r;
+      if (a.act != DIP_ACT_NONE) h[q] *= act_slope(xh[q] * ga[q] + be[q], a.act);
+      sg[q] += h[q] * xh[q];
+      sb[q] += h[q];
+      h[q] *= ga[q];
+      m1 += e.own(q) ? h[q] : 0.f;
+      m2 += e.own(q) ? h[q] * xh[q] : 0.f;
+    }
+    if (i + step < a.b) fetch(i + step);
+    if (!a.dx) continue;
+    m1 = wave_sum<LANES>(m1) * inv;
+    m2 = wave_sum<LANES>(m2) * inv;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) h[q] = r * (h[q] - m1 - xh[q] * m2);
+    if (on) store8(static_cast<T *>(a.dx) + i * a.dx_sb + c0 + e.at, e.left, h);   // skipped ones: the same values
+  }
+  if (!a.dgamma && !a.dbeta) return;
+  channel_sums(LANES * 8, ty, kRows, on, e.at, e.skip, sg, sb, s);
+  put_sums<T>(a, partial, blockIdx.x, c0, per, s, LANES * 8 * kRows);
 }
 
 // Split: a workgroup a column tile, chunk and sample, 256 threads.
@@ -502,9 +735,13 @@ __global__ __launch_bounds__(256) void split_sums_kernel(dip_group_norm_args a, 
   const Lanes l(vectors, lanes_y);
   const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, false);
   const int left = int(w.left);
-  float k[8], u[8], v[8];
-  moments(static_cast<const T *>(a.x) + w.i * a.x_sb + w.c, a.x_ss, left, l, w.r0, w.r1, k, u, v);
-  channel_sums(l, vectors, u, v, s);
+  float k[8] = {}, u[8] = {}, v[8] = {};
+  if (l.on && left > 0 && w.r0 < w.r1) {
+    const T *x = static_cast<const T *>(a.x) + w.i * a.x_sb + w.c;
+    load8(x + w.r0 * a.x_ss, left, k);
+    moments(x, a.x_ss, left, l, w.r0 + l.ty, w.r1, k, u, v);
+  }
+  channel_sums(vectors * 8, l.ty, l.TY, l.on, l.vx * 8, 0, u, v, s);
   const int half = vectors * 8 * l.TY;
   if (!l.on || l.ty != 0) return;
   const float n = float(max(w.r1 - w.r0, int64_t(1)));
@@ -570,14 +807,14 @@ __global__ __launch_bounds__(256) void split_write_kernel(dip_group_norm_args a,
   const Lanes l(vectors, lanes_y);
   // the chunks read last come first: they may still be in the caches
   const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, true);
-  const int left = int(w.left), per = int(a.c / a.groups);
+  const int left = int(w.left), per = int(a.c) / a.groups;
   const int64_t i = w.i, c = w.c;
   if (left <= 0) return;
   Channels ch;
   of_groups(stat + i * a.groups, stat + (a.b + i) * a.groups, c, per, left, ch.mean, ch.rstd);
   Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
   write_rows(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<T *>(a.y) + i * a.y_sb + c, a.y_ss, left,
-             l, w.r0, w.r1, ch, a.act);
+             l, w.r0 + l.ty, w.r1, ch, a.act);
 }
 
 template <class T>
@@ -586,15 +823,17 @@ __global__ __launch_bounds__(256) void split_grad_sums_kernel(dip_group_norm_gra
   extern __shared__ float s[];
   const Lanes l(vectors, lanes_y);
   const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, false);
-  const int left = int(w.left), per = int(a.c / a.groups);
+  const int left = int(w.left), per = int(a.c) / a.groups;
   const int64_t i = w.i, c = w.c;
   Channels ch;
-  of_groups(a.mean + i * a.groups, a.rstd + i * a.groups, c, per, left, ch.mean, ch.rstd);
-  Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
-  float u[8], v[8];
-  grad_sums(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<const T *>(a.dy) + i * a.dy_sb + c,
-            a.dy_ss, left, l, w.r0, w.r1, ch, a.act, u, v);
-  channel_sums(l, vectors, u, v, s);
+  float u[8] = {}, v[8] = {};
+  if (left > 0) {
+    of_groups(a.mean + i * a.groups, a.rstd + i * a.groups, c, per, left, ch.mean, ch.rstd);
+    Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, left, ch.gamma, ch.beta);
+    grad_sums(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<const T *>(a.dy) + i * a.dy_sb + c,
+              a.dy_ss, left, l, w.r0 + l.ty, w.r1, ch, a.act, u, v);
+  }
+  channel_sums(vectors * 8, l.ty, l.TY, l.on, l.vx * 8, 0, u, v, s);
   const int half = vectors * 8 * l.TY;
   if (!l.on || l.ty != 0) return;
 #pragma unroll
@@ -661,7 +900,7 @@ __global__ __launch_bounds__(256) void split_grad_write_kernel(dip_group_norm_gr
                                                                int chunks, int64_t chunk, const float *mean) {
   const Lanes l(vectors, lanes_y);
   const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, true);
-  const int left = int(w.left), per = int(a.c / a.groups);
+  const int left = int(w.left), per = int(a.c) / a.groups;
   const int64_t i = w.i, c = w.c;
   if (left <= 0) return;
   Channels ch;
@@ -670,7 +909,7 @@ __global__ __launch_bounds__(256) void split_grad_write_kernel(dip_group_norm_gr
   float m1[8], m2[8];
   of_groups(mean + i * a.groups, mean + (a.b + i) * a.groups, c, per, left, m1, m2);
   write_grad(static_cast<const T *>(a.x) + i * a.x_sb + c, a.x_ss, static_cast<const T *>(a.dy) + i * a.dy_sb + c,
-             a.dy_ss, static_cast<T *>(a.dx) + i * a.dx_sb + c, a.dx_ss, left, l, w.r0, w.r1, ch, m1, m2, a.act);
+             a.dy_ss, static_cast<T *>(a.dx) + i * a.dx_sb + c, a.dx_ss, left, l, w.r0 + l.ty, w.r1, ch, m1, m2, a.act);
 }
 
 // ------------------------------------------------------------ plans
@@ -681,6 +920,7 @@ struct Plan {
   int groups = 1, vectors = 1, lanes_y = 1, threads = 256, tiles = 1;   // block: groups a slab
   int64_t chunk = 0, chunks = 1;                                       // split
   int64_t row_blocks = 1;                                              // rows' gradient
+  int lanes = 8;                                                       // narrow rows
   size_t lds = 0;
   int64_t partial = 0, stat = 0, sums = 0;   // floats
   int64_t stat_at() const { return up16(partial * 4); }
@@ -702,8 +942,15 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   const int64_t per = c / groups;
   if (s == 1 && per <= kRowMost && groups < 65536) {
     p.way = kRows;
-    p.row_blocks = std::max<int64_t>(1, std::min<int64_t>(b, std::max<int64_t>(1, 512 / groups)));
-    p.partial = grad ? p.row_blocks * 2 * c : 0;
+    if (per <= 512) {   // narrow rows: four workgroups a CU
+      while (p.lanes < 64 && p.lanes * 8 < per) p.lanes *= 2;
+      const int64_t at_once = 256 / p.lanes;
+      p.row_blocks = std::max<int64_t>(1, std::min<int64_t>((b + at_once - 1) / at_once, std::max(1, 1024 / groups)));
+    } else {
+      p.row_blocks = std::max<int64_t>(1, std::min<int64_t>(b, std::max(1, 512 / groups)));
+    }
+    // one workgroup a group of narrow rows writes the parameters' gradients itself
+    p.partial = grad && !(per <= 512 && p.row_blocks == 1) ? p.row_blocks * 2 * c : 0;
     return p;
   }
   // a slab of at least 128 bytes of a row, and beyond that as many groups as still
@@ -721,7 +968,7 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
     p.lanes_y = pow2_at_most(std::min<int64_t>(std::max<int64_t>(s, 1), p.threads / p.vectors));
     p.tiles = int((groups + slab - 1) / slab);
     p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4 + size_t(2) * slab * 4;
-    p.partial = grad ? b * 2 * c : 0;
+    p.partial = grad && b > 1 ? b * 2 * c : 0;
     return p;
   }
   p.way = kSplit;
@@ -746,8 +993,15 @@ hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
   const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false);
   const int64_t per = a.c / a.groups, rows = a.b * a.groups;
   if (p.way == kRows) {
-    if (per <= 512)
-      rows_kernel<T, 64, 1><<<dim3(uint32_t((rows + 3) / 4)), dim3(256), 0, st>>>(a, rows);
+    const dim3 narrow(uint32_t((rows + 256 / p.lanes - 1) / (256 / p.lanes)));
+    if (per <= 64)
+      narrow_kernel<T, 8><<<narrow, dim3(256), 0, st>>>(a, rows);
+    else if (per <= 128)
+      narrow_kernel<T, 16><<<narrow, dim3(256), 0, st>>>(a, rows);
+    else if (per <= 256)
+      narrow_kernel<T, 32><<<narrow, dim3(256), 0, st>>>(a, rows);
+    else if (per <= 512)
+      narrow_kernel<T, 64><<<narrow, dim3(256), 0, st>>>(a, rows);
     else if (per <= 1024)
       rows_kernel<T, 64, 2><<<dim3(uint32_t((rows + 3) / 4)), dim3(256), 0, st>>>(a, rows);
     else if (per <= 2048)
@@ -778,7 +1032,7 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
   const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, true);
   const int64_t per = a.c / a.groups;
   float *partial = static_cast<float *>(a.workspace);
-  float *sums = a.dgamma || a.dbeta ? partial : nullptr;
+  float *sums = p.partial > 0 && (a.dgamma || a.dbeta) ? partial : nullptr;
   if (p.way == kSplit) {
     float *mean = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
     const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
@@ -795,8 +1049,14 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
   if (p.way == kRows) {
     rows = p.row_blocks;
     const dim3 grid(uint32_t(p.row_blocks), uint32_t(a.groups));
-    if (per <= 512)
-      rows_grad_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, sums);
+    if (per <= 64)
+      narrow_grad_kernel<T, 8><<<grid, dim3(256), 0, st>>>(a, sums);
+    else if (per <= 128)
+      narrow_grad_kernel<T, 16><<<grid, dim3(256), 0, st>>>(a, sums);
+    else if (per <= 256)
+      narrow_grad_kernel<T, 32><<<grid, dim3(256), 0, st>>>(a, sums);
+    else if (per <= 512)
+      narrow_grad_kernel<T, 64><<<grid, dim3(256), 0, st>>>(a, sums);
     else if (per <= 2048)
       rows_grad_kernel<T, 256, 1><<<grid, dim3(256), 0, st>>>(a, sums);
     else if (per <= 4096)
