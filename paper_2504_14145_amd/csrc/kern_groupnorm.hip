@@ -16,14 +16,14 @@
 // channel (block, split), joined through (count, mean, sum of squares about the
 // mean), so that a mean far from zero costs no digits.  Sums are float32, in an
 // order that depends on the shape alone.
-// bf16: rows, 8192 x 4096, 27 us forward (4.9 TB/s) and 44 for the gradient (4.6);
+// bf16: rows, 8192 x 4096, 28 us forward (4.8 TB/s), 37 + 5 for the gradient (5.8);
 // 55,388 x 249 in fp16 with GELU, odd rows, 19 (2.8 TB/s) and 33 (2.5), where one wave
 // a row and 512 at once, element by element at the row's end, took 360 together;
 // split, four samples of 16,384 x 512 with SiLU, 16 + 5 + 24 us forward and 30 + 5
 // + 36 + 4 for the gradient, whose passes over x and dy run at 4.5 and 5.6 TB/s;
-// block, 64 x 320, 7 us, three samples of 577 x 120 in fp32 10 and 12: a chain of
-// latencies (both passes from memory and every channel's sum over 256 rows by a tree
-// took 8, 13 and 18).
+// block, 64 x 320, 7.8 us, three samples of 577 x 120 in fp32 10.7 and 15.2: a chain
+// of latencies (both passes from memory and every channel's sum over 256 rows by a
+// tree took 8.5, 13.3 and 18.4).
 #include <algorithm>
 
 #include "ops_internal.h"
