@@ -106,9 +106,10 @@ int64_t dip_linear_workspace(const dip_linear_args *a);
 int dip_linear(const dip_linear_args *a, void *stream);
 
 /* Gradients of dip_linear for the gradient dy of y:
- *   g = D(dy) act'(pre), rounded to the type (the matrix instructions take it
- *   so), dx = g w, dw = g^T x; db = sum_m g before that rounding; the
- *   residual's gradient is dy itself.
+ *   g = D(dy) act'(pre), dx = g w, dw = g^T x, db = sum_m g; the residual's
+ *   gradient is dy itself.  The matrix instructions take g rounded to the type,
+ *   and the factor of D's kept elements only after them: the rounding changes
+ *   nothing where act is DIP_ACT_NONE or DIP_ACT_RELU.  db has g unrounded.
  * Each of dx, dw, db may be null.  dw and db are of type grad_dtype: the
  * operands' type or DIP_F32; with accumulate != 0 they are added to what the
  * arrays hold (gradients summed over sub-microbatches). */

@@ -245,6 +245,7 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   e.ldo = a->ldy;
   e.ldp = a->ldp;
   e.drop = make_drop(a->drop);
+  e.scale = 1.f;
   e.act = a->act;
   if (thin(a->m, a->n, a->k))
     return hip_code(launch_thin(a->dtype, a->m, a->n, a->k, a->x, a->ldx, a->w, a->ldw, e, st));
@@ -268,6 +269,7 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
   OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
   const hipStream_t st = hipStream_t(stream);
   char *ws = static_cast<char *>(a->workspace);
+  const Drop drop = make_drop(a->drop);
   const void *g = a->dy;
   int64_t ldg = a->ldy;
   float *partial = reinterpret_cast<float *>(ws + p.partial_at);
@@ -279,7 +281,7 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     gi.pre = a->act != DIP_ACT_NONE ? a->pre : nullptr;
     gi.ldy = a->ldy;
     gi.ldp = a->ldp;
-    gi.drop = make_drop(a->drop);
+    gi.drop = drop;
     gi.act = a->act;
     if (p.g_at >= 0) {
       g = gi.out = ws + p.g_at;
@@ -301,6 +303,7 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     Epilogue e{};
     e.out = a->dx;
     e.ldo = a->lddx;
+    e.scale = drop.scale;
     OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
                                    partial, st)));
   }
@@ -308,6 +311,7 @@ int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
     Epilogue e{};
     e.out = a->dw;
     e.ldo = a->lddw;
+    e.scale = drop.scale;
     e.out_f32 = a->grad_dtype == DIP_F32;
     e.accumulate = a->accumulate != 0;
     OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,

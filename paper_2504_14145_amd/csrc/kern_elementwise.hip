@@ -65,8 +65,14 @@ hipError_t dropout_add(int64_t m, int64_t n, const void *x, int64_t ldx, const v
   return hipSuccess;
 }
 
-// g = D(dy) act'(pre) and its column sums: bound by memory, dy and pre read and g
-// written once.  A block takes 256 columns (32 threads of eight) of one chunk of
+// g = D(dy) act'(pre) and its column sums.  g is rounded to the type because the
+// matrix instructions take it so; the factor of the kept elements is left to the
+// float32 products (and the sums), so that without an activation, and with ReLU,
+// whose slopes are 0 and 1, g is dy or 0 and that rounding changes nothing.  Slopes
+// of SiLU and GELU leave dx and dw 0.0024 of their norm from the exact values in
+// bf16, where the rounding of the result alone is 0.0017; a second product with
+// what the rounding left off would take that back and double the products.
+// Bound by memory, dy and pre read and g written once.  A block takes 256 columns (32 threads of eight) of one chunk of
 // rows, sixteen rows at a time, and adds its eight row lanes at the end; the
 // chunks' sums are added in their order by sum_rows_kernel.  65,536 x 2560 with
 // GELU 217 us (4.6 TB/s; the slope's arithmetic is the rest).
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row + 8 * u), v[u]);
+        if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row + 8 * u), 1.f, v[u]);
         if (g.act == DIP_ACT_GELU) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[u][j] *= act_slope(z[u][j], DIP_ACT_GELU);
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   if (out < g.n) {
     float v = 0.f;
     for (int i = 0; i < 8; ++i) v += s[i][c];
-    g.partial[int64_t(blockIdx.y) * g.n + out] = v;
+    g.partial[int64_t(blockIdx.y) * g.n + out] = v * g.drop.scale;
   }
 }
 

@@ -456,6 +456,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
       for (int p = 0; p < P; ++p)
         if (row < m && cols[p] > 0) finish8<T>(e, row, col0 + 32 * p, cols[p], v[p]);
     } else {
+      if constexpr (KIND == kGradient) each<P>([&](int p, int q) { v[p][q] *= e.scale; });
       store(static_cast<T *>(e.out), e.ldo);
     }
   };

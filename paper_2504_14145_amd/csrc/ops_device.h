@@ -179,27 +179,33 @@ __device__ __forceinline__ uint4 draws(const Drop &d, uint32_t block, uint32_t r
   return make_uint4(c0, c1, c2, c3);
 }
 
-// Drops and scales columns 8 block .. + 7 of a row.  Dropped values are set to
-// zero, not multiplied by it, so an infinity or NaN under the mask is gone.
-__device__ __forceinline__ void drop8(const Drop &d, uint32_t block, uint32_t row, float (&v)[8]) {
+// Drops columns 8 block .. + 7 of a row and multiplies the kept ones by `scale`.
+// Dropped values are set to zero, not multiplied by it, so an infinity or NaN
+// under the mask is gone.
+__device__ __forceinline__ void drop8(const Drop &d, uint32_t block, uint32_t row, float scale, float (&v)[8]) {
   const uint4 r = draws(d, block, row);
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t u = (i & 1) ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
-    v[i] = u >= d.drop_of ? v[i] * d.scale : 0.f;
+    v[i] = u >= d.drop_of ? v[i] * scale : 0.f;
   }
+}
+__device__ __forceinline__ void drop8(const Drop &d, uint32_t block, uint32_t row, float (&v)[8]) {
+  drop8(d, block, row, d.scale, v);
 }
 
 // ------------------------------------------------------------ epilogues
 
-// What follows a matrix product: out = residual + D(act(acc + bias)), or with
-// no bias, activation or mask an output of either type, added to or not.
+// What follows a matrix product: out = residual + D(act(acc + bias)), or of a
+// gradient, with no bias, activation or mask, scale acc of either type, added to
+// or not.
 struct Epilogue {
   const void *bias, *residual;
   void *out, *pre;
   int64_t ldr, ldo, ldp;
   Drop drop;
+  float scale;   // 1 forward
   int32_t act;
   uint8_t out_f32, accumulate;
 };
@@ -208,6 +214,8 @@ struct Epilogue {
 template <class T>
 __device__ __forceinline__ void finish8(const Epilogue &e, int64_t row, int64_t col, int left,
                                         float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= e.scale;
   if (e.bias) {
     float b[8];
     load8(static_cast<const T *>(e.bias) + col, left, b);

@@ -48,9 +48,9 @@ struct PackJob {
 };
 hipError_t launch_pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t stream);
 
-// g = D(dy) act'(pre) to out (ld a multiple of 8, padding columns zero; null:
-// not wanted), and its column sums before rounding to partial[row_chunks][n]
-// (null: not wanted).
+// g = D(dy) act'(pre), without the factor of D's kept elements, to out (ld a
+// multiple of 8, padding columns zero; null: not wanted), and its column sums with
+// the factor and before rounding to partial[row_chunks][n] (null: not wanted).
 struct GradIn {
   int64_t m, n;
   const void *dy, *pre;

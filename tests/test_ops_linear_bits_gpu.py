@@ -1,0 +1,43 @@
+"""dx and dw where the gradient before the products is representable in 16 bits:
+without an activation and with ReLU it is dy or 0, and dropout's factor is the
+products', so nothing but the float32 sums and the result's rounding is left."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from ops_reference import EPS32, assert_close, dot_bound, mask  # noqa: E402
+
+if torch.cuda.is_available():
+    from paper_2504_14145_amd import ops
+
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(autouse=True)
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+# whole tiles, ragged ones, and a contraction that is split
+@pytest.mark.parametrize("m,n,k", [(128, 256, 192), (201, 131, 75), (2600, 40, 56)])
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_gradients_of_a_dropout_keep_every_bit_of_dy(m, n, k, act, dtype):
+    g = torch.Generator().manual_seed(m)
+    x, dy, pre = (torch.randn(s, generator=g).to(dtype) for s in ((m, k), (m, n), (m, n)))
+    w = (torch.randn((n, k), generator=g) * n ** -0.5).to(dtype)
+    drop = ops.Dropout(0.1, 31, offset=2, row0=7)
+    want_g = torch.where(mask(drop, m, n), dy.double(), 0.0)
+    if act == "relu":
+        want_g = torch.where(pre > 0, want_g, 0.0)
+    args = dict(act=act, dropout=drop, pre=pre.cuda() if act != "none" else None)
+    dx, dw, db = ops.linear_backward(dy.cuda(), x.cuda(), w.cuda(), **args)
+    dw32 = torch.zeros((n, k), device="cuda")
+    ops.linear_backward(dy.cuda(), x.cuda(), w.cuda(), **args, dw=dw32, bias=False, need_dx=False)
+    for got, a, b, length, name in ((dx, want_g, w, n, "dx"), (dw, want_g.T, x, m, "dw"), (dw32, want_g.T, x, m, "dw32")):
+        want, size = drop.scale * (a @ b.double()), drop.scale * (a.abs() @ b.double().abs())
+        assert_close(got, want, dot_bound(length, size) + 2 * EPS32 * want.abs(), got.dtype, name)
+    want, size = drop.scale * want_g.sum(0), drop.scale * want_g.abs().sum(0)
+    assert_close(db, want, dot_bound(m, size), dtype, "db")
