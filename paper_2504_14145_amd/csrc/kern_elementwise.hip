@@ -99,7 +99,6 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row + 8 * u), 1.f, v[u]);
         if (g.act == DIP_ACT_GELU) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[u][j] *= act_slope(z[u][j], DIP_ACT_GELU);
@@ -110,6 +109,9 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[u][j] *= act_slope(z[u][j], DIP_ACT_RELU);
         }
+        // after the slope, which is NaN where pre is not finite: dropped ones are 0
+        // whatever they held
+        if (g.drop.drop_of) drop8(g.drop, uint32_t(col / 8), uint32_t(row + 8 * u), 1.f, v[u]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (j >= left) v[u][j] = 0.f;

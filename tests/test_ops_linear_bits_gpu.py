@@ -1,6 +1,7 @@
-"""dx and dw where the gradient before the products is representable in 16 bits:
+"""The gradient between dy and the products.  Where it is representable in 16 bits:
 without an activation and with ReLU it is dy or 0, and dropout's factor is the
-products', so nothing but the float32 sums and the result's rounding is left."""
+products', so nothing but the float32 sums and the result's rounding is left in dx and dw.
+Where an element is dropped: 0, whatever pre holds."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -41,3 +42,24 @@ def test_gradients_of_a_dropout_keep_every_bit_of_dy(m, n, k, act, dtype):
         assert_close(got, want, dot_bound(length, size) + 2 * EPS32 * want.abs(), got.dtype, name)
     want, size = drop.scale * want_g.sum(0), drop.scale * want_g.abs().sum(0)
     assert_close(db, want, dot_bound(m, size), dtype, "db")
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_what_pre_holds_under_the_mask_does_not_matter(act):
+    """NaN and infinities in pre at dropped places: the forward's result there is
+    the residual, so the gradients are those of any finite pre."""
+    m, n, k = 70, 88, 48
+    g = torch.Generator().manual_seed(2)
+    x, dy, pre = (torch.randn(s, generator=g).to(BF16) for s in ((m, k), (m, n), (m, n)))
+    w = torch.randn((n, k), generator=g).to(BF16)
+    drop = ops.Dropout(0.5, 3)
+    keep = mask(drop, m, n)
+    bad = pre.clone()
+    for i, v in enumerate((float("nan"), float("inf"), float("-inf"))):
+        at = torch.zeros((m, n), dtype=torch.bool)
+        at[i::5] = True
+        bad[at & ~keep] = v
+    call = lambda p: ops.linear_backward(dy.cuda(), x.cuda(), w.cuda(), act=act, dropout=drop, pre=p.cuda())  # noqa: E731
+    assert not bool(torch.isfinite(bad).all())
+    for got, want in zip(call(bad), call(pre)):
+        assert bool(torch.isfinite(want).all()) and torch.equal(got, want)
