@@ -25,6 +25,7 @@
 // of latencies (both passes from memory and every channel's sum over 256 rows by a
 // tree took 8.5, 13.3 and 18.4).
 #include <algorithm>
+#include <type_traits>
 
 #include "ops_internal.h"
 
@@ -300,38 +301,123 @@ __device__ __forceinline__ void channel_sums(int width, int ty, int TY, bool on,
   }
 }
 
-// The sums about a channel's own value k: a += sum (x - k), b += sum (x - k)^2,
-// over rows r, r + TY, .. below r1.
-template <class T>
-__device__ __forceinline__ void moments(const T *x, int64_t ss, int left, const Lanes &l, int64_t r, int64_t r1,
-                                        const float (&k)[8], float (&a)[8], float (&b)[8]) {
-  for (; r + 3 * l.TY < r1; r += 4 * l.TY) {
-    float v[4][8];
+// A sum of squares less what its mean was off, which rounding may take below zero.
+// One beyond float32 stays infinite, NaN stays NaN.
+__device__ __forceinline__ float less(float v, float off) { return v < INFINITY ? fmaxf(v - off, 0.f) : v; }
+
+// Joins the threads' moments of `n` rows, of which thread row ty has ty, ty + TY, ..;
+// every thread then finds channel c's mean at s[c] and the squares about it at
+// s[half + c], half = width TY.  s is not in use before.  As above a thread joins up
+// to sixteen rows; the mean is taken twice, the second time about the first, so that
+// it and the squares lose nothing to a row unlike the others.
+__device__ __forceinline__ void channel_moments(int width, int ty, int TY, bool on, int at, int skip, const float (&mean)[8],
+                                                const float (&m2)[8], int64_t n, float *s) {
+  const int half = width * TY;
+  if (on) {
+    float *p = s + ty * width + at;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load8(x + (r + u * l.TY) * ss, left, v[u]);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float d = v[u][q] - k[q];
-        a[q] += d;
-        b[q] += d * d;
-      }
+    for (int q = 0; q < 8; ++q)
+      if (q >= skip) p[q] = mean[q], p[half + q] = m2[q];
   }
-  for (; r < r1; r += l.TY) {
-    float v[8];
-    load8(x + r * ss, left, v);
+  __syncthreads();
+  for (int rows = TY; rows > 1;) {
+    const int parts = rows / min(rows, 16), step = parts * width;
+    // rows seen by the r-th of them: n / rows, and one more of the first n % rows
+    const int shift = __ffs(rows) - 1, more = int(n & (rows - 1));
+    const float few = float(n >> shift);
+    auto join = [&](auto count_) __attribute__((always_inline)) {
+      constexpr int kCount = decltype(count_)::value;
+      for (int j = threadIdx.x; j < step; j += blockDim.x) {
+        float *p = s + j, v[kCount], w[kCount], sum = 0.f, total = 0.f, a = 0.f, b = 0.f, c = 0.f;
+        const int first = j / width;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const float d = v[q] - k[q];
-      a[q] += d;
-      b[q] += d * d;
-    }
+        for (int r = 0; r < kCount; ++r) {
+          v[r] = p[r * step];
+          c += p[half + r * step];
+        }
+#pragma unroll
+        for (int r = 0; r < kCount; ++r) {
+          w[r] = few + (first + r * parts < more ? 1.f : 0.f);
+          sum += w[r] * v[r];
+          total += w[r];
+        }
+        const float inv = total > 0.f ? __builtin_amdgcn_rcpf(total) : 0.f, about = sum * inv;
+#pragma unroll
+        for (int r = 0; r < kCount; ++r) {
+          const float d = v[r] - about, wd = w[r] * d;
+          a += wd;
+          b += wd * d;
+        }
+        // row j / width of either half: no other thread of the step reads them
+        p[0] = about + a * inv;
+        p[half] = c + less(b, a * (a * inv));
+      }
+    };
+    if (rows >= 16) join(std::integral_constant<int, 16>{});
+    else if (rows == 8) join(std::integral_constant<int, 8>{});
+    else if (rows == 4) join(std::integral_constant<int, 4>{});
+    else join(std::integral_constant<int, 2>{});
+    __syncthreads();
+    rows = parts;
   }
 }
 
-// a sum of squares that rounding took below zero; NaN stays
-__device__ __forceinline__ float above_zero(float v) { return v < 0.f ? 0.f : v; }
+// Mean and sum of squares about it of eight channels over the rows a thread has
+// seen.  The mean is held as hi + lo, so that adding to it rounds away nothing that
+// counts.  Four rows are summed about hi and then about their own mean, and joined:
+// no sum is larger than what the rows are apart.
+struct Moments {
+  float n = 0.f, hi[8] = {}, lo[8] = {}, m2[8] = {};
+  // the first `count` of four rows; count at least 1
+  template <bool FOUR>
+  __device__ __forceinline__ void add(float (&v)[4][8], int count) {
+    if (n == 0.f) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) hi[q] = v[0][q];
+    }
+    // reciprocals to a rounding or two: of what the rows are apart
+    const float c = FOUR ? 4.f : float(count), inv = FOUR ? 0.25f : __builtin_amdgcn_rcpf(c), total = n + c,
+                part = n == 0.f ? 1.f : c * __builtin_amdgcn_rcpf(total), both = n * part;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float sum = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u][q] = FOUR || u < count ? v[u][q] - hi[q] : 0.f;
+        sum += v[u][q];
+      }
+      const float mean = sum * inv;
+      float sq = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float d = FOUR || u < count ? v[u][q] - mean : 0.f;
+        sq += d * d;
+      }
+      const float apart = mean - lo[q], low = lo[q] + apart * part, high = hi[q] + low;
+      m2[q] += sq + apart * (apart * both);   // 0 of the first rows, however far apart
+      lo[q] = low - (high - hi[q]);
+      hi[q] = high;
+    }
+    n = total;
+  }
+};
+
+// The moments of rows r, r + TY, .. below r1.
+template <class T>
+__device__ __forceinline__ void moments(const T *x, int64_t ss, int left, const Lanes &l, int64_t r, int64_t r1,
+                                        Moments &m) {
+  float v[4][8];
+  for (; r + 3 * l.TY < r1; r += 4 * l.TY) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load8(x + (r + u * l.TY) * ss, left, v[u]);
+    m.add<true>(v, 4);
+  }
+  if (r >= r1) return;
+  const int count = int((r1 - r + l.TY - 1) / l.TY);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) load8(x + min(r + u * l.TY, r1 - 1) * ss, left, v[u]);
+  m.add<false>(v, count);
+}
 
 // Eight channels' part in the forward's second pass and in both of the
 // gradient's: z = x scale + shift, xh = (x - mean) rstd.
@@ -468,7 +554,7 @@ __device__ __forceinline__ void of_groups(const float *p, const float *r, int64_
   }
 }
 
-constexpr int kHeld = 4;   // a thread's rows that a slab reads once
+constexpr int kHeld = 4;   // a thread's rows that a slab reads once, as many as Moments takes
 
 // Lanes for the channels of one group, a power of two, so that each adds up about
 // four of them.
@@ -496,42 +582,23 @@ __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int g
   l.on = l.on && l.vx * 8 < slab;
   const T *x = static_cast<const T *>(a.x) + i * a.x_sb + c;
   Channels ch;
-  float k[8] = {}, u[8] = {}, v[8] = {};
+  Moments mo;
   Held<T> held[kHeld];
-  if (l.on && a.s > 0) {
-    load8(x, e.left, k);
+  if (l.on && l.ty < a.s) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) held[j].get(x + min(int64_t(l.ty) + j * l.TY, a.s - 1) * a.x_ss, e.left);
     Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, e.left, ch.gamma, ch.beta);
+    float w[kHeld][8];
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) {
-      float w[8];
-      held[j].to(w);
-      if (l.ty + j * l.TY < a.s) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const float d = w[q] - k[q];
-          u[q] += d;
-          v[q] += d * d;
-        }
-      }
-    }
-    moments(x, a.x_ss, e.left, l, l.ty + int64_t(kHeld) * l.TY, a.s, k, u, v);
+    for (int j = 0; j < kHeld; ++j) held[j].to(w[j]);
+    const int64_t count = (a.s - l.ty + l.TY - 1) / l.TY;
+    if (count >= kHeld) mo.add<true>(w, kHeld);
+    else mo.add<false>(w, int(count));
+    moments(x, a.x_ss, e.left, l, l.ty + int64_t(kHeld) * l.TY, a.s, mo);
   }
   const int width = vectors * 8, half = width * l.TY;
-  channel_sums(width, l.ty, l.TY, l.on, e.at, e.skip, u, v, s);
-  // channel c: s[c] its mean, s[half + c] the squares about it
+  channel_moments(width, l.ty, l.TY, l.on, e.at, e.skip, mo.hi, mo.m2, a.s, s);
   const float n = float(max(a.s, int64_t(1)));
-  if (l.on && l.ty == 0) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      if (!e.own(q)) continue;
-      const float d = s[e.at + q];
-      s[half + e.at + q] = above_zero(s[half + e.at + q] - d * (d / n));
-      s[e.at + q] = k[q] + d / n;
-    }
-  }
-  __syncthreads();
   float *stat = s + 2 * half;   // [2][groups]
   const int lanes = group_lanes(per), t = threadIdx.x % lanes, at_once = blockDim.x / lanes;
   for (int b = 0; b < count; b += at_once) {
@@ -735,23 +802,15 @@ __global__ __launch_bounds__(256) void split_sums_kernel(dip_group_norm_args a, 
   const Lanes l(vectors, lanes_y);
   const Part w(l, vectors, tiles, chunks, chunk, a.c, a.s, false);
   const int left = int(w.left);
-  float k[8] = {}, u[8] = {}, v[8] = {};
-  if (l.on && left > 0 && w.r0 < w.r1) {
-    const T *x = static_cast<const T *>(a.x) + w.i * a.x_sb + w.c;
-    load8(x + w.r0 * a.x_ss, left, k);
-    moments(x, a.x_ss, left, l, w.r0 + l.ty, w.r1, k, u, v);
-  }
-  channel_sums(vectors * 8, l.ty, l.TY, l.on, l.vx * 8, 0, u, v, s);
+  Moments mo;
+  if (l.on && left > 0)
+    moments(static_cast<const T *>(a.x) + w.i * a.x_sb + w.c, a.x_ss, left, l, w.r0 + l.ty, w.r1, mo);
+  channel_moments(vectors * 8, l.ty, l.TY, l.on, l.vx * 8, 0, mo.hi, mo.m2, max(w.r1 - w.r0, int64_t(0)), s);
   const int half = vectors * 8 * l.TY;
   if (!l.on || l.ty != 0) return;
-  const float n = float(max(w.r1 - w.r0, int64_t(1)));
-  float *p = partial + w.at * 2 * a.c + w.c;
+  float *p = partial + w.at * 2 * a.c + w.c, u[8], v[8];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const float d = s[l.vx * 8 + q];
-    u[q] = k[q] + d / n;
-    v[q] = above_zero(s[half + l.vx * 8 + q] - d * (d / n));
-  }
+  for (int q = 0; q < 8; ++q) u[q] = s[l.vx * 8 + q], v[q] = s[half + l.vx * 8 + q];
   store8(p, left, u);
   store8(p + a.c, left, v);
 }
@@ -773,8 +832,8 @@ __device__ __forceinline__ void over_chunks(int chunks, int per, F &&f) {
 __global__ __launch_bounds__(256) void split_join_kernel(const float *partial, int64_t s_all, int64_t chunk,
                                                          int chunks, int64_t c, int per, float eps, float *mean,
                                                          float *rstd, float *stat) {
-  __shared__ float s[2 * 4];
-  int turn = 0;
+  __shared__ float s[2 * 4], s2[2 * 4];
+  int turn = 0, turn2 = 0;
   const uint32_t groups = uint32_t(c / per), i = blockIdx.x / groups, g = blockIdx.x % groups;
   const float *p = partial + int64_t(i) * chunks * 2 * c + int64_t(g) * per;
   const float total = float(max(s_all, int64_t(1))) * float(per), full = float(chunk);
@@ -785,14 +844,19 @@ __global__ __launch_bounds__(256) void split_join_kernel(const float *partial, i
   over_chunks(chunks, per, [&](int q, int j) {
     u += (p[int64_t(q) * 2 * c + j] - k) * (q + 1 < chunks ? full : rest);
   });
-  const float m = k + block_sum<256>(u, s, turn) / total;
+  float m = k + block_sum<256>(u, s, turn) / total;
+  // squares about that, and what it is off where k is unlike the other values
+  float off = 0.f;
   u = 0.f;
   over_chunks(chunks, per, [&](int q, int j) {
     const float *v = p + int64_t(q) * 2 * c + j;
-    const float d = v[0] - m;
-    u += v[c] + d * d * (q + 1 < chunks ? full : rest);
+    const float d = v[0] - m, w = d * (q + 1 < chunks ? full : rest);
+    off += w;
+    u += v[c] + d * w;
   });
-  const float r = 1.f / sqrtf(block_sum<256>(u, s, turn) / total + eps);
+  off = block_sum<256>(off, s2, turn2) / total;
+  m += off;
+  const float r = 1.f / sqrtf(less(block_sum<256>(u, s, turn) / total, off * off) + eps);
   if (threadIdx.x == 0) {
     stat[blockIdx.x] = m;
     stat[gridDim.x + blockIdx.x] = r;
