@@ -38,7 +38,7 @@
  *    index range: 2^31 rows, 2^22 columns and strides of a matrix),
  *    DIP_E_UNSUPPORTED (float32 in dip_linear), DIP_E_CAPACITY (workspace too
  *    small; nothing has been done), DIP_E_HIP.  Sizes of zero are legal: nothing
- *    is read, sums over nothing are zero.
+ *    is read, sums over nothing are zero (and so a norm's mean and variance).
  */
 #ifndef DIP_OPS_H
 #define DIP_OPS_H

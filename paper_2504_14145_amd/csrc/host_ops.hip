@@ -343,7 +343,7 @@ int64_t dip_group_norm_workspace(const dip_group_norm_args *a) {
 int dip_group_norm(const dip_group_norm_args *a, void *stream) {
   OPS_CHECK(check_group_norm(a));
   OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, group_norm_workspace(*a)));
-  if (a->b == 0 || a->c == 0) return DIP_OK;
+  if (a->b == 0) return DIP_OK;
   return hip_code(launch_group_norm(*a, hipStream_t(stream)));
 }
 

@@ -25,6 +25,7 @@
 // of latencies (both passes from memory and every channel's sum over 256 rows by a
 // tree took 8.5, 13.3 and 18.4).
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "ops_internal.h"
@@ -584,7 +585,7 @@ __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int g
   Channels ch;
   Moments mo;
   Held<T> held[kHeld];
-  if (l.on && l.ty < a.s) {
+  if (l.on) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) held[j].get(x + min(int64_t(l.ty) + j * l.TY, a.s - 1) * a.x_ss, e.left);
     Affine<T>{static_cast<const T *>(a.gamma), static_cast<const T *>(a.beta)}.get(c, e.left, ch.gamma, ch.beta);
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int g
   }
   const int width = vectors * 8, half = width * l.TY;
   channel_moments(width, l.ty, l.TY, l.on, e.at, e.skip, mo.hi, mo.m2, a.s, s);
-  const float n = float(max(a.s, int64_t(1)));
+  const float n = float(a.s);
   float *stat = s + 2 * half;   // [2][groups]
   const int lanes = group_lanes(per), t = threadIdx.x % lanes, at_once = blockDim.x / lanes;
   for (int b = 0; b < count; b += at_once) {
@@ -622,7 +623,7 @@ __global__ __launch_bounds__(512) void block_kernel(dip_group_norm_args a, int g
     }
   }
   __syncthreads();
-  if (!l.on || a.s == 0) return;
+  if (!l.on) return;
   of_groups(stat, stat + groups, e.at, per, e.left, ch.mean, ch.rstd);
   T *y = static_cast<T *>(a.y) + i * a.y_sb + c;
 #pragma unroll
@@ -836,7 +837,7 @@ __global__ __launch_bounds__(256) void split_join_kernel(const float *partial, i
   int turn = 0, turn2 = 0;
   const uint32_t groups = uint32_t(c / per), i = blockIdx.x / groups, g = blockIdx.x % groups;
   const float *p = partial + int64_t(i) * chunks * 2 * c + int64_t(g) * per;
-  const float total = float(max(s_all, int64_t(1))) * float(per), full = float(chunk);
+  const float total = float(s_all) * float(per), full = float(chunk);
   const float rest = float(s_all - chunk * (chunks - 1));   // rows of the last chunk
   // every value times its count, about the first chunk's first channel
   const float k = p[0];
@@ -976,6 +977,14 @@ __global__ __launch_bounds__(256) void split_grad_write_kernel(dip_group_norm_gr
              a.dy_ss, static_cast<T *>(a.dx) + i * a.dx_sb + c, a.dx_ss, left, l, w.r0 + l.ty, w.r1, ch, m1, m2, a.act);
 }
 
+// The statistics of groups of nothing: mean 0, variance 0.
+__global__ __launch_bounds__(256) void no_values_kernel(int64_t n, float r, float *mean, float *rstd) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) {
+    if (mean) mean[i] = 0.f;
+    if (rstd) rstd[i] = r;
+  }
+}
+
 // ------------------------------------------------------------ plans
 
 enum Way { kRows, kBlock, kSplit };
@@ -1001,6 +1010,7 @@ int pow2_at_most(int64_t n) {
 constexpr int kRowMost = 16384;      // channels a row held in registers
 constexpr int kSlabMost = 4096;      // channels a slab, eight a thread
 
+// of at least one sample, position and channel
 Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   Plan p;
   const int64_t per = c / groups;
@@ -1021,7 +1031,7 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   // leave workgroups for the whole card; where that would leave most of it idle,
   // of eight channels (the lines that slabs share come out of the caches)
   const int64_t least = b * c * elem >= 128 * 256 ? 128 / elem : 8;
-  int64_t slab = std::max<int64_t>(1, std::min<int64_t>(groups, (least + per - 1) / std::max<int64_t>(per, 1)));
+  int64_t slab = std::max<int64_t>(1, std::min<int64_t>(groups, (least + per - 1) / per));
   while (slab * 2 <= groups && slab * 2 * per <= 512 && b * ((groups + slab * 2 - 1) / (slab * 2)) >= 1024) slab *= 2;
   const int64_t blocks = b * ((groups + slab - 1) / slab);
   if (slab * per <= kSlabMost && (s * slab * per <= 32768 || blocks >= 512)) {
@@ -1029,7 +1039,7 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
     p.groups = int(slab);
     p.vectors = int((slab * per + 7) / 8);
     p.threads = s * p.vectors > 256 ? 512 : 256;
-    p.lanes_y = pow2_at_most(std::min<int64_t>(std::max<int64_t>(s, 1), p.threads / p.vectors));
+    p.lanes_y = pow2_at_most(std::min<int64_t>(s, p.threads / p.vectors));
     p.tiles = int((groups + slab - 1) / slab);
     p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4 + size_t(2) * slab * 4;
     p.partial = grad && b > 1 ? b * 2 * c : 0;
@@ -1043,8 +1053,8 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   // chunks for about four workgroups a CU, of at least two rows a thread
   const int64_t most = std::max<int64_t>(1, s / (int64_t(p.lanes_y) * 2));
   p.chunks = std::max<int64_t>(1, std::min<int64_t>(most, 1024 / std::max<int64_t>(1, b * p.tiles)));
-  p.chunk = std::max<int64_t>(1, (s + p.chunks - 1) / p.chunks);   // no positions: one empty chunk
-  p.chunks = std::max<int64_t>(1, (s + p.chunk - 1) / p.chunk);
+  p.chunk = (s + p.chunks - 1) / p.chunks;
+  p.chunks = (s + p.chunk - 1) / p.chunk;
   p.lds = size_t(2) * p.vectors * 8 * p.lanes_y * 4;
   p.partial = b * p.chunks * 2 * c;
   p.stat = 2 * b * groups;
@@ -1141,13 +1151,20 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
 }  // namespace
 
 int64_t group_norm_workspace(const dip_group_norm_args &a) {
-  return a.b > 0 && a.c > 0 ? plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false).bytes() : 0;
+  return a.b > 0 && a.c > 0 && a.s > 0 ? plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false).bytes() : 0;
 }
 int64_t group_norm_grad_workspace(const dip_group_norm_grad_args &a) {
   return a.b > 0 && a.c > 0 && a.s > 0 ? plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, true).bytes() : 0;
 }
 
 hipError_t launch_group_norm(const dip_group_norm_args &a, hipStream_t st) {
+  if (a.s == 0 || a.c == 0) {
+    const int64_t n = a.b * a.groups;
+    if (n == 0 || (!a.mean && !a.rstd)) return hipSuccess;
+    no_values_kernel<<<dim3(uint32_t(std::min<int64_t>((n + 255) / 256, 4096))), dim3(256), 0, st>>>(
+        n, 1.f / std::sqrt(a.eps), a.mean, a.rstd);
+    return hipGetLastError();
+  }
   return a.dtype == DIP_F32   ? forward<float>(a, st)
          : a.dtype == DIP_F16 ? forward<_Float16>(a, st)
                               : forward<__bf16>(a, st);

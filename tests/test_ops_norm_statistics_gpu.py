@@ -54,3 +54,14 @@ def test_huge_values_are_not_nan(s, huge):
     x[0, ::2] = huge
     y, mean, rstd = ops.group_norm(x, 4)
     assert bool((rstd == 0).all()) and bool((y == 0).all()) and bool(torch.isfinite(mean).all())
+
+
+@pytest.mark.parametrize("b,s,c,groups", [(3, 0, 4096, 1), (3, 0, 2056, 1), (2, 0, 8192, 2), (5, 0, 64, 8),
+                                          (2, 0, 40000, 1), (4, 7, 0, 3), (4, 0, 0, 2)])
+def test_statistics_of_nothing(b, s, c, groups):
+    """Mean 0 and variance 0, whatever kernels and memory held before."""
+    ops.group_norm(torch.full((64, 3, 4096), 5.0, device="cuda"), 1)
+    mean, rstd = (torch.full((b, groups), float("nan"), device="cuda") for _ in range(2))
+    x = torch.empty((b, s, c), device="cuda")
+    ops.group_norm(x, groups, eps=0.25, mean=mean, rstd=rstd)
+    assert bool((mean == 0).all()) and bool((rstd == 2).all())
