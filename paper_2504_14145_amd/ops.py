@@ -4,10 +4,11 @@ The operators that the cost tables price -- matrix product with its epilogue,
 dropout whose mask is never stored, group norm (layer norm) with an activation
 -- forward and their gradients, as HIP kernels of ``libdip_sim.so``.  Functions
 take torch device tensors (the last dimension contiguous, other strides free),
-check them, and enqueue on ``stream`` (torch's current one by default).  As in
-the rest of the package PyTorch provides device memory and the stream, nothing
-else: outputs and workspaces come from its allocator where none is given, and
-no call records an autograd graph.
+check them, and enqueue on ``stream`` (torch's current one by default), to which
+results and workspaces that a call allocates belong, as if that stream were the
+current one.  As in the rest of the package PyTorch provides device memory and the
+stream, nothing else: outputs and workspaces come from its allocator where none is
+given, and no call records an autograd graph.
 """
 from __future__ import annotations
 
@@ -200,43 +201,43 @@ def _type(t, name):
     return code, dtype, t.get_device()
 
 
-def _call(name, args, index, stream, used):
-    """Launch on the tensors' device, with a workspace where one is needed."""
+def _call(name, args, index):
+    """Launch on the tensors' device and its current stream, with a workspace where
+    one is needed."""
     if index != _device():
         with _torch.cuda.device(index):
-            return _call(name, args, index, stream, used)
+            return _call(name, args, index)
     run = getattr(_lib, name)
-    handle, other = _stream(stream, index)
+    handle = _raw_stream(index)
     code = run(args, handle)
     if code == E_CAPACITY:
         need = getattr(_lib, name + "_workspace")(args)
-        ws = _empty(need, dtype=_torch.uint8, device=used[0].device)
-        args = args[:-_WORKSPACE.size] + _WORKSPACE.pack(ws.data_ptr(), need)
-        used = (*used, ws)
-        code = run(args, handle)
+        ws = _empty(need, dtype=_torch.uint8, device=_torch.device("cuda", index))
+        code = run(args[:-_WORKSPACE.size] + _WORKSPACE.pack(ws.data_ptr(), need), handle)
     if code:
         _check(code, name)
-    if other is not None:
-        _keep(other, used)
 
 
-def _stream(stream, index):
-    """(its handle, the stream itself where it is not the current one)"""
-    current = _raw_stream(index)
-    if stream is None:
-        return current, None
+def _on(stream, operator, *args):
+    """operator(*args) with ``stream`` (or a handle of one) as the current stream, so
+    that results and workspaces come from its pool: a block of another stream's may
+    still be in use by that stream's pending work, which nothing orders before this
+    call.  What was given belongs to the caller; its memory is not handed out again
+    before ``stream`` has passed the call."""
+    index = args[0].get_device()
     handle = getattr(stream, "cuda_stream", stream)
-    return handle, None if handle == current else stream
-
-
-def _keep(stream, tensors):
-    """Memory that torch's allocator gave to the current stream and that another
-    one works on is not given out again before that one has passed."""
     if not isinstance(stream, _torch.cuda.Stream):
-        stream = _torch.cuda.ExternalStream(stream)
-    for t in tensors:
-        if t is not None:
+        stream = _torch.cuda.ExternalStream(handle, device=_torch.device("cuda", index))
+    elif stream.device.index != index:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{index}")
+    if handle == _raw_stream(index):
+        return operator(*args)
+    with _torch.cuda.stream(stream):
+        out = operator(*args)
+    for t in args:
+        if isinstance(t, _torch.Tensor):
             t.record_stream(stream)
+    return out
 
 
 def linear(x, w, bias=None, act="none", dropout=None, residual=None, pre=None, out=None,
@@ -244,10 +245,12 @@ def linear(x, w, bias=None, act="none", dropout=None, residual=None, pre=None, o
     """``residual + D(act(x w^T + bias))``: x [m, k], w [n, k], bias [n], residual
     and the result [m, n]; float16 or bfloat16, summed in float32.  ``pre``, if
     given, receives ``x w^T + bias``, which linear_backward needs when there is an
-    activation.  A result allocated here belongs to torch's current stream."""
+    activation."""
     if _lib is None:
         _load()
     code, dt, dev = _type(x, "x")
+    if stream is not None:
+        return _on(stream, linear, x, w, bias, act, dropout, residual, pre, out)
     _need(x.dim() == 2 and w.dim() == 2, "x and w are matrices")
     m, k = x.shape
     n = w.shape[0]
@@ -258,7 +261,7 @@ def linear(x, w, bias=None, act="none", dropout=None, residual=None, pre=None, o
                         *_matrix(residual, (m, n), dt, dev, "residual"), *_drop(dropout),
                         *_matrix(out, (m, n), dt, dev, "out"), *_matrix(pre, (m, n), dt, dev, "pre"),
                         0, 0)
-    _call("dip_linear", args, dev, stream, (x, w, bias, residual, pre, out))
+    _call("dip_linear", args, dev)
     return out
 
 
@@ -271,6 +274,9 @@ def linear_backward(dy, x, w, act="none", dropout=None, pre=None, bias=True, nee
     if _lib is None:
         _load()
     code, dt, dev = _type(dy, "dy")
+    if stream is not None:
+        return _on(stream, linear_backward, dy, x, w, act, dropout, pre, bias, need_dx, need_dw, dx, dw, db,
+                   accumulate)
     _need(dy.dim() == 2 and x.dim() == 2 and w.dim() == 2, "dy, x and w are matrices")
     m, n = dy.shape
     k = x.shape[1]
@@ -299,7 +305,7 @@ def linear_backward(dy, x, w, act="none", dropout=None, pre=None, bias=True, nee
                              *_drop(dropout), *_matrix(dx, (m, k), dt, dev, "dx"),
                              *_matrix(dw, (n, k), gt, dev, "dw"), _whole(db, (n,), gt, dev, "db"),
                              _types[gt], int(bool(accumulate)), 0, 0)
-    _call("dip_linear_grad", args, dev, stream, (dy, x, w, pre, dx, dw, db))
+    _call("dip_linear_grad", args, dev)
     return dx, dw, db
 
 
@@ -309,6 +315,8 @@ def dropout_add(x, dropout, residual=None, out=None, stream=None):
     if _lib is None:
         _load()
     code, dt, dev = _type(x, "x")
+    if stream is not None:
+        return _on(stream, dropout_add, x, dropout, residual, out)
     _need(x.dim() == 2, "x is a matrix")
     shape = m, n = x.shape
     if out is None:
@@ -318,13 +326,10 @@ def dropout_add(x, dropout, residual=None, out=None, stream=None):
     py, ldy = _matrix(out, shape, dt, dev, "out")
     if dev != _device():
         with _torch.cuda.device(dev):
-            return dropout_add(x, dropout, residual, out, stream)
-    handle, other = _stream(stream, dev)
-    code = _lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, dropout, py, ldy, handle)
+            return dropout_add(x, dropout, residual, out)
+    code = _lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, dropout, py, ldy, _raw_stream(dev))
     if code:
         _check(code, "dip_dropout_add")
-    if other is not None:
-        _keep(other, (x, residual, out))
     return out
 
 
@@ -336,6 +341,8 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None,
     if _lib is None:
         _load()
     code, dt, dev = _type(x, "x")
+    if stream is not None:
+        return _on(stream, group_norm, x, groups, gamma, beta, eps, act, out, mean, rstd)
     _need(x.dim() == 3, "x is [samples, positions, channels]")
     _need(1 <= groups < 1 << 31, f"{groups} groups")
     shape = b, s, c = x.shape
@@ -350,7 +357,7 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None,
                       _whole(gamma, (c,), dt, dev, "gamma"), _whole(beta, (c,), dt, dev, "beta"),
                       *_rows(out, shape, dt, dev, "out"), _whole(mean, stats, f32, dev, "mean"),
                       _whole(rstd, stats, f32, dev, "rstd"), 0, 0)
-    _call("dip_group_norm", args, dev, stream, (x, gamma, beta, out, mean, rstd))
+    _call("dip_group_norm", args, dev)
     return out, mean, rstd
 
 
@@ -361,6 +368,8 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
     if _lib is None:
         _load()
     code, dt, dev = _type(dy, "dy")
+    if stream is not None:
+        return _on(stream, group_norm_backward, dy, x, mean, rstd, groups, gamma, beta, act, need_dx, need_dparam, dx)
     _need(dy.dim() == 3, "dy is [samples, positions, channels]")
     _need(1 <= groups < 1 << 31, f"{groups} groups")
     _need(mean is not None and rstd is not None, "mean and rstd (the forward's) are needed")
@@ -378,5 +387,5 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
                            _whole(rstd, stats, f32, dev, "rstd"), *_rows(dx, shape, dt, dev, "dx"),
                            dgamma.data_ptr() if dgamma is not None else 0,
                            dbeta.data_ptr() if dbeta is not None else 0, 0, 0)
-    _call("dip_group_norm_grad", args, dev, stream, (dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta))
+    _call("dip_group_norm_grad", args, dev)
     return dx, dgamma, dbeta
