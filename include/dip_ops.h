@@ -35,7 +35,8 @@
  *    the host before anything is launched: DIP_E_INVAL (null or misaligned
  *    pointers, negative sizes, strides below the row, unknown type or
  *    activation, overlapping shapes), DIP_E_RANGE (sizes beyond the kernels'
- *    index range: 2^31 rows, 2^22 columns and strides of a matrix),
+ *    index range: 2^31 rows, 2^22 columns and strides of a matrix, 2^24 tiles of
+ *    256 x 256 of an output),
  *    DIP_E_UNSUPPORTED (float32 in dip_linear), DIP_E_CAPACITY (workspace too
  *    small; nothing has been done), DIP_E_HIP.  Sizes of zero are legal: nothing
  *    is read, sums over nothing are zero (and so a norm's mean and variance).

@@ -2,6 +2,7 @@
 // workspaces and launches.  Nothing here allocates or throws.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "host_state.h"
@@ -45,8 +46,10 @@ int check_drop(const dip_dropout &d, int64_t rows) {
 int check_sizes(int64_t m, int64_t n, int64_t k) {
   if (m < 0 || n < 0 || k < 0) return DIP_E_INVAL;
   if (m >= kMaxRows || n > kMaxCols || k > kMaxCols) return DIP_E_RANGE;
-  // launch grids: at least 16 x 64 elements of an output go to a workgroup
-  if (((m + 15) / 16) * (((n > k ? n : k) + 63) / 64) > INT32_MAX) return DIP_E_RANGE;
+  // outputs are m x n, m x k and n x k: a launch's workgroups of 256 threads, each with
+  // 256 x 256 elements of one, have fewer than 2^32 threads
+  const int64_t tm = (m + 255) / 256, tn = (n + 255) / 256, tk = (k + 255) / 256;
+  if (tm * std::max(tn, tk) >= kMaxTiles || tn * tk >= kMaxTiles) return DIP_E_RANGE;
   return DIP_OK;
 }
 int check_workspace(const void *p, int64_t have, int64_t need) {

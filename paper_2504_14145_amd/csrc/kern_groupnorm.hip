@@ -1062,9 +1062,18 @@ Plan plan(int64_t b, int64_t s, int64_t c, int groups, int elem, bool grad) {
   return p;
 }
 
+// Samples that one launch of each of a plan's kernels takes: a launch has fewer than
+// 2^32 threads, and one sample has at most 2^31.
+int64_t samples_a_launch(const Plan &p, int64_t per, int64_t groups) {
+  const int64_t a_row = per <= 512 ? p.lanes : per <= 1024 ? 64 : 256;
+  const int64_t threads = p.way == kRows    ? groups * a_row
+                          : p.way == kBlock ? int64_t(p.tiles) * p.threads
+                                            : std::max(p.tiles * p.chunks, groups) * 256;
+  return std::max<int64_t>(1, (int64_t(1) << 31) / threads);
+}
+
 template <class T>
-hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
-  const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false);
+hipError_t forward_piece(const dip_group_norm_args &a, const Plan &p, float *partial, float *stat, hipStream_t st) {
   const int64_t per = a.c / a.groups, rows = a.b * a.groups;
   if (p.way == kRows) {
     const dim3 narrow(uint32_t((rows + 256 / p.lanes - 1) / (256 / p.lanes)));
@@ -1091,8 +1100,6 @@ hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
                                                                                       p.lanes_y);
     return hipGetLastError();
   }
-  float *partial = static_cast<float *>(a.workspace);
-  float *stat = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
   const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
   split_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, partial);
   split_join_kernel<<<dim3(uint32_t(rows)), dim3(256), 0, st>>>(partial, a.s, p.chunk, int(p.chunks), a.c, int(per),
@@ -1101,21 +1108,62 @@ hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// f(first sample, samples) over pieces of b samples until one fails.
+template <class F>
+hipError_t pieces(int64_t b, int64_t at_once, F &&f) {
+  for (int64_t i = 0; i < b; i += at_once) {
+    const hipError_t e = f(i, std::min(at_once, b - i));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <class T>
+hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
+  const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, false);
+  float *partial = static_cast<float *>(a.workspace);
+  float *stat = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
+  return pieces(a.b, samples_a_launch(p, a.c / a.groups, a.groups), [&](int64_t i, int64_t n) {
+    dip_group_norm_args q = a;
+    q.b = n;
+    q.x = static_cast<const T *>(a.x) + i * a.x_sb;
+    q.y = static_cast<T *>(a.y) + i * a.y_sb;
+    if (a.mean) q.mean += i * a.groups;
+    if (a.rstd) q.rstd += i * a.groups;
+    return forward_piece<T>(q, p, partial + i * p.chunks * 2 * a.c, stat + i * 2 * a.groups, st);
+  });
+}
+
 template <class T>
 hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
   const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, true);
-  const int64_t per = a.c / a.groups;
+  const int64_t per = a.c / a.groups, at_once = samples_a_launch(p, per, a.groups);
   float *partial = static_cast<float *>(a.workspace);
   float *sums = p.partial > 0 && (a.dgamma || a.dbeta) ? partial : nullptr;
+  auto piece = [&](int64_t i, int64_t n) {
+    dip_group_norm_grad_args q = a;
+    q.b = n;
+    q.dy = static_cast<const T *>(a.dy) + i * a.dy_sb;
+    q.x = static_cast<const T *>(a.x) + i * a.x_sb;
+    q.mean += i * a.groups;
+    q.rstd += i * a.groups;
+    if (a.dx) q.dx = static_cast<T *>(a.dx) + i * a.dx_sb;
+    return q;
+  };
   if (p.way == kSplit) {
-    float *mean = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
-    const dim3 grid(uint32_t(p.tiles * p.chunks * a.b));
-    split_grad_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, partial);
+    float *means = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.stat_at());
     if (sums) sums = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.sums_at());
-    split_grad_join_kernel<T><<<dim3(uint32_t(a.b * a.groups)), dim3(256), 0, st>>>(
-        partial, a.s, int(p.chunks), a.c, int(per), static_cast<const T *>(a.gamma), sums, mean);
-    if (a.dx) split_grad_write_kernel<T><<<grid, dim3(256), 0, st>>>(a, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, mean);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = pieces(a.b, at_once, [&](int64_t i, int64_t n) {
+      const dip_group_norm_grad_args q = piece(i, n);
+      float *part = partial + i * p.chunks * 2 * a.c, *mean = means + i * 2 * a.groups;
+      const dim3 grid(uint32_t(p.tiles * p.chunks * n));
+      split_grad_sums_kernel<T><<<grid, dim3(256), p.lds, st>>>(q, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, part);
+      split_grad_join_kernel<T><<<dim3(uint32_t(n * a.groups)), dim3(256), 0, st>>>(
+          part, a.s, int(p.chunks), a.c, int(per), static_cast<const T *>(a.gamma), sums ? sums + i * 2 * a.c : nullptr,
+          mean);
+      if (a.dx) split_grad_write_kernel<T><<<grid, dim3(256), 0, st>>>(q, p.vectors, p.lanes_y, p.tiles, int(p.chunks), p.chunk, mean);
+      return hipGetLastError();
+    });
     if (e != hipSuccess || !sums) return e;
     return launch_sum_rows(SumRows{sums, a.b, 2 * a.c, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
   }
@@ -1140,8 +1188,12 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
     else
       rows_grad_kernel<T, 512, 4><<<grid, dim3(512), 0, st>>>(a, sums);
   } else {
-    block_grad_kernel<T><<<dim3(uint32_t(p.tiles * a.b)), dim3(p.threads), p.lds, st>>>(
-        a, p.groups, p.vectors, p.lanes_y, sums);
+    const hipError_t e = pieces(a.b, at_once, [&](int64_t i, int64_t n) {
+      block_grad_kernel<T><<<dim3(uint32_t(p.tiles * n)), dim3(p.threads), p.lds, st>>>(
+          piece(i, n), p.groups, p.vectors, p.lanes_y, sums ? sums + i * 2 * a.c : nullptr);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !sums) return e;

@@ -580,6 +580,7 @@ GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows) {
   for (int tile = 0; tile < (a_rows ? 4 : 3); ++tile) {
     const Shape &s = shapes[tile];
     const int64_t tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
+    if (tiles >= kMaxTiles) continue;   // the largest tile fits by the caller's check
     for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * 2 <= steps); ++splits) {
       const int64_t each = (steps + splits - 1) / splits;
       if (splits > 1 && (steps + each - 1) / each != splits) continue;
@@ -611,6 +612,20 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
 
 hipError_t launch_pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t stream) {
   const int64_t na = (a.rows * (a.ldo / 8) + 255) / 256, nb = (b.rows * (b.ldo / 8) + 255) / 256;
+  if (na + nb >= kMaxTiles) {   // a launch's workgroups: one array after the other, by rows
+    for (const PackJob *j : {&a, &b}) {
+      const int64_t most = (kMaxTiles - 1) * 256 / (j->ldo / 8);
+      for (int64_t row = 0; row < j->rows; row += most) {
+        PackJob q = *j;
+        q.rows = std::min(most, j->rows - row);
+        q.p = static_cast<const char *>(j->p) + row * j->ld * 2;
+        q.out = static_cast<char *>(j->out) + row * j->ldo * 2;
+        const hipError_t e = launch_pack(dtype, q, PackJob{}, stream);
+        if (e != hipSuccess) return e;
+      }
+    }
+    return hipSuccess;
+  }
   const dim3 grid(uint32_t(na + nb));
   if (dtype == DIP_BF16)
     pack_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, b, uint32_t(na));

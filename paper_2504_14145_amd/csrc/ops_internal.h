@@ -26,6 +26,7 @@ struct GemmPlan {
   int64_t steps = 0;           // contraction steps a split
   int64_t bytes = 0;           // of partial products
 };
+constexpr int64_t kMaxTiles = int64_t(1) << 24;   // 256-thread workgroups a launch
 GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows);   // by sizes and a's layout (not k_rows)
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
