@@ -172,7 +172,8 @@ int dip_group_norm(const dip_group_norm_args *a, void *stream);
 /* Its gradients: g = dy act'(z), xh = (x - mean) rstd, dgamma = sum g xh and
  * dbeta = sum g over samples and positions, and with h = g gamma
  * dx = rstd (h - mean(h) - xh mean(h xh)), means over the group.  dx, dgamma,
- * dbeta may each be null; they are of the inputs' type. */
+ * dbeta may each be null; dx is of the inputs' type, dgamma and dbeta too or, for
+ * gradients summed over sub-microbatches, float32. */
 typedef struct {
   int64_t b, s, c;
   int32_t groups, dtype, act;
@@ -185,6 +186,8 @@ typedef struct {
   void *dx;
   int64_t dx_sb, dx_ss;
   void *dgamma, *dbeta;      /* [c]                                             */
+  int32_t accumulate;        /* 0: dgamma and dbeta are of the type; else float32 */
+                             /* and added to what the arrays hold               */
   void *workspace;           /* 16-byte aligned, dip_group_norm_grad_workspace() */
   int64_t workspace_bytes;
 } dip_group_norm_grad_args;

@@ -220,8 +220,8 @@ int check_group_norm_grad(const dip_group_norm_grad_args *a) {
   OPS_CHECK(check_vector(a->rstd, 4));
   OPS_CHECK(check_vector(a->gamma, e));
   OPS_CHECK(check_vector(a->beta, e));
-  OPS_CHECK(check_vector(a->dgamma, e));
-  return check_vector(a->dbeta, e);
+  OPS_CHECK(check_vector(a->dgamma, a->accumulate ? 4 : e));
+  return check_vector(a->dbeta, a->accumulate ? 4 : e);
 }
 
 }  // namespace

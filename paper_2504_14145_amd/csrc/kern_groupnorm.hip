@@ -646,6 +646,9 @@ __device__ __forceinline__ void put_sums(const dip_group_norm_grad_args &a, floa
   for (int j = threadIdx.x; j < n; j += blockDim.x) {
     if (partial) {
       p[j] = s[j], p[a.c + j] = s[half + j];
+    } else if (a.accumulate) {
+      if (dgamma) static_cast<float *>(a.dgamma)[c0 + j] += s[j];
+      if (dbeta) static_cast<float *>(a.dbeta)[c0 + j] += s[half + j];
     } else {
       if (dgamma) dgamma[c0 + j] = T(s[j]);
       if (dbeta) dbeta[c0 + j] = T(s[half + j]);
@@ -1134,6 +1137,9 @@ hipError_t forward(const dip_group_norm_args &a, hipStream_t st) {
   });
 }
 
+// of dgamma and dbeta
+int param_type(const dip_group_norm_grad_args &a) { return a.accumulate ? DIP_F32 : a.dtype; }
+
 template <class T>
 hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
   const Plan p = plan(a.b, a.s, a.c, a.groups, a.dtype == DIP_F32 ? 4 : 2, true);
@@ -1165,7 +1171,7 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
       return hipGetLastError();
     });
     if (e != hipSuccess || !sums) return e;
-    return launch_sum_rows(SumRows{sums, a.b, 2 * a.c, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
+    return launch_sum_rows(SumRows{sums, a.b, 2 * a.c, a.c, a.dgamma, a.dbeta, a.accumulate}, param_type(a), st);
   }
   int64_t rows = a.b;
   if (p.way == kRows) {
@@ -1197,7 +1203,7 @@ hipError_t backward(const dip_group_norm_grad_args &a, hipStream_t st) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !sums) return e;
-  return launch_sum_rows(SumRows{partial, rows, 2 * a.c, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
+  return launch_sum_rows(SumRows{partial, rows, 2 * a.c, a.c, a.dgamma, a.dbeta, a.accumulate}, param_type(a), st);
 }
 
 }  // namespace
@@ -1224,7 +1230,7 @@ hipError_t launch_group_norm(const dip_group_norm_args &a, hipStream_t st) {
 
 hipError_t launch_group_norm_grad(const dip_group_norm_grad_args &a, hipStream_t st) {
   if (a.b == 0 || a.s == 0)   // sums over nothing
-    return launch_sum_rows(SumRows{nullptr, 0, 0, a.c, a.dgamma, a.dbeta, 0}, a.dtype, st);
+    return launch_sum_rows(SumRows{nullptr, 0, 0, a.c, a.dgamma, a.dbeta, a.accumulate}, param_type(a), st);
   return a.dtype == DIP_F32   ? backward<float>(a, st)
          : a.dtype == DIP_F16 ? backward<_Float16>(a, st)
                               : backward<__bf16>(a, st);

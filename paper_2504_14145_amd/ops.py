@@ -78,7 +78,7 @@ class _GroupNormGrad(ctypes.Structure):
                 ("act", _i32), ("dy", _vp), ("dy_sb", _i64), ("dy_ss", _i64), ("x", _vp),
                 ("x_sb", _i64), ("x_ss", _i64), ("gamma", _vp), ("beta", _vp), ("mean", _vp),
                 ("rstd", _vp), ("dx", _vp), ("dx_sb", _i64), ("dx_ss", _i64), ("dgamma", _vp),
-                ("dbeta", _vp), ("workspace", _vp), ("workspace_bytes", _i64)]
+                ("dbeta", _vp), ("accumulate", _i32), ("workspace", _vp), ("workspace_bytes", _i64)]
 
 
 # A call's arguments go to the library as the bytes of its struct, in one step.
@@ -362,14 +362,16 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None,
 
 
 def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="none", need_dx=True,
-                        need_dparam=True, dx=None, stream=None):
+                        need_dparam=True, dx=None, stream=None, dgamma=None, dbeta=None, accumulate=False):
     """Gradients (dx, dgamma, dbeta) of group_norm; dgamma and dbeta are None
-    without ``need_dparam`` or where gamma and beta are None."""
+    without ``need_dparam`` or where gamma and beta are None.  They may be given; with
+    ``accumulate`` they have to be, are float32 and are added to."""
     if _lib is None:
         _load()
     code, dt, dev = _type(dy, "dy")
     if stream is not None:
-        return _on(stream, group_norm_backward, dy, x, mean, rstd, groups, gamma, beta, act, need_dx, need_dparam, dx)
+        return _on(stream, group_norm_backward, dy, x, mean, rstd, groups, gamma, beta, act, need_dx, need_dparam, dx, None,
+                   dgamma, dbeta, accumulate)
     _need(dy.dim() == 3, "dy is [samples, positions, channels]")
     _need(1 <= groups < 1 << 31, f"{groups} groups")
     _need(mean is not None and rstd is not None, "mean and rstd (the forward's) are needed")
@@ -379,13 +381,24 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
         dx = None
     elif dx is None:
         dx = dy.new_empty(shape)
-    dgamma = dy.new_empty((c,)) if need_dparam and gamma is not None else None
-    dbeta = dy.new_empty((c,)) if need_dparam and beta is not None else None
+    _need((dgamma is None or gamma is not None) and (dbeta is None or beta is not None),
+          "dgamma and dbeta go with gamma and beta")
+    if accumulate:
+        _need(not need_dparam or ((dgamma is not None or gamma is None) and (dbeta is not None or beta is None)),
+              "accumulate: dgamma and dbeta have to be given")
+    pt = f32 if accumulate else dt
+    if not need_dparam:
+        dgamma = dbeta = None
+    else:
+        if dgamma is None and gamma is not None:
+            dgamma = dy.new_empty((c,))
+        if dbeta is None and beta is not None:
+            dbeta = dy.new_empty((c,))
     args = _pack_norm_grad(b, s, c, groups, code, _act(act), *_rows(dy, shape, dt, dev, "dy"),
                            *_rows(x, shape, dt, dev, "x"), _whole(gamma, (c,), dt, dev, "gamma"),
                            _whole(beta, (c,), dt, dev, "beta"), _whole(mean, stats, f32, dev, "mean"),
                            _whole(rstd, stats, f32, dev, "rstd"), *_rows(dx, shape, dt, dev, "dx"),
-                           dgamma.data_ptr() if dgamma is not None else 0,
-                           dbeta.data_ptr() if dbeta is not None else 0, 0, 0)
+                           _whole(dgamma, (c,), pt, dev, "dgamma"), _whole(dbeta, (c,), pt, dev, "dbeta"),
+                           int(bool(accumulate)), 0, 0)
     _call("dip_group_norm_grad", args, dev)
     return dx, dgamma, dbeta

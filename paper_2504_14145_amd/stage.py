@@ -72,8 +72,6 @@ class Block:
                                        dw=g["w2"], db=g["b2"], accumulate=True)
         dn, _, _ = ops.linear_backward(du, n, self.w1, act=self.act, pre=pre, dw=g["w1"],
                                        db=g["b1"], accumulate=True)
-        dx, dgamma, dbeta = ops.group_norm_backward(dn.unsqueeze(1), x.unsqueeze(1), mean, rstd, 1,
-                                                    self.gamma, self.beta)
-        g["gamma"] += dgamma
-        g["beta"] += dbeta
+        dx, _, _ = ops.group_norm_backward(dn.unsqueeze(1), x.unsqueeze(1), mean, rstd, 1, self.gamma, self.beta,
+                                           dgamma=g["gamma"], dbeta=g["beta"], accumulate=True)
         return ops.dropout_add(dx.squeeze(1), ops.Dropout(0.0, 0), residual=dy)
