@@ -46,17 +46,19 @@ __device__ __forceinline__ i32x4 descriptor(const void *p, uint32_t bytes) {
   return d;
 }
 
-// 16 bytes a lane from the buffer straight to LDS: lds_at(to, OFF), then
-// load_lds(d, offset) loads to to + OFF + 16 lane.  Written out, because for the
-// builtin the compiler waits for all loads before any LDS read that follows; the
-// waits below are this file's own.  No register receives the data, the offset is
-// read when the instruction issues, and the no-op is the wait that a new M0 needs.
+// 16 bytes a lane from the buffer straight to LDS address to + OFF + 16 lane.
+// Written out, because for the builtin the compiler waits for all loads before any
+// LDS read that follows; the waits below are this file's own.  No register receives
+// the data, the offset is read when the instruction issues, and the no-op is the wait
+// that a new M0 needs.  M0, the LDS address, is a value that the first statement gives
+// and the second takes, so the compiler leaves it alone between them (in one statement
+// the allocation of the 256 x 256 forward's registers falls apart: 8192^3 1123 us
+// against 752).
 template <int OFF>
-__device__ __forceinline__ void lds_at(uint32_t to) {
-  asm volatile("s_add_u32 m0, %0, %1" : : "s"(to), "n"(OFF) : "scc", "memory");
-}
-__device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t offset) {
-  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(d) : "memory");
+__device__ __forceinline__ void load_lds(const i32x4 &d, uint32_t offset, uint32_t to) {
+  uint32_t at;
+  asm volatile("s_add_u32 %0, %1, %2" : "={m0}"(at) : "s"(to), "n"(OFF) : "scc", "memory");
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(d), "{m0}"(at) : "memory");
 }
 
 // Where a row's 16-byte chunks sit in LDS when the contraction runs along rows:
@@ -314,24 +316,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
   int left = __builtin_amdgcn_readfirstlane(int((k1 - k0 + kStep - 1) / kStep));
   const uint32_t last = uint32_t(k1 - k0 - int64_t(left - 1) * kStep);
   auto present = [&](int steps) { return steps > 1 ? uint32_t(kStep) : steps == 1 ? last : 0u; };
-  auto aim = [&](auto j_) __attribute__((always_inline)) {
-    constexpr int j = decltype(j_)::value, i = Order::index(j);
-    lds_at<i * kThreads * 16>(Order::of_a(j) ? sa.to : sb.to);
-  };
   auto load = [&](auto j_) __attribute__((always_inline)) {
     constexpr int j = decltype(j_)::value, i = Order::index(j);
-    if constexpr (Order::of_a(j)) load_lds(sa.desc, sa.voff[i]);
-    else load_lds(sb.desc, sb.voff[i]);
+    if constexpr (Order::of_a(j)) load_lds<i * kThreads * 16>(sa.desc, sa.voff[i], sa.to);
+    else load_lds<i * kThreads * 16>(sb.desc, sb.voff[i], sb.to);
   };
   if (left > 0) {
     unrolled<R>([&](auto p_) __attribute__((always_inline)) {
       constexpr int p = decltype(p_)::value;
       sa.begin(lds_a + p * StageA::kBytes, present(left - p), wave);
       sb.begin(lds_b + p * StageB::kBytes, present(left - p), wave);
-      unrolled<p + 1 < R ? kLoads : kFirst>([&](auto j_) __attribute__((always_inline)) {
-        aim(j_);
-        load(j_);
-      });
+      unrolled<p + 1 < R ? kLoads : kFirst>(load);
     });
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((R - 2) * kLoads + kFirst) : "memory");
     __builtin_amdgcn_s_barrier();
@@ -377,7 +372,6 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
             constexpr int at = (ahead ? r : s) * kWay + o - 1;
             if constexpr (at < FN) w[ahead ? 0 : 1][at] = rb.read(at, ahead ? 0 : 1);
           } else {
-            aim(std::integral_constant<int, d0 + o - 1 - n_w>{});
             load(std::integral_constant<int, d0 + o - 1 - n_w>{});
           }
         });
