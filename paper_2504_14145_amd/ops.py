@@ -8,12 +8,14 @@ check them, and enqueue on ``stream`` (torch's current one by default), to which
 results and workspaces that a call allocates belong, as if that stream were the
 current one.  As in the rest of the package PyTorch provides device memory and the
 stream, nothing else: outputs and workspaces come from its allocator where none is
-given, and no call records an autograd graph.
+given, and no call records an autograd graph: a forward of tensors that require
+gradients, where torch records them, warns that its result is cut off from theirs.
 """
 from __future__ import annotations
 
 import ctypes
 import struct
+import warnings
 
 from . import E_CAPACITY, _check, load
 
@@ -98,12 +100,13 @@ _torch = None
 _empty = None
 _raw_stream = None   # device index -> handle of torch's current stream
 _device = None       # () -> index of the current device
+_recording = None    # () -> whether torch records gradients
 _types = {}
 
 
 def _load():
     """The library with the operators' signatures, and torch."""
-    global _lib, _torch, _empty, _raw_stream, _device
+    global _lib, _torch, _empty, _raw_stream, _device, _recording
     if _lib is None:
         import torch
         lib = load()
@@ -119,6 +122,7 @@ def _load():
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                               lambda index: torch.cuda.current_stream(index).cuda_stream)
         _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _recording = torch.is_grad_enabled
         _torch, _empty, _lib = torch, torch.empty, lib
     return _lib
 
@@ -129,6 +133,11 @@ _NO_DROP = (0, 0, 0, 0)
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
+
+
+def _cut_off(name):
+    warnings.warn(f"{name} records no gradients: its result is cut off from tensors that require them; run its "
+                  f"backward yourself, or call it without recording (torch.no_grad, detach)", stacklevel=3)
 
 
 def _act(name) -> int:
@@ -261,6 +270,9 @@ def linear(x, w, bias=None, act="none", dropout=None, residual=None, pre=None, o
                         *_matrix(residual, (m, n), dt, dev, "residual"), *_drop(dropout),
                         *_matrix(out, (m, n), dt, dev, "out"), *_matrix(pre, (m, n), dt, dev, "pre"),
                         0, 0)
+    if _recording() and (x.requires_grad or w.requires_grad or bias is not None and bias.requires_grad
+                         or residual is not None and residual.requires_grad):
+        _cut_off("linear")
     _call("dip_linear", args, dev)
     return out
 
@@ -327,6 +339,8 @@ def dropout_add(x, dropout, residual=None, out=None, stream=None):
     if dev != _device():
         with _torch.cuda.device(dev):
             return dropout_add(x, dropout, residual, out)
+    if _recording() and (x.requires_grad or residual is not None and residual.requires_grad):
+        _cut_off("dropout_add")
     code = _lib.dip_dropout_add(code, m, n, px, ldx, pr, ldr, dropout, py, ldy, _raw_stream(dev))
     if code:
         _check(code, "dip_dropout_add")
@@ -357,6 +371,9 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None,
                       _whole(gamma, (c,), dt, dev, "gamma"), _whole(beta, (c,), dt, dev, "beta"),
                       *_rows(out, shape, dt, dev, "out"), _whole(mean, stats, f32, dev, "mean"),
                       _whole(rstd, stats, f32, dev, "rstd"), 0, 0)
+    if _recording() and (x.requires_grad or gamma is not None and gamma.requires_grad
+                         or beta is not None and beta.requires_grad):
+        _cut_off("group_norm")
     _call("dip_group_norm", args, dev)
     return out, mean, rstd
 
