@@ -151,7 +151,8 @@ int dip_dropout_add(int32_t dtype, int64_t m, int64_t n, const void *x, int64_t 
  * With s = 1 and groups = 1 this is a layer norm of b rows.  gamma and beta may
  * be null (1 and 0).  mean and rstd: float32 [b][groups], outputs of the forward
  * and inputs of the gradient; null in the forward where no gradient follows.
- * Strides in elements: sb between samples, ss between positions. */
+ * Strides in elements, up to 2^46: sb between samples, ss between positions, in
+ * either order ([b][s][c] or [s][b][c]). */
 typedef struct {
   int64_t b, s, c;
   int32_t groups, dtype, act;

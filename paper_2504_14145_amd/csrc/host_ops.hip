@@ -185,14 +185,17 @@ int check_norm(int64_t b, int64_t s, int64_t c, int32_t groups, int32_t dtype, i
   if (b * groups > INT32_MAX || s * (c / groups) > (int64_t(1) << 40)) return DIP_E_RANGE;
   return DIP_OK;
 }
-// [b][s][c] with the given strides: positions and samples that do not overlap
+// [b][s][c] with the given strides: positions and samples that do not overlap, either
+// of them the outer one; a stride that nothing steps over may be anything
 int check_rows(const void *p, int64_t b, int64_t s, int64_t c, int64_t sb, int64_t ss, int elem) {
   if (b == 0 || s == 0 || c == 0) return DIP_OK;
   if (!p || reinterpret_cast<uintptr_t>(p) % elem) return DIP_E_INVAL;
-  if (s > 1 && ss < c) return DIP_E_INVAL;
-  if (ss > (int64_t(1) << 31) || sb > (int64_t(1) << 46)) return DIP_E_RANGE;
-  if (b > 1 && sb < (s > 1 ? (s - 1) * ss + c : c)) return DIP_E_INVAL;
-  return DIP_OK;
+  if ((s > 1 && ss < c) || (b > 1 && sb < c)) return DIP_E_INVAL;
+  if ((s > 1 && ss > (int64_t(1) << 46)) || (b > 1 && sb > (int64_t(1) << 46))) return DIP_E_RANGE;
+  if (b == 1 || s == 1) return DIP_OK;
+  // outer >= (n - 1) inner + c, without the product
+  const int64_t outer = std::max(sb, ss), inner = std::min(sb, ss), n = sb >= ss ? s : b;
+  return (outer - c) / inner >= n - 1 ? DIP_OK : DIP_E_INVAL;
 }
 
 int check_group_norm(const dip_group_norm_args *a) {

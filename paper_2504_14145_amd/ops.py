@@ -3,7 +3,7 @@
 The operators that the cost tables price -- matrix product with its epilogue,
 dropout whose mask is never stored, group norm (layer norm) with an activation
 -- forward and their gradients, as HIP kernels of ``libdip_sim.so``.  Functions
-take torch device tensors (the last dimension contiguous, other strides free),
+take torch device tensors (the last dimension contiguous, rows that do not overlap),
 check them, and enqueue on ``stream`` (torch's current one by default), to which
 results and workspaces that a call allocates belong, as if that stream were the
 current one.  As in the rest of the package PyTorch provides device memory and the
@@ -170,7 +170,7 @@ def _matrix(t, shape, dtype, index, name):
     try:
         ld, one = t.stride()
         if t.shape == shape and t.dtype is dtype and t.get_device() == index and (one == 1 or shape[1] <= 1):
-            return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
+            return t.data_ptr(), ld if shape[0] > 1 else -(-shape[1] // 8) * 8   # one row: any
     except (AttributeError, ValueError):
         pass
     _refuse(t, shape, dtype, index, name)
