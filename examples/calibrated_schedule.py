@@ -2,8 +2,9 @@
 
     python examples/calibrated_schedule.py [--workload 2] [--candidates 4096]
 
-1. runs one layer block of each module forward and backward with the stage
-   operators, kept and recomputed, and checks that both give the same gradients;
+1. runs one layer block of each module's sizes (the MLP without a gate) forward
+   and backward with the stage operators, kept and recomputed, and checks that both
+   give the same gradients;
 2. times the operators at the workload's token counts and fits the cost tables'
    coefficients to them (kinds without an operator here keep a factor of 1 on
    the card's nominal rates);

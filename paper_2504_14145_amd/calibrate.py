@@ -30,20 +30,27 @@ class Sample:
     name: str
 
 
-def _time(run, repeats: int, calls: int = 10) -> float:
-    """Median seconds of a call of ``run`` among others on the current stream."""
+CALLS = 10                # timed in a row
+APART = 1 << 29           # bytes between two uses of an array: twice the memory-side cache
+
+
+def _time(run, sets, repeats: int) -> float:
+    """Median seconds of a call of ``run`` among others on the current stream, each on
+    the next of ``sets`` of arrays, none of which the caches hold."""
     import torch
-    run()
-    run()
+    run(sets[0])
+    run(sets[-1])
+    other = torch.empty(APART, dtype=torch.uint8, device="cuda")
     times = []
     for _ in range(repeats):
+        other.zero_()
         a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
         a.record()
-        for _ in range(calls):
-            run()
+        for i in range(CALLS):
+            run(sets[i % len(sets)])
         b.record()
         b.synchronize()
-        times.append(a.elapsed_time(b) * 1e-3 / calls)
+        times.append(a.elapsed_time(b) * 1e-3 / CALLS)
     return sorted(times)[len(times) // 2]
 
 
@@ -51,35 +58,38 @@ def measure(modules, tokens, tp: int = 4, p: float = 0.1, repeats: int = 7, dtyp
             device="cuda") -> list:
     """Samples of every module (hidden, ffn) at every token count: the MLP's two
     products, one with the activation and one with dropout and the residual in
-    its epilogue, and the layer norm, forward and backward."""
+    its epilogue, and the layer norm, forward and backward, on arrays from memory."""
     import torch
     dtype = torch.bfloat16 if dtype is None else dtype
     out = []
     drop = ops.Dropout(p, 1) if p else None
     for h, f in modules:
         f = f // tp
-        w1, w2, gamma, beta = (torch.empty(s, dtype=dtype, device=device).normal_(0, 0.02)
-                               for s in ((f, h), (h, f), (h,), (h,)))
+        gamma, beta = (torch.empty(h, dtype=dtype, device=device).normal_(0, 0.02) for _ in range(2))
         for t in tokens:
-            x, u = (torch.empty((t, c), dtype=dtype, device=device).normal_() for c in (h, f))
-            pre = torch.empty_like(u)
+            sets = []
+            for _ in range(min(CALLS, -(-APART // (t * min(h, f) * gamma.element_size())))):
+                x, u = (torch.empty((t, c), dtype=dtype, device=device).normal_() for c in (h, f))
+                w1, w2 = (torch.empty(s, dtype=dtype, device=device).normal_(0, 0.02) for s in ((f, h), (h, f)))
+                sets.append((x, u, torch.empty_like(u), w1, w2, x.unsqueeze(1)))
             calls = (
-                ("MLP in", lambda: ops.linear(x, w1, act="gelu", pre=pre),
-                 lambda: ops.linear_backward(u, x, w1, act="gelu", pre=pre, bias=False)),
-                ("MLP out", lambda: ops.linear(u, w2, dropout=drop, residual=x),
-                 lambda: ops.linear_backward(x, u, w2, dropout=drop, bias=False)))
+                ("MLP in", lambda a: ops.linear(a[0], a[3], act="gelu", pre=a[2]),
+                 lambda a: ops.linear_backward(a[1], a[0], a[3], act="gelu", pre=a[2], bias=False)),
+                ("MLP out", lambda a: ops.linear(a[1], a[4], dropout=drop, residual=a[0]),
+                 lambda a: ops.linear_backward(a[0], a[1], a[4], dropout=drop, bias=False)))
             fop, mem = 2.0 * t * h * f, 2.0 * (t * h + h * f + t * f)
             for name, forward, backward in calls:
-                out.append(Sample(K_GEMM, fop, mem, _time(forward, repeats), f"{name} {t} x {h} x {f}"))
-                out.append(Sample(K_GEMM, 2 * fop, 2 * mem, _time(backward, repeats),
+                for a in sets:
+                    forward(a)
+                out.append(Sample(K_GEMM, fop, mem, _time(forward, sets, repeats), f"{name} {t} x {h} x {f}"))
+                out.append(Sample(K_GEMM, 2 * fop, 2 * mem, _time(backward, sets, repeats),
                                   f"{name} {t} x {h} x {f} backward"))
-            x3 = x.unsqueeze(1)
-            _, mean, rstd = ops.group_norm(x3, 1, gamma, beta)
+            _, mean, rstd = ops.group_norm(sets[0][5], 1, gamma, beta)
             fop, mem = 8.0 * t * h, 4.0 * t * h
-            out.append(Sample(K_ELEM, fop, mem, _time(lambda: ops.group_norm(x3, 1, gamma, beta), repeats),
+            out.append(Sample(K_ELEM, fop, mem, _time(lambda a: ops.group_norm(a[5], 1, gamma, beta), sets, repeats),
                               f"layer norm {t} x {h}"))
             out.append(Sample(K_ELEM, 2 * fop, 2 * mem, _time(
-                lambda: ops.group_norm_backward(x3, x3, mean, rstd, 1, gamma, beta), repeats),
+                lambda a: ops.group_norm_backward(a[5], a[5], mean, rstd, 1, gamma, beta), sets, repeats),
                 f"layer norm {t} x {h} backward"))
     return out
 
