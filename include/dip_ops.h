@@ -178,6 +178,8 @@ int dip_group_norm(const dip_group_norm_args *a, void *stream);
 typedef struct {
   int64_t b, s, c;
   int32_t groups, dtype, act;
+  int32_t accumulate;        /* 0: dgamma and dbeta are of the type; else float32 */
+                             /* and added to what the arrays hold               */
   const void *dy;
   int64_t dy_sb, dy_ss;
   const void *x;
@@ -187,8 +189,6 @@ typedef struct {
   void *dx;
   int64_t dx_sb, dx_ss;
   void *dgamma, *dbeta;      /* [c]                                             */
-  int32_t accumulate;        /* 0: dgamma and dbeta are of the type; else float32 */
-                             /* and added to what the arrays hold               */
   void *workspace;           /* 16-byte aligned, dip_group_norm_grad_workspace() */
   int64_t workspace_bytes;
 } dip_group_norm_grad_args;

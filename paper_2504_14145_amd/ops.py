@@ -77,10 +77,10 @@ class _GroupNorm(ctypes.Structure):
 
 class _GroupNormGrad(ctypes.Structure):
     _fields_ = [("b", _i64), ("s", _i64), ("c", _i64), ("groups", _i32), ("dtype", _i32),
-                ("act", _i32), ("dy", _vp), ("dy_sb", _i64), ("dy_ss", _i64), ("x", _vp),
+                ("act", _i32), ("accumulate", _i32), ("dy", _vp), ("dy_sb", _i64), ("dy_ss", _i64), ("x", _vp),
                 ("x_sb", _i64), ("x_ss", _i64), ("gamma", _vp), ("beta", _vp), ("mean", _vp),
                 ("rstd", _vp), ("dx", _vp), ("dx_sb", _i64), ("dx_ss", _i64), ("dgamma", _vp),
-                ("dbeta", _vp), ("accumulate", _i32), ("workspace", _vp), ("workspace_bytes", _i64)]
+                ("dbeta", _vp), ("workspace", _vp), ("workspace_bytes", _i64)]
 
 
 # A call's arguments go to the library as the bytes of its struct, in one step.
@@ -411,11 +411,10 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
             dgamma = dy.new_empty((c,))
         if dbeta is None and beta is not None:
             dbeta = dy.new_empty((c,))
-    args = _pack_norm_grad(b, s, c, groups, code, _act(act), *_rows(dy, shape, dt, dev, "dy"),
+    args = _pack_norm_grad(b, s, c, groups, code, _act(act), int(bool(accumulate)), *_rows(dy, shape, dt, dev, "dy"),
                            *_rows(x, shape, dt, dev, "x"), _whole(gamma, (c,), dt, dev, "gamma"),
                            _whole(beta, (c,), dt, dev, "beta"), _whole(mean, stats, f32, dev, "mean"),
                            _whole(rstd, stats, f32, dev, "rstd"), *_rows(dx, shape, dt, dev, "dx"),
-                           _whole(dgamma, (c,), pt, dev, "dgamma"), _whole(dbeta, (c,), pt, dev, "dbeta"),
-                           int(bool(accumulate)), 0, 0)
+                           _whole(dgamma, (c,), pt, dev, "dgamma"), _whole(dbeta, (c,), pt, dev, "dbeta"), 0, 0)
     _call("dip_group_norm_grad", args, dev)
     return dx, dgamma, dbeta
