@@ -398,23 +398,32 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None, act="n
         dx = None
     elif dx is None:
         dx = dy.new_empty(shape)
-    _need((dgamma is None or gamma is not None) and (dbeta is None or beta is not None),
-          "dgamma and dbeta go with gamma and beta")
-    if accumulate:
-        _need(not need_dparam or ((dgamma is not None or gamma is None) and (dbeta is not None or beta is None)),
+    pt = dt
+    if accumulate or dgamma is not None or dbeta is not None:
+        pt = f32 if accumulate else dt
+        _need((dgamma is None or gamma is not None) and (dbeta is None or beta is not None),
+              "dgamma and dbeta go with gamma and beta")
+        _need(not accumulate or not need_dparam or ((dgamma is not None or gamma is None)
+                                                    and (dbeta is not None or beta is None)),
               "accumulate: dgamma and dbeta have to be given")
-    pt = f32 if accumulate else dt
+    pg = pb = 0
     if not need_dparam:
         dgamma = dbeta = None
     else:
-        if dgamma is None and gamma is not None:
+        if dgamma is not None:
+            pg = _whole(dgamma, (c,), pt, dev, "dgamma")
+        elif gamma is not None:
             dgamma = dy.new_empty((c,))
-        if dbeta is None and beta is not None:
+            pg = dgamma.data_ptr()
+        if dbeta is not None:
+            pb = _whole(dbeta, (c,), pt, dev, "dbeta")
+        elif beta is not None:
             dbeta = dy.new_empty((c,))
+            pb = dbeta.data_ptr()
     args = _pack_norm_grad(b, s, c, groups, code, _act(act), int(bool(accumulate)), *_rows(dy, shape, dt, dev, "dy"),
                            *_rows(x, shape, dt, dev, "x"), _whole(gamma, (c,), dt, dev, "gamma"),
                            _whole(beta, (c,), dt, dev, "beta"), _whole(mean, stats, f32, dev, "mean"),
                            _whole(rstd, stats, f32, dev, "rstd"), *_rows(dx, shape, dt, dev, "dx"),
-                           _whole(dgamma, (c,), pt, dev, "dgamma"), _whole(dbeta, (c,), pt, dev, "dbeta"), 0, 0)
+                           pg, pb, 0, 0)
     _call("dip_group_norm_grad", args, dev)
     return dx, dgamma, dbeta
