@@ -138,6 +138,8 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   switch (act) {
     case DIP_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
     case DIP_ACT_SILU: {
+      // e is 0 or 1 there; a pre beyond float16's range is stored as an infinity
+      if (fabsf(z) > 120.f) return z > 0.f ? 1.f : 0.f;
       const float e = logistic2(silu_arg(z));
       return e * (1.f + z * (1.f - e));
     }

@@ -1,7 +1,8 @@
 """The gradient between dy and the products.  Where it is representable in 16 bits:
 without an activation and with ReLU it is dy or 0, and dropout's factor is the
 products', so nothing but the float32 sums and the result's rounding is left in dx and dw.
-Where an element is dropped: 0, whatever pre holds."""
+Where an element is dropped: 0, whatever pre holds.  Where pre is stored as an
+infinity: the slope's limit."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -63,3 +64,25 @@ def test_what_pre_holds_under_the_mask_does_not_matter(act):
     assert not bool(torch.isfinite(bad).all())
     for got, want in zip(call(bad), call(pre)):
         assert bool(torch.isfinite(want).all()) and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_a_pre_beyond_the_types_range_has_the_slopes_limit(act):
+    """float16 holds a finite -70000 as an infinity; the forward's result there is 0 and
+    so is the gradient.  Far on the other side the slope is 1."""
+    m, n, k = 40, 48, 8
+    x = torch.ones((m, k), dtype=F16)
+    w = torch.full((n, k), -10000.0, dtype=F16)
+    w[::3] = 10000.0
+    g = torch.Generator().manual_seed(1)
+    dy = torch.randn((m, n), generator=g).to(F16)
+    pre = torch.empty((m, n), dtype=F16, device="cuda")
+    y = ops.linear(x.cuda(), w.cuda(), act=act, pre=pre)
+    up = torch.zeros((m, n), dtype=torch.bool)
+    up[:, ::3] = True
+    assert bool((y.cpu()[~up] == 0).all()) and bool(torch.isinf(pre).all())
+    _, dw, db = ops.linear_backward(dy.cuda(), x.cuda(), w.cuda(), act=act, pre=pre, need_dx=False)
+    kept = torch.where(up, dy.double(), 0.0)
+    assert_close(db, kept.sum(0), dot_bound(m, kept.abs().sum(0)), F16, "db")
+    want = kept.T @ x.double()
+    assert_close(dw, want, dot_bound(m, kept.abs().T @ x.double()), F16, "dw")
