@@ -138,10 +138,10 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   switch (act) {
     case DIP_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
     case DIP_ACT_SILU: {
-      // e is 0 or 1 there; a pre beyond float16's range is stored as an infinity
-      if (fabsf(z) > 120.f) return z > 0.f ? 1.f : 0.f;
+      // e is 0 or 1 beyond 120, and z may be infinite: a pre beyond float16's range is
+      // stored so.  NaN comes through e.
       const float e = logistic2(silu_arg(z));
-      return e * (1.f + z * (1.f - e));
+      return e * (1.f + __builtin_amdgcn_fmed3f(z, -120.f, 120.f) * (1.f - e));
     }
     case DIP_ACT_GELU: {
       if (fabsf(z) > 12.f) return z > 0.f ? 1.f : 0.f;   // e is 0 or 1 there, z^2 may overflow
