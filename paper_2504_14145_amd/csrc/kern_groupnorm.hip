@@ -101,7 +101,6 @@ struct Eight {
   __device__ __forceinline__ bool own(int q) const { return q >= skip && q < left; }
 };
 
-// THREADS a row of `per` channels, NV vectors of eight a thread.
 // Up to 512 channels: as many lanes as a row has vectors, to the next power of two.
 template <class T, int LANES>
 __global__ __launch_bounds__(256) void narrow_kernel(dip_group_norm_args a, int64_t rows) {
@@ -136,6 +135,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(dip_group_norm_args a, int6
   store8(static_cast<T *>(a.y) + i * a.y_sb + c, e.left, v);   // the skipped ones: what their own lane writes
 }
 
+// THREADS a row of `per` channels, NV vectors of eight a thread.
 template <class T, int THREADS, int NV>
 __global__ __launch_bounds__(256) void rows_kernel(dip_group_norm_args a, int64_t rows) {
   constexpr int kRows = 256 / THREADS;

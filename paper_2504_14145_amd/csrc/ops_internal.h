@@ -32,11 +32,14 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
                        hipStream_t stream);
 // The same for few rows of an x that is read where it is, as w is: any alignment,
-// no workspace.  Every 16 or 32 rows of w read x again, from the caches, so it
-// pays for up to 16 rows, and up to 32 where w is small: 32 rows, k 4096 x n 3584
-// 13 us against 17 by tiles, 4096 x 14336 37 against 35, 14336 x 4096 49 against
-// 29; 16 rows 9.8, 32 and 33.
-inline bool thin(int64_t m, int64_t n, int64_t k) { return m <= 16 || (m <= 32 && n * k <= (int64_t(1) << 25)); }
+// no workspace.  Every 8 to 32 rows of w read x again, from the caches, so it pays
+// for few rows, and for more where w is small.  bf16, w from memory, this way
+// against tiles, us (k x n): 1 row 4096 x 3584 9.6 / 13.8, 4096 x 14336 26 / 28; 8
+// rows 12.2 / 14.8 and 13696 x 1664 17.5 / 19.3; 16 rows 13.1 / 14.9, 32 / 29 and
+// 14336 x 4096 33.6 / 32.4; 17 rows 2048 x 4096 9.1 / 12.9, 8192 x 4096 24 / 21; 32
+// rows 1000 x 1000 5.8 / 10.3, 2048 x 4096 10.6 / 13.3, 4096 x 3584 17 / 15.4, 8192 x
+// 4096 30 / 21.
+inline bool thin(int64_t m, int64_t n, int64_t k) { return m <= 16 || (m <= 32 && n * k <= (int64_t(1) << 23)); }
 hipError_t launch_thin(int dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w,
                        int64_t ldw, const Epilogue &e, hipStream_t stream);
 // rows x cols from p to out (16-byte aligned, stride ldo a multiple of 8), zeros
