@@ -12,16 +12,17 @@
 //         it reads a second time, out of the caches.
 //  split  a sample's positions are cut into chunks: a pass for the sums of every
 //         channel of a chunk, a small kernel that joins them, a pass that writes.
-// Variances are sums of squares about the mean (rows), or about a value of the
-// channel (block, split), joined through (count, mean, sum of squares about the
-// mean), so that a mean far from zero costs no digits.  Sums are float32, in an
+// Variances are sums of squares about the mean (rows), or about the mean of four
+// rows at a time, joined by (count, mean, sum of squares about the mean) over a
+// thread's rows, the threads and the channels (block, split): neither a mean far
+// from zero nor a row unlike the others costs digits.  Sums are float32, in an
 // order that depends on the shape alone.
-// bf16: rows, 8192 x 4096, 28 us forward (4.8 TB/s), 37 + 5 for the gradient (5.8);
+// bf16: rows, 8192 x 4096, 28 us forward (4.9 TB/s), 37 + 5 for the gradient (5.8);
 // 55,388 x 249 in fp16 with GELU, odd rows, 19 (2.8 TB/s) and 33 (2.5), where one wave
 // a row and 512 at once, element by element at the row's end, took 360 together;
-// split, four samples of 16,384 x 512 with SiLU, 16 + 5 + 24 us forward and 30 + 5
+// split, four samples of 16,384 x 512 with SiLU, 15 + 6 + 25 us forward and 30 + 5
 // + 36 + 4 for the gradient, whose passes over x and dy run at 4.5 and 5.6 TB/s;
-// block, 64 x 320, 7.8 us, three samples of 577 x 120 in fp32 10.7 and 15.2: a chain
+// block, 64 x 320, 7.4 us, three samples of 577 x 120 in fp32 10.5 and 15.5: a chain
 // of latencies (both passes from memory and every channel's sum over 256 rows by a
 // tree took 8.5, 13.3 and 18.4).
 #include <algorithm>

@@ -12,10 +12,11 @@
 // as b a^T: a lane then holds eight consecutive columns of a row of the output,
 // which its epilogue (bias, activation, eight dropout draws of one counter,
 // residual) and its 16-byte stores want.
-// bf16, 8192^3: 1.43 to 1.5 PFLOP/s forward, 1.46 to 1.51 and 1.44 to 1.5 for the
+// bf16, 8192^3: 1.41 to 1.5 PFLOP/s forward, 1.45 to 1.51 and 1.44 to 1.5 for the
 // gradients of x and w, the card's clock falling under the load; 65,536 x 3584 x
-// 2560: 1.32, 1.33, 1.26.  Of a step's 2500 cycles 2048 are products, 280 waits at
-// the two barriers; a tile's start and end take another 20,000.
+// 2560: 1.34, 1.33, 1.26, and 1.16 forward with bias, GELU and the value before it
+// written.  Of a step's 2500 cycles 2048 are products, 280 waits at the two barriers;
+// a tile's start and end take another 20,000.
 #include <algorithm>
 #include <type_traits>
 #include <utility>

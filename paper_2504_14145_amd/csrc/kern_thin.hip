@@ -6,7 +6,7 @@
 // loads are on their way before the first product, at any alignment; what is left
 // of the wave's part is one more batch.  The partial results meet in LDS: one
 // launch, no workspace.
-// bf16, w from memory: one row, 4096 x 3584 8.5 us alone (3.4 TB/s of w) and 9.6 a
+// bf16, w from memory: one row, 4096 x 3584 8.5 to 8.8 us alone (3.4 TB/s of w) and 9.6 a
 // launch among others, 4096 x 14336 26 (4.5); 8 rows, 13696 x 1664 17.5 (28 with 16 rows
 // of w a workgroup, on 104 CUs of 256), 7 rows, 5184 x 256 7.5 (12).
 #include "ops_internal.h"
