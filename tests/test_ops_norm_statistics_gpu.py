@@ -26,11 +26,13 @@ def test_first_rows_unlike_the_others(b, s, c, groups, first, rows, mean):
     """The variance is a sum of squares about means that are right to a float32
     rounding, added up by many threads whose roundings average out: within 16 u
     of rstd at any length.  The mean: 8 u of its size and the spread, one rounding
-    of the result, a few of the sums and their joins."""
+    of the result, a few of the sums and their joins.  The 64-bit form is taken on the
+    CPU: torch's sums over two dimensions of such arrays on the GPU have differed from
+    run to run by percents."""
     x = torch.randn((b, s, c), generator=torch.Generator(device="cuda").manual_seed(s), device="cuda") + mean
     x[:, :rows] = first
     per = c // groups
-    y, got_mean, got_rstd = ops.group_norm(x, groups)
+    x, y, got_mean, got_rstd = (t.cpu() for t in (x, *ops.group_norm(x, groups)))
     for at in range(0, b, 64):
         part = slice(at, min(b, at + 64))
         v = x[part].double().view(-1, s, groups, per)
