@@ -40,7 +40,7 @@ def _time(run, sets, repeats: int) -> float:
     import torch
     run(sets[0])
     run(sets[-1])
-    other = torch.empty(APART, dtype=torch.uint8, device="cuda")
+    other = torch.empty(APART, dtype=torch.uint8, device=sets[0][0].device)
     times = []
     for _ in range(repeats):
         other.zero_()
