@@ -11,6 +11,13 @@
  *   dip_dropout_add  y = residual + D(x), and with no residual its own gradient
  *   dip_group_norm   y = act(gamma (x - mean) rstd + beta), channels last
  *   dip_group_norm_grad
+ *   dip_rms_norm     t = x + residual, y = gamma t rstd, also in 8 bits
+ *   dip_rms_norm_grad
+ *   dip_rotary       queries and keys turned by positions along several axes
+ *   dip_pack8        activations kept in 8 bits (a memory strategy of Sec. 5.3
+ *   dip_unpack8      between keeping and recomputing), restored, and
+ *   dip_linear_kept  written and read by the products and their gradients
+ *   dip_linear_grad_kept
  *
  * D is dropout whose mask is a function of (seed, offset, row, column), never
  * stored: forward, backward and a recomputed forward (Sec. 5.3) draw the same
@@ -195,6 +202,125 @@ typedef struct {
 
 int64_t dip_group_norm_grad_workspace(const dip_group_norm_grad_args *a);
 int dip_group_norm_grad(const dip_group_norm_grad_args *a, void *stream);
+
+/* A matrix in 8 bits.  32 consecutive columns of a row (the last ones: what is
+ * left) share a scale 2^e, the smallest with e >= -126 by which the largest finite
+ * magnitude of them divides to at most 448; its byte is e + 127.  Values are v / 2^e
+ * rounded to nearest even with four significant bits and steps of at least 2^-9
+ * (sign, 4 bits of exponent, 3 of mantissa; OCP FP8 E4M3).  Infinities and NaN are
+ * kept as NaN.  What is read may have any bytes: scales 0 and 255 are 2^-127 and NaN.
+ * Restored values are exact in float32, and in bfloat16 from 2^-126 on; one that
+ * rounded up beyond the largest value of the type it is restored to becomes that
+ * value. */
+typedef struct {
+  void *values;              /* [m][n] bytes, ld; any alignment                 */
+  int64_t ld;
+  void *scales;              /* [m][(n + 31) / 32] bytes, lds                   */
+  int64_t lds;
+} dip_packed8;
+
+/* x[m][n] in 8 bits, and y[m][n] = act(x) of a matrix in 8 bits, x exact and y
+ * rounded to dtype. */
+int dip_pack8(int32_t dtype, int64_t m, int64_t n, const void *x, int64_t ldx, const dip_packed8 *out, void *stream);
+int dip_unpack8(int32_t dtype, int64_t m, int64_t n, const dip_packed8 *x, int32_t act, void *y, int64_t ldy,
+                void *stream);
+
+/* dip_linear with pre kept in 8 bits, from the float32 sums; a->pre is not used. */
+int64_t dip_linear_kept_workspace(const dip_linear_args *a, const dip_packed8 *pre);
+int dip_linear_kept(const dip_linear_args *a, const dip_packed8 *pre, void *stream);
+/* dip_linear_grad from activations kept in 8 bits: x is x_act of the kept matrix,
+ * rounded to the type, and slopes are those at the kept pre.  Either may be null: then
+ * a->x (x_act not used) or a->pre is read. */
+int64_t dip_linear_grad_kept_workspace(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act,
+                                       const dip_packed8 *pre);
+int dip_linear_grad_kept(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act, const dip_packed8 *pre,
+                         void *stream);
+
+/* Root-mean-square norm of m rows of c: t = x + residual rounded to the type (the
+ * stream of residuals; x itself without one), rstd = 1 / sqrt(mean(t^2) + eps),
+ * y = gamma t rstd.  The mean is summed in float32: rows whose sum of squares is
+ * beyond its range have rstd 0.  total (t) may be the residual itself or null; y,
+ * rstd and packed.values too, where they are not wanted.  packed has y in 8 bits, from
+ * the float32 values.  gamma may be null (1). */
+typedef struct {
+  int64_t m, c;
+  int32_t dtype;
+  float eps;                 /* >= 0                                            */
+  const void *x;             /* [m][c], ldx                                     */
+  int64_t ldx;
+  const void *residual;      /* [m][c], ldr, or null                            */
+  int64_t ldr;
+  const void *gamma;         /* [c] of the type, or null                        */
+  void *total;               /* [m][c], ldt                                     */
+  int64_t ldt;
+  void *y;                   /* [m][c], ldy                                     */
+  int64_t ldy;
+  dip_packed8 packed;
+  float *rstd;               /* [m]                                             */
+} dip_rms_norm_args;
+
+int dip_rms_norm(const dip_rms_norm_args *a, void *stream);
+
+/* Its gradients for the gradients dy of y and dtotal of t (null: none): with
+ * xh = t rstd and h = dy gamma, dx = dtotal + rstd (h - xh mean(h xh)), which is the
+ * gradient of x and of the residual, and dgamma = sum over rows of dy xh.  Either may
+ * be null.  dx may be dtotal itself.  dgamma is of the type; with accumulate != 0
+ * float32 and added to. */
+typedef struct {
+  int64_t m, c;
+  int32_t dtype, accumulate;
+  const void *dy;            /* [m][c], ldy                                     */
+  int64_t ldy;
+  const void *total;         /* [m][c], ldt                                     */
+  int64_t ldt;
+  const void *gamma;
+  const float *rstd;
+  const void *dtotal;        /* [m][c], lddt, or null                           */
+  int64_t lddt;
+  void *dx;                  /* [m][c], lddx                                    */
+  int64_t lddx;
+  void *dgamma;              /* [c]                                             */
+  void *workspace;           /* 16-byte aligned, dip_rms_norm_grad_workspace()  */
+  int64_t workspace_bytes;
+} dip_rms_norm_grad_args;
+
+int64_t dip_rms_norm_grad_workspace(const dip_rms_norm_grad_args *a);
+int dip_rms_norm_grad(const dip_rms_norm_grad_args *a, void *stream);
+
+/* types of positions */
+#define DIP_POS_I32 0
+#define DIP_POS_I64 1
+#define DIP_POS_F32 2
+
+/* Rotary positions with several axes: pair j of every head of token i is turned by
+ * the angle pos[i][axis[j]] freq[j] radians (inverse != 0: by its negative, which is
+ * the gradient), (a, b) to (a cos - b sin, a sin + b cos).  Pair j is elements
+ * j and pairs + j of the head, or with interleaved != 0 2 j and 2 j + 1; elements from
+ * 2 pairs on are copied.  Angles are float64 up to their sine and cosine.  A pair whose
+ * axis is not one of the axes stays as it is.  k with its heads goes along where
+ * keys > 0.  Strides in elements, up to 2^46: st between tokens, sh between heads, in
+ * either order; pos st and sa between tokens and axes.  An output may be its input
+ * itself (same pointer and strides). */
+typedef struct {
+  int64_t t;                 /* tokens                                          */
+  int32_t heads, keys;       /* heads of q and of k                             */
+  int32_t dim, pairs, axes;  /* elements a head, up to 2048; 2 pairs <= dim     */
+  int32_t dtype, pos_type, interleaved, inverse;
+  const void *q;             /* [t][heads][dim]                                 */
+  int64_t q_st, q_sh;
+  const void *k;             /* [t][keys][dim]                                  */
+  int64_t k_st, k_sh;
+  const void *pos;           /* [t][axes]                                       */
+  int64_t p_st, p_sa;
+  const double *freq;        /* [pairs]                                         */
+  const int32_t *axis;       /* [pairs]                                         */
+  void *q_out;
+  int64_t qo_st, qo_sh;
+  void *k_out;
+  int64_t ko_st, ko_sh;
+} dip_rotary_args;
+
+int dip_rotary(const dip_rotary_args *a, void *stream);
 
 #ifdef __cplusplus
 }

@@ -12,7 +12,8 @@ SOURCES = [os.path.join(CSRC, f) for f in
             "kern_general.hip", "kern_check.hip", "kern_pool.hip", "kern_sim.hip",
             "kern_greedy.hip", "kern_rollout.hip", "kern_costmodel.hip", "kern_memopt.hip",
             "kern_argmin.hip", "kern_selcheck.hip", "kern_direct.hip",
-            "host_ops.hip", "kern_linear.hip", "kern_thin.hip", "kern_elementwise.hip", "kern_groupnorm.hip")]
+            "host_ops.hip", "kern_linear.hip", "kern_thin.hip", "kern_elementwise.hip", "kern_groupnorm.hip",
+            "kern_pack8.hip", "kern_rmsnorm.hip", "kern_rotary.hip")]
 LIB = os.path.join(HERE, "libdip_sim.so")
 INCLUDE = os.path.join(ROOT, "include")
 

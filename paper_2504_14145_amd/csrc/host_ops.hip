@@ -78,7 +78,23 @@ int check_linear(const dip_linear_args *a) {
   return DIP_OK;
 }
 
-int check_linear_grad(const dip_linear_grad_args *a) {
+// A matrix in 8 bits that a call reads or writes.
+int check_packed(const dip_packed8 &p, int64_t rows, int64_t cols) {
+  OPS_CHECK(check_matrix(p.values, rows, cols, p.ld, 1));
+  return check_matrix(p.scales, rows, (cols + 31) / 32, p.lds, 1);
+}
+
+int check_linear_kept(const dip_linear_args *a, const dip_packed8 *pre) {
+  if (!a || !pre) return DIP_E_INVAL;
+  dip_linear_args b = *a;
+  b.pre = nullptr;
+  OPS_CHECK(check_linear(&b));
+  return check_packed(*pre, a->m, a->n);
+}
+
+// x8 and pre8: what is read in the place of a->x and a->pre, or null
+int check_linear_grad(const dip_linear_grad_args *a, const dip_packed8 *x8 = nullptr, const dip_packed8 *pre8 = nullptr,
+                      int32_t x_act = DIP_ACT_NONE) {
   if (!a || !known_type(a->dtype) || !known_act(a->act)) return DIP_E_INVAL;
   if (a->dtype == DIP_F32) return DIP_E_UNSUPPORTED;
   if (a->grad_dtype != a->dtype && a->grad_dtype != DIP_F32) return DIP_E_INVAL;
@@ -86,15 +102,17 @@ int check_linear_grad(const dip_linear_grad_args *a) {
   OPS_CHECK(check_drop(a->drop, a->m));
   if (a->dx || a->dw || a->db) {
     OPS_CHECK(check_matrix(a->dy, a->m, a->n, a->ldy, 2));
-    if (a->act != DIP_ACT_NONE) OPS_CHECK(check_matrix(a->pre, a->m, a->n, a->ldp, 2));
+    if (a->act != DIP_ACT_NONE)
+      OPS_CHECK(pre8 ? check_packed(*pre8, a->m, a->n) : check_matrix(a->pre, a->m, a->n, a->ldp, 2));
   }
+  if (x8 && !known_act(x_act)) return DIP_E_INVAL;
   const int ge = elem_bytes(a->grad_dtype);
   if (a->dx) {
     OPS_CHECK(check_matrix(a->w, a->n, a->k, a->ldw, 2));
     OPS_CHECK(check_matrix(a->dx, a->m, a->k, a->lddx, 2));
   }
   if (a->dw) {
-    OPS_CHECK(check_matrix(a->x, a->m, a->k, a->ldx, 2));
+    OPS_CHECK(x8 ? check_packed(*x8, a->m, a->k) : check_matrix(a->x, a->m, a->k, a->ldx, 2));
     OPS_CHECK(check_matrix(a->dw, a->n, a->k, a->lddw, ge));
   }
   return check_vector(a->db, ge);
@@ -122,9 +140,9 @@ struct LinearPlan {
   GemmPlan gemm;
   int64_t x_at = -1, w_at = -1, partial_at = 0, total = 0;   // -1: read in place
 };
-LinearPlan plan_linear(const dip_linear_args *a) {
+LinearPlan plan_linear(const dip_linear_args *a, bool kept = false) {
   LinearPlan p;
-  if (a->m == 0 || a->n == 0 || thin(a->m, a->n, a->k)) return p;
+  if (a->m == 0 || a->n == 0 || (!kept && thin(a->m, a->n, a->k))) return p;
   Space s;
   p.gemm = plan_gemm(a->m, a->n, a->k, true);
   if (!direct(a->x, a->ldx, a->k, true)) p.x_at = s.take(a->m * up8(a->k) * 2);
@@ -139,7 +157,7 @@ struct GradPlan {
   int64_t g_at = -1, x_at = -1, w_at = -1, sums_at = -1, partial_at = 0, total = 0;
   int32_t chunks = 0;
 };
-GradPlan plan_grad(const dip_linear_grad_args *a) {
+GradPlan plan_grad(const dip_linear_grad_args *a, bool x8 = false) {
   GradPlan p;
   if (a->m == 0 || a->n == 0) return p;
   Space s;
@@ -159,7 +177,7 @@ GradPlan plan_grad(const dip_linear_grad_args *a) {
     partial = p.dx.bytes;
   }
   if (a->dw && a->k > 0) {
-    if (!direct(a->x, a->ldx, a->k, false)) p.x_at = s.take(a->m * up8(a->k) * 2);
+    if (x8 || !direct(a->x, a->ldx, a->k, false)) p.x_at = s.take(a->m * up8(a->k) * 2);
     p.dw = plan_gemm(a->n, a->k, a->m, false);
     partial = partial > p.dw.bytes ? partial : p.dw.bytes;
   }
@@ -176,6 +194,99 @@ Operand place(const void *p, int64_t rows, int64_t cols, int64_t ld, bool k_rows
 }
 int pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t st) {
   return a.rows || b.rows ? hip_code(launch_pack(dtype, a, b, st)) : int(DIP_OK);
+}
+
+// dip_linear's epilogue, pre aside
+Epilogue epilogue(const dip_linear_args *a) {
+  Epilogue e{};
+  e.bias = a->bias;
+  e.residual = a->residual;
+  e.out = a->y;
+  e.ldr = a->ldr;
+  e.ldo = a->ldy;
+  e.ldp = a->ldp;
+  e.drop = make_drop(a->drop);
+  e.scale = 1.f;
+  e.act = a->act;
+  return e;
+}
+// its operands, where the plan has them
+int operands(const dip_linear_args *a, const LinearPlan &p, hipStream_t st, Operand *x, Operand *w) {
+  char *ws = static_cast<char *>(a->workspace);
+  PackJob px, pw;
+  *x = place(a->x, a->m, a->k, a->ldx, false, ws, p.x_at, &px);
+  *w = place(a->w, a->n, a->k, a->ldw, false, ws, p.w_at, &pw);
+  return pack(a->dtype, px, pw, st);
+}
+float *partial_of(const dip_linear_args *a, const LinearPlan &p) {
+  return reinterpret_cast<float *>(static_cast<char *>(a->workspace) + p.partial_at);
+}
+
+// dip_linear_grad; x8 and pre8, if given, in the place of a->x and a->pre
+int linear_grad(const dip_linear_grad_args *a, const dip_packed8 *x8, int32_t x_act, const dip_packed8 *pre8, void *stream) {
+  OPS_CHECK(check_linear_grad(a, x8, pre8, x_act));
+  const GradPlan p = plan_grad(a, x8 != nullptr);
+  OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
+  const hipStream_t st = hipStream_t(stream);
+  char *ws = static_cast<char *>(a->workspace);
+  const Drop drop = make_drop(a->drop);
+  const void *g = a->dy;
+  int64_t ldg = a->ldy;
+  float *partial = reinterpret_cast<float *>(ws + p.partial_at);
+  if (p.g_at >= 0 || p.sums_at >= 0) {
+    GradIn gi{};
+    gi.m = a->m;
+    gi.n = a->n;
+    gi.dy = a->dy;
+    gi.pre = a->act != DIP_ACT_NONE && !pre8 ? a->pre : nullptr;
+    if (a->act != DIP_ACT_NONE && pre8) gi.kept = make_packed(*pre8);
+    gi.ldy = a->ldy;
+    gi.ldp = a->ldp;
+    gi.drop = drop;
+    gi.act = a->act;
+    if (p.g_at >= 0) {
+      g = gi.out = ws + p.g_at;
+      ldg = gi.ldo = up8(a->n);
+    }
+    gi.row_chunks = p.chunks ? p.chunks : grad_row_chunks(a->m, a->n);
+    gi.partial = a->db ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr;
+    OPS_CHECK(hip_code(launch_grad_in(a->dtype, gi, st)));
+  }
+  if (a->db && a->n > 0 && !(a->m == 0 && a->accumulate))
+    OPS_CHECK(hip_code(launch_sum_rows(SumRows{reinterpret_cast<const float *>(ws + p.sums_at), p.chunks, a->n, a->n,
+                                               a->db, nullptr, a->accumulate},
+                                       a->grad_dtype, st)));
+  PackJob px, pw;
+  Operand x;
+  if (x8) {
+    x = Operand{p.x_at >= 0 ? ws + p.x_at : nullptr, up8(a->k), true};
+    if (p.x_at >= 0)
+      OPS_CHECK(hip_code(launch_unpack8(a->dtype, a->m, a->k, make_packed(*x8), x_act, ws + p.x_at, up8(a->k),
+                                        up8(a->k), st)));
+  } else {
+    x = place(a->x, a->dw ? a->m : 0, a->k, a->ldx, true, ws, p.x_at, &px);
+  }
+  const Operand w = place(a->w, a->dx ? a->n : 0, a->k, a->ldw, true, ws, p.w_at, &pw);
+  OPS_CHECK(pack(a->dtype, px, pw, st));
+  if (a->dx && a->m > 0 && a->k > 0) {
+    Epilogue e{};
+    e.out = a->dx;
+    e.ldo = a->lddx;
+    e.scale = drop.scale;
+    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
+                                   partial, st)));
+  }
+  if (a->dw && a->n > 0 && a->k > 0) {
+    Epilogue e{};
+    e.out = a->dw;
+    e.ldo = a->lddw;
+    e.scale = drop.scale;
+    e.out_f32 = a->grad_dtype == DIP_F32;
+    e.accumulate = a->accumulate != 0;
+    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,
+                                   partial, st)));
+  }
+  return DIP_OK;
 }
 
 int check_norm(int64_t b, int64_t s, int64_t c, int32_t groups, int32_t dtype, int32_t act) {
@@ -227,6 +338,60 @@ int check_group_norm_grad(const dip_group_norm_grad_args *a) {
   return check_vector(a->dbeta, a->accumulate ? 4 : e);
 }
 
+int check_rms_norm(const dip_rms_norm_args *a) {
+  if (!a || !known_type(a->dtype) || !(a->eps >= 0.f)) return DIP_E_INVAL;
+  OPS_CHECK(check_sizes(a->m, a->c, 0));
+  const int e = elem_bytes(a->dtype);
+  OPS_CHECK(check_matrix(a->x, a->m, a->c, a->ldx, e));
+  if (a->residual) OPS_CHECK(check_matrix(a->residual, a->m, a->c, a->ldr, e));
+  if (a->total) OPS_CHECK(check_matrix(a->total, a->m, a->c, a->ldt, e));
+  if (a->y) OPS_CHECK(check_matrix(a->y, a->m, a->c, a->ldy, e));
+  if (a->packed.values || a->packed.scales) OPS_CHECK(check_packed(a->packed, a->m, a->c));
+  OPS_CHECK(check_vector(a->gamma, e));
+  return check_vector(a->rstd, 4);
+}
+
+int check_rms_norm_grad(const dip_rms_norm_grad_args *a) {
+  if (!a || !known_type(a->dtype)) return DIP_E_INVAL;
+  OPS_CHECK(check_sizes(a->m, a->c, 0));
+  const int e = elem_bytes(a->dtype);
+  if (a->dx || a->dgamma) {
+    OPS_CHECK(check_matrix(a->dy, a->m, a->c, a->ldy, e));
+    OPS_CHECK(check_matrix(a->total, a->m, a->c, a->ldt, e));
+    if (a->m > 0 && a->c > 0 && !a->rstd) return DIP_E_INVAL;
+  }
+  if (a->dx) {
+    OPS_CHECK(check_matrix(a->dx, a->m, a->c, a->lddx, e));
+    if (a->dtotal) OPS_CHECK(check_matrix(a->dtotal, a->m, a->c, a->lddt, e));
+  }
+  OPS_CHECK(check_vector(a->rstd, 4));
+  OPS_CHECK(check_vector(a->gamma, e));
+  return check_vector(a->dgamma, a->accumulate ? 4 : e);
+}
+
+// [t][heads][dim] with the given strides, as check_rows
+int check_heads(const void *p, const dip_rotary_args *a, int32_t heads, int64_t st, int64_t sh) {
+  return check_rows(p, a->t, heads, a->dim, st, sh, elem_bytes(a->dtype));
+}
+int check_rotary(const dip_rotary_args *a) {
+  if (!a || !known_type(a->dtype) || a->pos_type < DIP_POS_I32 || a->pos_type > DIP_POS_F32) return DIP_E_INVAL;
+  if (a->t < 0 || a->heads < 0 || a->keys < 0 || a->dim < 0 || a->pairs < 0 || a->axes < 0 || 2 * int64_t(a->pairs) > a->dim)
+    return DIP_E_INVAL;
+  if (a->t >= kMaxRows || a->dim > 2048 || int64_t(a->heads) + a->keys > (int64_t(1) << 20)) return DIP_E_RANGE;
+  OPS_CHECK(check_heads(a->q, a, a->heads, a->q_st, a->q_sh));
+  OPS_CHECK(check_heads(a->q_out, a, a->heads, a->qo_st, a->qo_sh));
+  OPS_CHECK(check_heads(a->k, a, a->keys, a->k_st, a->k_sh));
+  OPS_CHECK(check_heads(a->k_out, a, a->keys, a->ko_st, a->ko_sh));
+  if (a->t == 0 || a->heads + a->keys == 0 || a->pairs == 0) return DIP_OK;
+  if (!a->freq || reinterpret_cast<uintptr_t>(a->freq) % 8 || !a->axis || reinterpret_cast<uintptr_t>(a->axis) % 4)
+    return DIP_E_INVAL;
+  const int pe = a->pos_type == DIP_POS_I64 ? 8 : 4;
+  if (a->axes > 0 && (!a->pos || reinterpret_cast<uintptr_t>(a->pos) % pe)) return DIP_E_INVAL;
+  constexpr int64_t most = int64_t(1) << 46;   // positions may lie anyhow, also one for all tokens
+  const int64_t st = a->p_st < 0 ? -a->p_st : a->p_st, sa = a->p_sa < 0 ? -a->p_sa : a->p_sa;
+  return (a->t > 1 && st > most) || (a->axes > 1 && sa > most) ? DIP_E_RANGE : DIP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -242,26 +407,30 @@ int dip_linear(const dip_linear_args *a, void *stream) {
   OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
   if (a->m == 0 || a->n == 0) return DIP_OK;
   const hipStream_t st = hipStream_t(stream);
-  Epilogue e{};
-  e.bias = a->bias;
-  e.residual = a->residual;
-  e.out = a->y;
+  Epilogue e = epilogue(a);
   e.pre = a->pre;
-  e.ldr = a->ldr;
-  e.ldo = a->ldy;
-  e.ldp = a->ldp;
-  e.drop = make_drop(a->drop);
-  e.scale = 1.f;
-  e.act = a->act;
   if (thin(a->m, a->n, a->k))
     return hip_code(launch_thin(a->dtype, a->m, a->n, a->k, a->x, a->ldx, a->w, a->ldw, e, st));
-  char *ws = static_cast<char *>(a->workspace);
-  PackJob px, pw;
-  const Operand x = place(a->x, a->m, a->k, a->ldx, false, ws, p.x_at, &px);
-  const Operand w = place(a->w, a->n, a->k, a->ldw, false, ws, p.w_at, &pw);
-  OPS_CHECK(pack(a->dtype, px, pw, st));
-  return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm,
-                              reinterpret_cast<float *>(ws + p.partial_at), st));
+  Operand x, w;
+  OPS_CHECK(operands(a, p, st, &x, &w));
+  return hip_code(launch_gemm(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm, partial_of(a, p), st));
+}
+
+int64_t dip_linear_kept_workspace(const dip_linear_args *a, const dip_packed8 *pre) {
+  OPS_CHECK(check_linear_kept(a, pre));
+  return plan_linear(a, true).total;
+}
+
+int dip_linear_kept(const dip_linear_args *a, const dip_packed8 *pre, void *stream) {
+  OPS_CHECK(check_linear_kept(a, pre));
+  const LinearPlan p = plan_linear(a, true);
+  OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
+  if (a->m == 0 || a->n == 0) return DIP_OK;
+  const hipStream_t st = hipStream_t(stream);
+  KeptEpilogue e{epilogue(a), make_packed(*pre)};
+  Operand x, w;
+  OPS_CHECK(operands(a, p, st, &x, &w));
+  return hip_code(launch_gemm_kept(a->dtype, a->m, a->n, a->k, x, w, e, p.gemm, partial_of(a, p), st));
 }
 
 int64_t dip_linear_grad_workspace(const dip_linear_grad_args *a) {
@@ -270,60 +439,59 @@ int64_t dip_linear_grad_workspace(const dip_linear_grad_args *a) {
 }
 
 int dip_linear_grad(const dip_linear_grad_args *a, void *stream) {
-  OPS_CHECK(check_linear_grad(a));
-  const GradPlan p = plan_grad(a);
-  OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, p.total));
-  const hipStream_t st = hipStream_t(stream);
-  char *ws = static_cast<char *>(a->workspace);
-  const Drop drop = make_drop(a->drop);
-  const void *g = a->dy;
-  int64_t ldg = a->ldy;
-  float *partial = reinterpret_cast<float *>(ws + p.partial_at);
-  if (p.g_at >= 0 || p.sums_at >= 0) {
-    GradIn gi{};
-    gi.m = a->m;
-    gi.n = a->n;
-    gi.dy = a->dy;
-    gi.pre = a->act != DIP_ACT_NONE ? a->pre : nullptr;
-    gi.ldy = a->ldy;
-    gi.ldp = a->ldp;
-    gi.drop = drop;
-    gi.act = a->act;
-    if (p.g_at >= 0) {
-      g = gi.out = ws + p.g_at;
-      ldg = gi.ldo = up8(a->n);
-    }
-    gi.row_chunks = p.chunks ? p.chunks : grad_row_chunks(a->m, a->n);
-    gi.partial = a->db ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr;
-    OPS_CHECK(hip_code(launch_grad_in(a->dtype, gi, st)));
-  }
-  if (a->db && a->n > 0 && !(a->m == 0 && a->accumulate))
-    OPS_CHECK(hip_code(launch_sum_rows(SumRows{reinterpret_cast<const float *>(ws + p.sums_at), p.chunks, a->n, a->n,
-                                               a->db, nullptr, a->accumulate},
-                                       a->grad_dtype, st)));
-  PackJob px, pw;
-  const Operand x = place(a->x, a->dw ? a->m : 0, a->k, a->ldx, true, ws, p.x_at, &px);
-  const Operand w = place(a->w, a->dx ? a->n : 0, a->k, a->ldw, true, ws, p.w_at, &pw);
-  OPS_CHECK(pack(a->dtype, px, pw, st));
-  if (a->dx && a->m > 0 && a->k > 0) {
-    Epilogue e{};
-    e.out = a->dx;
-    e.ldo = a->lddx;
-    e.scale = drop.scale;
-    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
-                                   partial, st)));
-  }
-  if (a->dw && a->n > 0 && a->k > 0) {
-    Epilogue e{};
-    e.out = a->dw;
-    e.ldo = a->lddw;
-    e.scale = drop.scale;
-    e.out_f32 = a->grad_dtype == DIP_F32;
-    e.accumulate = a->accumulate != 0;
-    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,
-                                   partial, st)));
-  }
-  return DIP_OK;
+  return linear_grad(a, nullptr, DIP_ACT_NONE, nullptr, stream);
+}
+
+int64_t dip_linear_grad_kept_workspace(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act,
+                                       const dip_packed8 *pre) {
+  OPS_CHECK(check_linear_grad(a, x, pre, x_act));
+  return plan_grad(a, x != nullptr).total;
+}
+
+int dip_linear_grad_kept(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act, const dip_packed8 *pre,
+                         void *stream) {
+  return linear_grad(a, x, x_act, pre, stream);
+}
+
+int dip_pack8(int32_t dtype, int64_t m, int64_t n, const void *x, int64_t ldx, const dip_packed8 *out, void *stream) {
+  if (!out || !known_type(dtype)) return DIP_E_INVAL;
+  OPS_CHECK(check_sizes(m, n, 0));
+  OPS_CHECK(check_matrix(x, m, n, ldx, elem_bytes(dtype)));
+  OPS_CHECK(check_packed(*out, m, n));
+  if (m == 0 || n == 0) return DIP_OK;
+  return hip_code(launch_pack8(dtype, m, n, x, ldx, make_packed(*out), hipStream_t(stream)));
+}
+
+int dip_unpack8(int32_t dtype, int64_t m, int64_t n, const dip_packed8 *x, int32_t act, void *y, int64_t ldy,
+                void *stream) {
+  if (!x || !known_type(dtype) || !known_act(act)) return DIP_E_INVAL;
+  OPS_CHECK(check_sizes(m, n, 0));
+  OPS_CHECK(check_packed(*x, m, n));
+  OPS_CHECK(check_matrix(y, m, n, ldy, elem_bytes(dtype)));
+  if (m == 0 || n == 0) return DIP_OK;
+  return hip_code(launch_unpack8(dtype, m, n, make_packed(*x), act, y, ldy, n, hipStream_t(stream)));
+}
+
+int dip_rms_norm(const dip_rms_norm_args *a, void *stream) {
+  OPS_CHECK(check_rms_norm(a));
+  return hip_code(launch_rms_norm(*a, hipStream_t(stream)));
+}
+
+int64_t dip_rms_norm_grad_workspace(const dip_rms_norm_grad_args *a) {
+  OPS_CHECK(check_rms_norm_grad(a));
+  return rms_norm_grad_workspace(*a);
+}
+
+int dip_rms_norm_grad(const dip_rms_norm_grad_args *a, void *stream) {
+  OPS_CHECK(check_rms_norm_grad(a));
+  OPS_CHECK(check_workspace(a->workspace, a->workspace_bytes, rms_norm_grad_workspace(*a)));
+  return hip_code(launch_rms_norm_grad(*a, hipStream_t(stream)));
+}
+
+int dip_rotary(const dip_rotary_args *a, void *stream) {
+  OPS_CHECK(check_rotary(a));
+  if (a->t == 0 || a->heads + a->keys == 0 || a->dim == 0) return DIP_OK;
+  return hip_code(launch_rotary(*a, hipStream_t(stream)));
 }
 
 int dip_dropout_add(int32_t dtype, int64_t m, int64_t n, const void *x, int64_t ldx,

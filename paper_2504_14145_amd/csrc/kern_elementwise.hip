@@ -10,17 +10,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// n / d for n below 2^31, d at least 1, by one high product.
-struct Divide {
-  uint32_t by, mul, shift;
-  explicit Divide(uint32_t d) : by(d), mul(0), shift(0) {
-    while ((uint64_t(1) << shift) < d) ++shift;
-    // ceil(2^(32 + shift) / d) - 2^32, below 2^32
-    mul = uint32_t(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - d)) / d + 1);
-  }
-  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
-};
-
 // Bound by memory while a counter's 128 bits serve eight elements: its twenty
 // 32 x 32 products take 320 cycles a wave, less than the wave's 24 bytes a lane
 // take to come and go.  Eight columns of a row a thread.  65,536 x 3584 bf16 with a
@@ -76,7 +65,7 @@ hipError_t dropout_add(int64_t m, int64_t n, const void *x, int64_t ldx, const v
 // rows, sixteen rows at a time, and adds its eight row lanes at the end; the
 // chunks' sums are added in their order by sum_rows_kernel.  65,536 x 2560 with
 // GELU 217 us (4.6 TB/s; the slope's arithmetic is the rest).
-template <class T>
+template <class T, bool KEPT>
 __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   __shared__ float s[8][256 + 8];
   const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
@@ -93,7 +82,17 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
       float v[U][8], z[U][8];
 #pragma unroll
       for (int u = 0; u < U; ++u) load8(dy + (row + 8 * u) * g.ldy, left, v[u]);
-      if (g.pre) {
+      if constexpr (KEPT) {
+        u32x2 bits[U];
+        uint32_t scale[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          bits[u] = load8bits(g.kept.q + (row + 8 * u) * g.kept.ld + col, left);
+          scale[u] = g.kept.s[(row + 8 * u) * g.kept.lds + col / 32];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) from8bits(bits[u], scale_of(scale[u]), z[u]);
+      } else if (g.pre) {
 #pragma unroll
         for (int u = 0; u < U; ++u) load8(pre + (row + 8 * u) * g.ldp, left, z[u]);
       }
@@ -196,10 +195,9 @@ int32_t grad_row_chunks(int64_t m, int64_t n) {
 
 hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream) {
   const dim3 grid(uint32_t((g.n + 255) / 256), uint32_t(g.row_chunks));
-  if (dtype == DIP_BF16)
-    grad_in_kernel<__bf16><<<grid, dim3(kThreads), 0, stream>>>(g);
-  else
-    grad_in_kernel<_Float16><<<grid, dim3(kThreads), 0, stream>>>(g);
+  auto go = [&](auto kernel) { kernel<<<grid, dim3(kThreads), 0, stream>>>(g); };
+  if (dtype == DIP_BF16) g.kept.q ? go(grad_in_kernel<__bf16, true>) : go(grad_in_kernel<__bf16, false>);
+  else g.kept.q ? go(grad_in_kernel<_Float16, true>) : go(grad_in_kernel<_Float16, false>);
   return hipGetLastError();
 }
 

@@ -256,13 +256,17 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 }
 
 // what a workgroup does with its tile: the epilogue, a plain output of the
-// operands' type, one of either type or added to, a part of a split
-constexpr int kForward = 0, kGradient = 1, kGradientAny = 2, kPartial = 3;
+// operands' type, one of either type or added to, a part of a split, the epilogue
+// whose pre is kept in 8 bits
+constexpr int kForward = 0, kGradient = 1, kGradientAny = 2, kPartial = 3, kForwardKept = 4;
+template <int KIND>
+using EpilogueOf = std::conditional_t<KIND == kForwardKept, KeptEpilogue, Epilogue>;
 
 // out tile BM x BN by WM x WN waves.
 template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R, int KIND>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
-                                                            Operand b, Epilogue e, Split split) {
+                                                            Operand b, EpilogueOf<KIND> e, Split split) {
+  constexpr bool kIsForward = KIND == kForward || KIND == kForwardKept;
   typedef typename Vec8<T>::type V;
   constexpr int kThreads = 64 * WM * WN;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
   for (int p = 0; p < P; ++p) cols[p] = int(max(int64_t(0), min(int64_t(8), n - col0 - 32 * p)));
   V bias[P];
-  if (KIND == kForward && e.bias) {
+  if (kIsForward && e.bias) {
 #pragma unroll
     for (int p = 0; p < P; ++p) bias[p] = take8(static_cast<const T *>(e.bias) + col0 + 32 * p, cols[p]);
   }
@@ -412,7 +416,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
     for (int p = 0; p < P; ++p) r[at][p] = take8(q + 32 * p, row < m ? cols[p] : 0);
   };
-  if (KIND == kForward && e.residual) {
+  if (kIsForward && e.residual) {
 #pragma unroll
     for (int i = 0; i < kRows; ++i) residual(i, i);
   }
@@ -431,9 +435,25 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
         if (row < m && cols[p] > 0) store8(q + 32 * p, 8, v[p]);
       return;
     }
-    if constexpr (KIND == kForward) {
+    if constexpr (kIsForward) {
       if (e.bias) each<P>([&](int p, int q) { v[p][q] += float(bias[p][q]); });
-      if (e.pre) store(static_cast<T *>(e.pre), e.ldp);
+      if constexpr (KIND == kForwardKept) {
+        // the four lanes that hold a row's 32 columns are sixteen apart
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          float most = finite_most(v[p]);   // columns beyond the matrix are zeros
+          most = fmaxf(most, __shfl_xor(most, 16));
+          most = fmaxf(most, __shfl_xor(most, 32));
+          const uint32_t byte = scale_byte(most);
+          const int left = row < m ? cols[p] : 0;
+          if (left > 0) {
+            store8bits(e.kept.q + row * e.kept.ld + col0 + 32 * p, left, round8bits(byte, v[p]));
+            if (lane < 16) e.kept.s[row * e.kept.lds + (col0 >> 5) + p] = uint8_t(byte);
+          }
+        }
+      } else {
+        if (e.pre) store(static_cast<T *>(e.pre), e.ldp);
+      }
       if (e.act == DIP_ACT_SILU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_SILU); });
       else if (e.act == DIP_ACT_GELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_GELU); });
       else if (e.act == DIP_ACT_RELU) each<P>([&](int p, int q) { v[p][q] = act_of(v[p][q], DIP_ACT_RELU); });
@@ -461,7 +481,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[p][q] = acc[decltype(i_)::value][2 * p + q / 4][q % 4];
   };
-  if constexpr ((KIND == kForward && kRows < FM) || KIND == kGradientAny) {
+  if constexpr ((kIsForward && kRows < FM) || KIND == kGradientAny) {
 #pragma unroll 1
     for (int i = 0; i < FM; ++i) {
       // read by instructions written out: the compiler would make one array
@@ -498,6 +518,70 @@ __global__ __launch_bounds__(256) void join_kernel(int64_t m, int64_t n, Epilogu
     for (int j = 0; j < 8; ++j) v[j] += q[j];
   }
   finish8<T>(e, row, col, int(min(int64_t(8), n - col)), v);
+}
+
+// The same with pre kept in 8 bits: four threads in a row share a scale.
+template <class T>
+__global__ __launch_bounds__(256) void join_kept_kernel(int64_t m, int64_t n, KeptEpilogue e, Split split, int splits) {
+  const int64_t per = (n + 31) / 32 * 4, all = m * per;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= all) return;
+  const int64_t row = i / per, col = i % per * 8;
+  const int left = int(min(int64_t(8), n - col));
+  float v[8] = {};
+  if (left > 0) {
+    load8(split.partial + row * split.n8 + col, 8, v);
+    for (int s = 1; s < splits; ++s) {
+      float q[8];
+      load8(split.partial + (int64_t(s) * m + row) * split.n8 + col, 8, q);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += q[j];
+    }
+    if (e.bias) {
+      float b[8];
+      load8(static_cast<const T *>(e.bias) + col, left, b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] : 0.f;
+  }
+  pack8_quad(e.kept, row, col, left, v);
+  if (left <= 0) return;
+  Epilogue rest = e;
+  rest.bias = nullptr;
+  finish8<T>(rest, row, col, left, v);
+}
+
+template <class T, int BM, int BN, int WM, int WN, int R>
+hipError_t run_kept(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const KeptEpilogue &e,
+                    const GemmPlan &plan, float *partial, hipStream_t stream) {
+  const int64_t tiles = ((m + BM - 1) / BM) * ((n + BN - 1) / BN);
+  const dim3 block(64 * WM * WN);
+  Split s{partial, plan.steps, (n + 7) / 8 * 8};
+  if (plan.splits <= 1) {
+    gemm_kernel<T, false, false, BM, BN, WM, WN, R, kForwardKept>
+        <<<dim3(uint32_t(tiles)), block, 0, stream>>>(m, n, k, a, b, e, s);
+    return hipGetLastError();
+  }
+  gemm_kernel<T, false, false, BM, BN, WM, WN, R, kPartial>
+      <<<dim3(uint32_t(tiles), uint32_t(plan.splits)), block, 0, stream>>>(m, n, k, a, b, e, s);
+  const hipError_t rc = hipGetLastError();
+  if (rc != hipSuccess) return rc;
+  join_kept_kernel<T><<<dim3(uint32_t((m * ((n + 31) / 32 * 4) + 255) / 256)), dim3(256), 0, stream>>>(m, n, e, s,
+                                                                                                      plan.splits);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t pick_kept(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b, const KeptEpilogue &e,
+                     const GemmPlan &plan, float *partial, hipStream_t stream) {
+  switch (plan.tile) {
+    case 0: return run_kept<T, 256, 256, 2, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
+    case 1: return run_kept<T, 128, 128, 2, 2, 2>(m, n, k, a, b, e, plan, partial, stream);
+    case 3: return run_kept<T, 192, 128, 2, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
+    default: return run_kept<T, 128, 128, 2, 2, 4>(m, n, k, a, b, e, plan, partial, stream);
+  }
 }
 
 template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R>
@@ -603,6 +687,12 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
   if (!a.k_rows && !b.k_rows) return pick<_Float16, false, false>(m, n, k, a, b, e, plan, partial, stream);
   if (!a.k_rows) return pick<_Float16, false, true>(m, n, k, a, b, e, plan, partial, stream);
   return pick<_Float16, true, true>(m, n, k, a, b, e, plan, partial, stream);
+}
+
+hipError_t launch_gemm_kept(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
+                            const KeptEpilogue &e, const GemmPlan &plan, float *partial, hipStream_t stream) {
+  return dtype == DIP_BF16 ? pick_kept<__bf16>(m, n, k, a, b, e, plan, partial, stream)
+                           : pick_kept<_Float16>(m, n, k, a, b, e, plan, partial, stream);
 }
 
 hipError_t launch_pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t stream) {

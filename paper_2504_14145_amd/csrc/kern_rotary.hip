@@ -1,0 +1,198 @@
+// kern_rotary.hip -- rotary positions with several axes: the pairs of every head of a
+// token turned by the angles of its positions.
+//
+// Bound by memory, every head read and written once; a token's sines and cosines are
+// as many as one head has pairs and serve all heads.  A workgroup takes a few tokens
+// and a share of their heads, puts the tokens' sines and cosines into LDS (the angle
+// in turns in float64, less its whole turns: far positions lose nothing) and goes over
+// the heads, a vector of pairs a thread.
+#include <algorithm>
+#include <type_traits>
+
+#include "ops_internal.h"
+
+namespace dipops {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ double position(const dip_rotary_args &a, int64_t at) {
+  switch (a.pos_type) {
+    case DIP_POS_I32: return double(static_cast<const int32_t *>(a.pos)[at]);
+    case DIP_POS_I64: return double(static_cast<const int64_t *>(a.pos)[at]);
+    default: return double(static_cast<const float *>(a.pos)[at]);
+  }
+}
+
+template <class T, int V>
+struct Vector {
+  typedef T type __attribute__((ext_vector_type(V)));
+  typedef type any __attribute__((aligned(sizeof(T))));
+};
+template <class T>
+struct Vector<T, 1> {
+  typedef T type, any;
+};
+template <class T, int V>
+__device__ __forceinline__ void load(const T *p, float (&v)[V]) {
+  const typename Vector<T, V>::type t = *reinterpret_cast<const typename Vector<T, V>::any *>(p);
+  if constexpr (V == 1) v[0] = float(t);
+  else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = float(t[i]);
+  }
+}
+template <class T, int V>
+__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
+  typename Vector<T, V>::type t;
+  if constexpr (V == 1) t = T(v[0]);
+  else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = T(v[i]);
+  }
+  *reinterpret_cast<typename Vector<T, V>::any *>(p) = t;
+}
+
+// Tokens and heads a workgroup takes; dividers of an item's index.
+struct Shares {
+  int32_t tokens, heads;
+  Divide vectors, in_head;   // vectors a head; heads a token
+};
+
+// V pairs a thread.
+template <class T, int V, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int64_t token0, Shares sh) {
+  extern __shared__ float2 table[];   // [tokens][pairs]: cosine, sine
+  const int64_t i0 = token0 + int64_t(blockIdx.x) * sh.tokens;
+  const int tokens = int(min(int64_t(sh.tokens), a.t - i0)), all = a.heads + a.keys;
+  const int h0 = int(blockIdx.y) * sh.heads, heads = min(sh.heads, all - h0);
+  for (int i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
+    const int n = i / a.pairs, j = i - n * a.pairs, axis = a.axis[j];
+    float2 cs = {1.f, 0.f};
+    if (axis >= 0 && axis < a.axes) {
+      double turns = position(a, (i0 + n) * a.p_st + axis * a.p_sa) * a.freq[j] * 0.15915494309189533577;
+      turns -= rint(turns);
+      sincospif(2.f * float(turns), &cs.y, &cs.x);
+      if (a.inverse) cs.y = -cs.y;
+    }
+    table[i] = cs;
+  }
+  __syncthreads();
+  const uint32_t items = uint32_t(tokens) * uint32_t(heads) * sh.vectors.by;
+  for (uint32_t i = threadIdx.x; i < items; i += kThreads) {
+    const uint32_t x = sh.vectors(i), v = i - x * sh.vectors.by;
+    uint32_t n, h;
+    if (heads == sh.heads) {
+      n = sh.in_head(x);
+      h = x - n * sh.in_head.by;
+    } else {
+      n = x / uint32_t(heads);
+      h = x - n * uint32_t(heads);
+    }
+    h += h0;
+    const int64_t token = i0 + n;
+    const bool of_q = int(h) < a.heads;
+    const int64_t hk = of_q ? h : int64_t(h) - a.heads;
+    const T *p = of_q ? static_cast<const T *>(a.q) + token * a.q_st + hk * a.q_sh
+                      : static_cast<const T *>(a.k) + token * a.k_st + hk * a.k_sh;
+    T *o = of_q ? static_cast<T *>(a.q_out) + token * a.qo_st + hk * a.qo_sh
+                : static_cast<T *>(a.k_out) + token * a.ko_st + hk * a.ko_sh;
+    const int first = int(v) * V * (INTERLEAVED ? 2 : 1), second = INTERLEAVED ? first + V : first + a.pairs;
+    float u[V], w[V];
+    load<T, V>(p + first, u);
+    load<T, V>(p + second, w);
+    const float2 *cs = table + n * a.pairs + v * V;
+    float ou[V], ow[V];
+    if constexpr (INTERLEAVED && V > 1) {
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        const float2 c = cs[j], d = cs[V / 2 + j];
+        ou[2 * j] = u[2 * j] * c.x - u[2 * j + 1] * c.y;
+        ou[2 * j + 1] = u[2 * j] * c.y + u[2 * j + 1] * c.x;
+        ow[2 * j] = w[2 * j] * d.x - w[2 * j + 1] * d.y;
+        ow[2 * j + 1] = w[2 * j] * d.y + w[2 * j + 1] * d.x;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float2 c = cs[j];
+        ou[j] = u[j] * c.x - w[j] * c.y;
+        ow[j] = u[j] * c.y + w[j] * c.x;
+      }
+    }
+    store<T, V>(o + first, ou);
+    store<T, V>(o + second, ow);
+  }
+}
+
+// Elements 2 pairs .. dim - 1 of every head, where the output is not the input.
+template <class T>
+__global__ __launch_bounds__(kThreads) void rotary_rest_kernel(dip_rotary_args a, int64_t items) {
+  const int rest = a.dim - 2 * a.pairs, all = a.heads + a.keys;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < items; i += int64_t(gridDim.x) * kThreads) {
+    const int64_t x = i / rest, token = x / all;
+    const int e = 2 * a.pairs + int(i - x * rest), h = int(x - token * all);
+    if (h < a.heads)
+      static_cast<T *>(a.q_out)[token * a.qo_st + h * a.qo_sh + e] = static_cast<const T *>(a.q)[token * a.q_st + h * a.q_sh + e];
+    else
+      static_cast<T *>(a.k_out)[token * a.ko_st + (h - a.heads) * a.ko_sh + e] =
+          static_cast<const T *>(a.k)[token * a.k_st + (h - a.heads) * a.k_sh + e];
+  }
+}
+
+template <class T>
+hipError_t rotary(const dip_rotary_args &a, hipStream_t st) {
+  const int all = a.heads + a.keys;
+  if (a.pairs > 0) {
+    const int V = a.pairs % 8 == 0 ? 8 : a.pairs % 4 == 0 ? 4 : a.pairs % 2 == 0 ? 2 : 1;
+    const int vectors = a.pairs / V;
+    // tokens for about eight items a thread, of up to 2048 pairs; where the tokens are
+    // few the heads are shared out too
+    Shares sh{1, all, Divide(uint32_t(vectors)), Divide(1)};
+    const int64_t an = int64_t(all) * vectors;
+    sh.tokens = int32_t(std::max<int64_t>(1, std::min<int64_t>({8 * kThreads / an, 2048 / a.pairs, (a.t + 1023) / 1024})));
+    if (a.t * an < int64_t(1024) * 8 * kThreads && an > kThreads)
+      sh.heads = std::max<int32_t>(1, kThreads / vectors);
+    while ((all + sh.heads - 1) / sh.heads > 65535) sh.heads *= 2;
+    sh.in_head = Divide(uint32_t(sh.heads));
+    const uint32_t parts = uint32_t((all + sh.heads - 1) / sh.heads);
+    // a launch has fewer than 2^32 threads
+    const int64_t blocks = std::max<int64_t>(1, ((int64_t(1) << 31) / kThreads) / parts), most = blocks * sh.tokens;
+    for (int64_t token0 = 0; token0 < a.t; token0 += most) {
+      dip_rotary_args b = a;
+      b.t = std::min(a.t, token0 + most);
+      const dim3 grid(uint32_t((b.t - token0 + sh.tokens - 1) / sh.tokens), parts);
+      const size_t lds = size_t(sh.tokens) * a.pairs * sizeof(float2);
+      auto go = [&](auto v) {
+        constexpr int kV = decltype(v)::value;
+        if (a.interleaved) rotary_kernel<T, kV, true><<<grid, dim3(kThreads), lds, st>>>(b, token0, sh);
+        else rotary_kernel<T, kV, false><<<grid, dim3(kThreads), lds, st>>>(b, token0, sh);
+      };
+      if (V == 8) go(std::integral_constant<int, 8>{});
+      else if (V == 4) go(std::integral_constant<int, 4>{});
+      else if (V == 2) go(std::integral_constant<int, 2>{});
+      else go(std::integral_constant<int, 1>{});
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  const bool moved = (a.heads > 0 && a.q != a.q_out) || (a.keys > 0 && a.k != a.k_out);
+  if (a.dim > 2 * a.pairs && moved) {
+    const int64_t items = a.t * all * (a.dim - 2 * a.pairs);
+    rotary_rest_kernel<T><<<dim3(uint32_t(std::min<int64_t>((items + kThreads - 1) / kThreads, 1 << 16))), dim3(kThreads), 0, st>>>(a, items);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const dip_rotary_args &a, hipStream_t stream) {
+  switch (a.dtype) {
+    case DIP_F32: return rotary<float>(a, stream);
+    case DIP_F16: return rotary<_Float16>(a, stream);
+    default: return rotary<__bf16>(a, stream);
+  }
+}
+
+}  // namespace dipops

@@ -152,6 +152,106 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   }
 }
 
+// ------------------------------------------------------------ values in 8 bits
+
+struct Packed {
+  uint8_t *q;
+  int64_t ld;
+  uint8_t *s;
+  int64_t lds;
+};
+inline Packed make_packed(const dip_packed8 &p) {
+  return Packed{static_cast<uint8_t *>(p.values), p.ld, static_cast<uint8_t *>(p.scales), p.lds};
+}
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+
+// The largest finite magnitude of eight values.
+__device__ __forceinline__ float finite_most(const float (&v)[8]) {
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = fabsf(v[i]);
+    most = a < INFINITY && a > most ? a : most;
+  }
+  return most;
+}
+// The largest over the four lanes 4 j .. 4 j + 3, which are all on.
+__device__ __forceinline__ float quad_most(float a) {
+  const int x = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0xb1, 0xf, 0xf, true);   // lane ^ 1
+  a = fmaxf(a, __builtin_bit_cast(float, x));
+  const int y = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0x4e, 0xf, 0xf, true);   // lane ^ 2
+  return fmaxf(a, __builtin_bit_cast(float, y));
+}
+// The byte e + 127 of the smallest 2^e, e >= -126, with most / 2^e <= 448 = 1.75 2^8.
+__device__ __forceinline__ uint32_t scale_byte(float most) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, most);
+  return uint32_t(max(int(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), 1));
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  const uint32_t b = byte ? byte << 23 : 0x400000u;
+  return __builtin_bit_cast(float, byte == 255 ? 0x7fc00000u : b);
+}
+// Eight values over 2^e in 8 bits.  The conversion rounds to nearest even; its inputs
+// are at most 448, or NaN for what is not finite.
+__device__ __forceinline__ u32x2 round8bits(uint32_t byte, const float (&v)[8]) {
+  const float inv = __builtin_bit_cast(float, (254u - byte) << 23);   // 2^-e, byte 1 .. 247
+  float q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = fabsf(v[i]) < INFINITY ? v[i] * inv : NAN;
+  u32x2 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], w, true);
+    r[i] = uint32_t(w);
+  }
+  return r;
+}
+__device__ __forceinline__ void store8bits(uint8_t *p, int left, u32x2 r) {
+  if (left >= 8) {
+    *reinterpret_cast<u32x2_any *>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = uint8_t(r[i / 4] >> (8 * (i % 4)));
+  }
+}
+__device__ __forceinline__ u32x2 load8bits(const uint8_t *p, int left) {
+  if (left >= 8) return *reinterpret_cast<const u32x2_any *>(p);
+  u32x2 r = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < left) r[i / 4] |= uint32_t(p[i]) << (8 * (i % 4));
+  return r;
+}
+__device__ __forceinline__ void from8bits(u32x2 r, float scale, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(r[i]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(r[i]), true);
+    v[4 * i] = lo[0] * scale;
+    v[4 * i + 1] = lo[1] * scale;
+    v[4 * i + 2] = hi[0] * scale;
+    v[4 * i + 3] = hi[1] * scale;
+  }
+}
+// What rounded up beyond the largest value of T in 8 bits is that value; NaN stays.
+template <class T>
+__device__ __forceinline__ float within(float v) {
+  constexpr float kMost = sizeof(T) == 4 ? 3.402823466e38f
+                          : __is_same(T, _Float16) ? 65504.f : 3.389531389e38f;   // (2 - 2^-7) 2^127
+  return v > kMost ? kMost : v < -kMost ? -kMost : v;
+}
+// Packs a quad's 32 columns from `col` % 32 == 8 (lane % 4) on, of which the lane has
+// `left`; all four lanes are on, one without columns writes nothing.
+__device__ __forceinline__ void pack8_quad(const Packed &p, int64_t row, int64_t col, int left, const float (&v)[8]) {
+  const uint32_t byte = scale_byte(quad_most(finite_most(v)));
+  if (left <= 0) return;
+  store8bits(p.q + row * p.ld + col, left, round8bits(byte, v));
+  if (col % 32 == 0) p.s[row * p.lds + col / 32] = uint8_t(byte);
+}
+
 // ------------------------------------------------------------ dropout
 
 struct Drop {

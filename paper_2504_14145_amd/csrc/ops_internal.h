@@ -10,12 +10,28 @@
 
 namespace dipops {
 
+// n / d for n below 2^31, d at least 1, by one high product.
+struct Divide {
+  uint32_t by, mul, shift;
+  explicit Divide(uint32_t d) : by(d), mul(0), shift(0) {
+    while ((uint64_t(1) << shift) < d) ++shift;
+    // ceil(2^(32 + shift) / d) - 2^32, below 2^32
+    mul = uint32_t(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - d)) / d + 1);
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
+
 // One operand of a matrix product: element (i, k), i the output's row or
 // column, k the contraction, at p[i * ld + k], or with k_rows at p[k * ld + i].
 struct Operand {
   const void *p;
   int64_t ld;
   bool k_rows;
+};
+
+// The epilogue whose pre goes out in 8 bits (e.pre is null).
+struct KeptEpilogue : Epilogue {
+  Packed kept;
 };
 
 // out[m][n] = epilogue(sum_k a(m, k) b(n, k)).  Operands are 16-byte aligned with
@@ -31,6 +47,9 @@ GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows);   // by sizes 
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
                        hipStream_t stream);
+// a and b along the contraction, pre kept in 8 bits
+hipError_t launch_gemm_kept(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
+                            const KeptEpilogue &e, const GemmPlan &plan, float *partial, hipStream_t stream);
 // The same for few rows of an x that is read where it is, as w is: any alignment,
 // no workspace.  Every 8 to 32 rows of w read x again, from the caches, so it pays
 // for few rows, and for more where w is small.  bf16, w from memory, this way
@@ -65,6 +84,7 @@ struct GradIn {
   int64_t ldo;
   float *partial;
   int32_t row_chunks;
+  Packed kept;               // pre in 8 bits, in the place of pre; q null: none
 };
 int32_t grad_row_chunks(int64_t m, int64_t n);
 hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream);
@@ -82,6 +102,16 @@ hipError_t launch_sum_rows(const SumRows &s, int out_dtype, hipStream_t stream);
 hipError_t launch_dropout_add(int dtype, int64_t m, int64_t n, const void *x, int64_t ldx,
                               const void *residual, int64_t ldr, const Drop &drop, void *y,
                               int64_t ldy, hipStream_t stream);
+
+hipError_t launch_pack8(int dtype, int64_t m, int64_t n, const void *x, int64_t ldx, const Packed &out,
+                        hipStream_t stream);
+// y = act(x), zeros in columns n .. fill - 1
+hipError_t launch_unpack8(int dtype, int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill,
+                          hipStream_t stream);
+hipError_t launch_rms_norm(const dip_rms_norm_args &a, hipStream_t stream);
+hipError_t launch_rms_norm_grad(const dip_rms_norm_grad_args &a, hipStream_t stream);
+int64_t rms_norm_grad_workspace(const dip_rms_norm_grad_args &a);
+hipError_t launch_rotary(const dip_rotary_args &a, hipStream_t stream);
 
 hipError_t launch_group_norm(const dip_group_norm_args &a, hipStream_t stream);
 hipError_t launch_group_norm_grad(const dip_group_norm_grad_args &a, hipStream_t stream);
