@@ -441,13 +441,19 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
         // the four lanes that hold a row's 32 columns are sixteen apart
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-          float most = finite_most(v[p]);   // columns beyond the matrix are zeros
-          most = fmaxf(most, __shfl_xor(most, 16));
-          most = fmaxf(most, __shfl_xor(most, 32));
+          auto over = [](uint32_t a) {
+            a = max(a, uint32_t(__shfl_xor(int(a), 16)));
+            return max(a, uint32_t(__shfl_xor(int(a), 32)));
+          };
+          float k[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) k[q] = v[p][q];   // columns beyond the matrix: 0, or NaN
+          uint32_t most = over(most_of(k));
+          if (most >= kInfinity) most = over(finite_most(k));
           const uint32_t byte = scale_byte(most);
           const int left = row < m ? cols[p] : 0;
           if (left > 0) {
-            store8bits(e.kept.q + row * e.kept.ld + col0 + 32 * p, left, round8bits(byte, v[p]));
+            store8bits(e.kept.q + row * e.kept.ld + col0 + 32 * p, left, round8bits(byte, k));
             if (lane < 16) e.kept.s[row * e.kept.lds + (col0 >> 5) + p] = uint8_t(byte);
           }
         }
@@ -546,7 +552,10 @@ __global__ __launch_bounds__(256) void join_kept_kernel(int64_t m, int64_t n, Ke
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] : 0.f;
   }
-  pack8_quad(e.kept, row, col, left, v);
+  float kept[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) kept[j] = v[j];
+  pack8_quad(e.kept, row, col, left, kept);
   if (left <= 0) return;
   Epilogue rest = e;
   rest.bias = nullptr;

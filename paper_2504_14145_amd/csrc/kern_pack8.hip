@@ -18,12 +18,46 @@ __global__ __launch_bounds__(kThreads) void pack8_kernel(uint32_t items, uint32_
   const uint32_t in = per(i);
   const int64_t row = int64_t(row0) + in, col = int64_t(i - in * per.by) * 8;
   const int left = int(min(int64_t(8), n - col));
+  if constexpr (sizeof(T) == 2) {
+    // magnitudes compared and rounded two at a time, as they lie in memory
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    const auto t = take8(x + row * ldx + col, left);
+    const u32x4 w = __builtin_bit_cast(u32x4, t) & 0x7fff7fffu;
+    auto two = [&](int j) { return __builtin_bit_cast(u16x2, uint32_t(w[j])); };
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(0), two(1)),
+                                              __builtin_elementwise_max(two(2), two(3)));
+    const uint32_t most = quad_most(max(uint32_t(m[0]), uint32_t(m[1])));
+    if (most < (__is_same(T, _Float16) ? 0x7c00u : 0x7f80u)) {   // the four lanes agree
+      if (left <= 0) return;
+      const uint32_t byte = scale_byte(magnitude(float(__builtin_bit_cast(T, uint16_t(most)))));
+      const float scale = scale_of(byte);
+      u32x2 r;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const T2 a = {t[4 * j], t[4 * j + 1]}, b = {t[4 * j + 2], t[4 * j + 3]};
+        s16x2 q = {0, 0};
+        if constexpr (__is_same(T, _Float16)) {
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(q, a, scale, false);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(q, b, scale, true);
+        } else {
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, a, scale, false);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, b, scale, true);
+        }
+        r[j] = __builtin_bit_cast(uint32_t, q);
+      }
+      store8bits(out.q + row * out.ld + col, left, r);
+      if (col % 32 == 0) out.s[row * out.lds + col / 32] = uint8_t(byte);
+      return;
+    }
+  }
   float v[8];
   load8(x + row * ldx + col, left, v);
   pack8_quad(out, row, col, left, v);
 }
 
-template <class T>
+template <class T, bool ACT>
 __global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint32_t row0, Divide per, int64_t n,
                                                            Packed x, int act, T *y, int64_t ldy, int64_t fill) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
@@ -31,23 +65,36 @@ __global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint3
   const uint32_t in = per(i);
   const int64_t row = int64_t(row0) + in, col = int64_t(i - in * per.by) * 8;
   const int left = int(min(int64_t(8), n - col));
-  float v[8] = {};
+  u32x2 bits = {0, 0};
+  uint32_t byte = 127;
   if (left > 0) {
-    from8bits(load8bits(x.q + row * x.ld + col, left), scale_of(x.s[row * x.lds + col / 32]), v);
+    bits = load8bits(x.q + row * x.ld + col, left);
+    byte = x.s[row * x.lds + col / 32];
+  }
+  T *out = y + row * ldy + col;
+  if constexpr (!ACT && sizeof(T) == 2) {
+    if (held_by(T(), byte) && fill - col >= 8) {
+      *reinterpret_cast<typename Any8<T>::type *>(out) = from8bits_to<T>(bits, scale_of(byte));
+      return;
+    }
+  }
+  float v[8];
+  from8bits(bits, scale_of(byte), v);
+  if constexpr (ACT) {
     if (act == DIP_ACT_SILU) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_SILU);
     } else if (act == DIP_ACT_GELU) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_GELU);
-    } else if (act == DIP_ACT_RELU) {
+    } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_RELU);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < left ? within<T>(v[j]) : 0.f;
   }
-  store8(y + row * ldy + col, int(min(int64_t(8), fill - col)), v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
+  store8(out, int(min(int64_t(8), fill - col)), v);   // beyond n act(0) = 0
 }
 
 // f(items, row0, Divide(per)) over launches of fewer than 2^31 items.
@@ -72,7 +119,10 @@ hipError_t pack(int64_t m, int64_t n, const void *x, int64_t ldx, const Packed &
 template <class T>
 hipError_t unpack(int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill, hipStream_t st) {
   return pieces(m, (fill + 7) / 8, [&](dim3 grid, uint32_t items, uint32_t row0, const Divide &per) {
-    unpack8_kernel<T><<<grid, dim3(kThreads), 0, st>>>(items, row0, per, n, x, act, static_cast<T *>(y), ldy, fill);
+    auto go = [&](auto kernel) {
+      kernel<<<grid, dim3(kThreads), 0, st>>>(items, row0, per, n, x, act, static_cast<T *>(y), ldy, fill);
+    };
+    act != DIP_ACT_NONE ? go(unpack8_kernel<T, true>) : go(unpack8_kernel<T, false>);
   });
 }
 

@@ -113,23 +113,34 @@ __device__ __forceinline__ void total8(const Held<T> &x, const Held<T> &r, bool 
   }
 }
 
-__device__ __forceinline__ float rstd_of(float sum, float inv, float eps) { return 1.f / sqrtf(sum * inv + eps); }
+// 1 / sqrt(sum / n + eps) and what its rounding left off, by one step of Newton's
+// iteration on the residual: the norm and its 8 bits are then as good as a product of
+// exact factors (the root's rounding would put a whole row off by it).
+struct Rstd {
+  float v, rest;
+  __device__ __forceinline__ Rstd(float sum, int n, float eps) {
+    const float m = sum / float(n) + eps;
+    v = 1.f / sqrtf(m);
+    const float t = m * v, below = fmaf(m, v, -t);
+    const float off = fmaf(-below, v, fmaf(-t, v, 1.f));   // 1 - m v^2
+    rest = fabsf(off) < 1e-3f ? 0.5f * v * off : 0.f;      // not of an infinity or zero
+  }
+};
 
 // y and its 8 bits from t; of the four lanes that share a scale all are here.
 template <class T, bool PACK>
-__device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed &p, int64_t row, int c, float rstd,
+__device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed &p, int64_t row, int c, const Rstd &rstd,
                                        const float (&v)[8]) {
   const int n = int(a.c), left = n - c;
   float g[8], y[8];
   gamma8<T>(a.gamma, c, n, g);
 #pragma unroll
-  for (int q = 0; q < 8; ++q) y[q] = v[q] * rstd * g[q];
-  if (a.y && left > 0) store8(static_cast<T *>(a.y) + row * a.ldy + c, left, y);
-  if constexpr (PACK) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) y[q] = q < left ? y[q] : 0.f;
-    pack8_quad(p, row, c, left, y);
+  for (int q = 0; q < 8; ++q) {
+    const float t = v[q] * g[q];   // exact of 2-byte types
+    y[q] = fmaf(t, rstd.v, t * rstd.rest);
   }
+  if (a.y && left > 0) store8(static_cast<T *>(a.y) + row * a.ldy + c, left, y);
+  if constexpr (PACK) pack8_quad(p, row, c, left, y);   // zeros beyond the row, or NaN
 }
 
 // LANES threads a row, at least four, NV vectors a thread.
@@ -162,8 +173,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_rows_kernel(dip
       if (c < n) store8(static_cast<T *>(a.total) + row * a.ldt + c, n - c, v[j]);
     }
   }
-  const float rstd = rstd_of(lanes_sum<LANES>(sum, s, turn), 1.f / float(n), a.eps);
-  if (t == 0 && a.rstd) a.rstd[row] = rstd;
+  const Rstd rstd(lanes_sum<LANES>(sum, s, turn), n, a.eps);
+  if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
 #pragma unroll
   for (int j = 0; j < NV; ++j) write8<T, PACK>(a, p, row, (t + j * LANES) * 8, rstd, v[j]);
 }
@@ -197,8 +208,8 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int
     for (int q = 0; q < 8; ++q) sum += v[q] * v[q];
     if (total) store8(total + c, n - c, v);
   }
-  const float rstd = rstd_of(lanes_sum<1024>(sum, s, turn), 1.f / float(n), a.eps);
-  if (t == 0 && a.rstd) a.rstd[row] = rstd;
+  const Rstd rstd(lanes_sum<1024>(sum, s, turn), n, a.eps);
+  if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
   for (int c = t * 8; c < (n + 31) / 32 * 32; c += 1024 * 8) {
     float v[8] = {};
     if (c < n) {
@@ -293,6 +304,98 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_grad_kernel(dip
   }
 }
 
+// Few rows: dx by workgroups of kRows rows, and dgamma beside them by workgroups of 64
+// columns that read the rows again, out of the caches: one launch, no workspace.
+template <class T, class G, int LANES, int NV>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel(dip_rms_norm_grad_args a, int row_blocks) {
+  constexpr int kThreads = LANES < 256 ? 256 : LANES, kRows = kThreads / LANES;
+  __shared__ float s[2 * (LANES > 64 ? LANES / 64 : 1)];
+  __shared__ float sums[kThreads / 8][64 + 2];
+  const int n = int(a.c);
+  if (int(blockIdx.x) < row_blocks) {
+    int turn = 0;
+    const int t = threadIdx.x % LANES;
+    const int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+    if (row >= a.m) return;   // all lanes of a row
+    const float rstd = a.rstd[row];
+    Held<T> x[NV], d[NV], along[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (t + j * LANES) * 8;
+      x[j].get(static_cast<const T *>(a.total) + row * a.ldt, c, n);
+      d[j].get(static_cast<const T *>(a.dy) + row * a.ldy, c, n);
+      if (a.dtotal) along[j].get(static_cast<const T *>(a.dtotal) + row * a.lddt, c, n);
+    }
+    float xh[NV][8], h[NV][8], dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float g[8];
+      gamma8<T>(a.gamma, (t + j * LANES) * 8, n, g);
+      x[j].to(xh[j]);
+      d[j].to(h[j]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        xh[j][q] *= rstd;
+        h[j][q] *= g[q];
+        dot += h[j][q] * xh[j][q];
+      }
+    }
+    dot = lanes_sum<LANES>(dot, s, turn) / float(n);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (t + j * LANES) * 8;
+      float v[8] = {};
+      if (a.dtotal) along[j].to(v);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += rstd * (h[j][q] - xh[j][q] * dot);
+      if (c < n) store8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, v);
+    }
+    return;
+  }
+  const int c0 = (int(blockIdx.x) - row_blocks) * 64, c = c0 + int(threadIdx.x % 8) * 8, ty = threadIdx.x / 8;
+  float sum[8] = {};
+  if (c < n) {
+    // rows ty, ty + kThreads / 8, ..: four at a time, their loads first
+    const T *x = static_cast<const T *>(a.total), *dy = static_cast<const T *>(a.dy);
+    constexpr int kStep = kThreads / 8;
+    for (int64_t row = ty; row < a.m; row += 4 * kStep) {
+      Held<T> p[4], q[4];
+      float r[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t at = row + u * kStep;
+        r[u] = 0.f;
+        if (at < a.m) {
+          r[u] = a.rstd[at];
+          p[u].get(x + at * a.ldt, c, n);
+          q[u].get(dy + at * a.ldy, c, n);
+        } else {
+          p[u].t = q[u].t = typename Held<T>::Words(0);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float v[8], w[8];
+        p[u].to(v);
+        q[u].to(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += w[i] * (v[i] * r[u]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[ty][threadIdx.x % 8 * 8 + i] = sum[i];
+  __syncthreads();
+  if (threadIdx.x < 64 && c0 + int(threadIdx.x) < n) {
+    float v = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < kThreads / 8; ++i) v += sums[i][threadIdx.x];
+    G *out = static_cast<G *>(a.dgamma) + c0 + threadIdx.x;
+    if (a.accumulate) v += float(*out);
+    *out = G(v);
+  }
+}
+
 // Rows of any length: dx by a workgroup that goes over its row twice.
 template <class T>
 __global__ __launch_bounds__(1024) void rms_long_grad_kernel(dip_rms_norm_grad_args a, int64_t row0) {
@@ -362,8 +465,10 @@ __global__ __launch_bounds__(256) void rms_no_columns_kernel(int64_t n, float r,
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) rstd[i] = r;
 }
 
-// f(lanes, vectors) for a row of c columns that registers hold.
-template <class F>
+// f(lanes, vectors) for a row of c columns that registers hold.  Up to 4096 columns the
+// gradient, which has more to hold, takes 512 threads of one vector (65,536 x 3584 bf16
+// 318 us, 256 threads of two 325).
+template <bool GRAD, class F>
 void shape(int64_t c, F &&f) {
   const auto i = [](auto v) { return v; };
   using std::integral_constant;
@@ -376,16 +481,25 @@ void shape(int64_t c, F &&f) {
   DIP_SHAPE(64, 1);
   DIP_SHAPE(64, 2);
   DIP_SHAPE(256, 1);
-  DIP_SHAPE(256, 2);
+  if constexpr (GRAD) {
+    DIP_SHAPE(512, 1);
+  } else {
+    DIP_SHAPE(256, 2);
+  }
   DIP_SHAPE(512, 2);
   DIP_SHAPE(1024, 2);
 #undef DIP_SHAPE
 }
+template <bool GRAD>
 int lanes_of(int64_t c) {
   int lanes = 1024;
-  shape(c, [&](auto l, auto) { lanes = l; });
+  shape<GRAD>(c, [&](auto l, auto) { lanes = l; });
   return lanes;
 }
+
+// Rows up to which dgamma is summed beside dx
+constexpr int64_t kFewRows = 256;
+bool few_rows(const dip_rms_norm_grad_args &a) { return a.m <= kFewRows && a.c <= kGradHeldMost && a.dx && a.dgamma; }
 
 struct GradPlan {
   int64_t blocks = 1, chunk = 0;   // workgroups that each leave a row of partial sums; rows a chunk (long rows)
@@ -398,10 +512,12 @@ GradPlan grad_plan(const dip_rms_norm_grad_args &a) {
     p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + 15) / 16, 2048 / cols));
     p.chunk = (a.m + p.blocks - 1) / p.blocks;
   } else {
-    const int lanes = lanes_of(a.c), rows = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
-    p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + rows - 1) / rows, 256 * 1024 / threads));
+    const int lanes = lanes_of<true>(a.c), rows = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
+    // eight waves a CU: more keep no more loads on their way, leave more sums, and run
+    // into each other (65,536 x 3584 bf16: 256 workgroups of 512 318 us, 512 332, 1024 357)
+    p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + rows - 1) / rows, std::max(1, 512 / threads) * 256));
   }
-  p.bytes = a.dgamma ? up16(p.blocks * a.c * 4) : 0;
+  p.bytes = a.dgamma && !few_rows(a) ? up16(p.blocks * a.c * 4) : 0;
   return p;
 }
 
@@ -409,7 +525,7 @@ template <class T, bool PACK>
 hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
   const Packed p = make_packed(a.packed);
   // a launch has fewer than 2^32 threads
-  const int64_t most = (int64_t(1) << 31) / (a.c > kHeldMost ? 1024 : lanes_of(a.c));
+  const int64_t most = (int64_t(1) << 31) / (a.c > kHeldMost ? 1024 : lanes_of<false>(a.c));
   for (int64_t row0 = 0; row0 < a.m; row0 += most) {
     dip_rms_norm_args b = a;
     b.m = std::min(a.m, row0 + most);
@@ -417,7 +533,7 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
     if (a.c > kHeldMost) {
       rms_long_kernel<T, PACK><<<dim3(uint32_t(rows)), dim3(1024), 0, st>>>(b, row0, p);
     } else {
-      shape(a.c, [&](auto l, auto v) {
+      shape<false>(a.c, [&](auto l, auto v) {
         constexpr int kLanes = decltype(l)::value, kThreads = kLanes < 256 ? 256 : kLanes, kRows = kThreads / kLanes;
         rms_rows_kernel<T, kLanes, decltype(v)::value, PACK>
             <<<dim3(uint32_t((rows + kRows - 1) / kRows)), dim3(kThreads), 0, st>>>(b, row0, p);
@@ -431,6 +547,18 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
 
 template <class T>
 hipError_t backward(const dip_rms_norm_grad_args &a, hipStream_t st) {
+  if (few_rows(a)) {
+    shape<true>(a.c, [&](auto l, auto v) {
+      constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value, kThreads = kLanes < 256 ? 256 : kLanes;
+      if constexpr (kLanes * kNV * 8 <= kGradHeldMost) {
+        const int rows = int((a.m + kThreads / kLanes - 1) / (kThreads / kLanes));
+        const dim3 grid(uint32_t(rows + (a.c + 63) / 64));
+        if (a.accumulate) rms_few_grad_kernel<T, float, kLanes, kNV><<<grid, dim3(kThreads), 0, st>>>(a, rows);
+        else rms_few_grad_kernel<T, T, kLanes, kNV><<<grid, dim3(kThreads), 0, st>>>(a, rows);
+      }
+    });
+    return hipGetLastError();
+  }
   const GradPlan p = grad_plan(a);
   float *partial = a.dgamma ? static_cast<float *>(a.workspace) : nullptr;
   if (a.c > kGradHeldMost) {
@@ -444,7 +572,7 @@ hipError_t backward(const dip_rms_norm_grad_args &a, hipStream_t st) {
       rms_long_dgamma_kernel<T>
           <<<dim3(uint32_t((a.c + 255) / 256), uint32_t(p.blocks)), dim3(256), 0, st>>>(a, p.chunk, partial);
   } else {
-    shape(a.c, [&](auto l, auto v) {
+    shape<true>(a.c, [&](auto l, auto v) {
       constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value, kThreads = kLanes < 256 ? 256 : kLanes;
       if constexpr (kLanes * kNV * 8 <= kGradHeldMost)
         rms_grad_kernel<T, kLanes, kNV><<<dim3(uint32_t(p.blocks)), dim3(kThreads), 0, st>>>(a, partial);

@@ -59,6 +59,27 @@ struct Shares {
   Divide vectors, in_head;   // vectors a head; heads a token
 };
 
+// Where an item's pairs lie and go.
+template <class T>
+struct Item {
+  const T *p;
+  T *o;
+  uint32_t v, n;   // vector of the head, token of the workgroup
+  __device__ __forceinline__ Item(const dip_rotary_args &a, const Shares &sh, uint32_t i, int64_t i0, int h0, int heads) {
+    const uint32_t x = sh.vectors(i);
+    v = i - x * sh.vectors.by;
+    n = heads == sh.heads ? sh.in_head(x) : x / uint32_t(heads);
+    const int h = int(x - n * uint32_t(heads)) + h0;
+    const int64_t token = i0 + n;
+    const bool of_q = h < a.heads;
+    const int64_t hk = of_q ? h : h - a.heads;
+    p = of_q ? static_cast<const T *>(a.q) + token * a.q_st + hk * a.q_sh
+             : static_cast<const T *>(a.k) + token * a.k_st + hk * a.k_sh;
+    o = of_q ? static_cast<T *>(a.q_out) + token * a.qo_st + hk * a.qo_sh
+             : static_cast<T *>(a.k_out) + token * a.ko_st + hk * a.ko_sh;
+  }
+};
+
 // V pairs a thread.
 template <class T, int V, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int64_t token0, Shares sh) {
@@ -66,42 +87,31 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int
   const int64_t i0 = token0 + int64_t(blockIdx.x) * sh.tokens;
   const int tokens = int(min(int64_t(sh.tokens), a.t - i0)), all = a.heads + a.keys;
   const int h0 = int(blockIdx.y) * sh.heads, heads = min(sh.heads, all - h0);
-  for (int i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
-    const int n = i / a.pairs, j = i - n * a.pairs, axis = a.axis[j];
+  const uint32_t items = uint32_t(tokens) * uint32_t(heads) * sh.vectors.by;
+  const int step = INTERLEAVED ? V : a.pairs;   // from an item's first vector to its second
+  float u[V], w[V];
+  auto fetch = [&](const Item<T> &it) __attribute__((always_inline)) {
+    const T *p = it.p + int(it.v) * V * (INTERLEAVED ? 2 : 1);
+    load<T, V>(p, u);
+    load<T, V>(p + step, w);
+  };
+  uint32_t i = threadIdx.x;
+  if (i < items) fetch(Item<T>(a, sh, i, i0, h0, heads));   // on its way while the table is made
+  for (int j = threadIdx.x; j < tokens * a.pairs; j += kThreads) {
+    const int n = j / a.pairs, pair = j - n * a.pairs, axis = a.axis[pair];
     float2 cs = {1.f, 0.f};
     if (axis >= 0 && axis < a.axes) {
-      double turns = position(a, (i0 + n) * a.p_st + axis * a.p_sa) * a.freq[j] * 0.15915494309189533577;
+      double turns = position(a, (i0 + n) * a.p_st + axis * a.p_sa) * a.freq[pair] * 0.15915494309189533577;
       turns -= rint(turns);
       sincospif(2.f * float(turns), &cs.y, &cs.x);
       if (a.inverse) cs.y = -cs.y;
     }
-    table[i] = cs;
+    table[j] = cs;
   }
   __syncthreads();
-  const uint32_t items = uint32_t(tokens) * uint32_t(heads) * sh.vectors.by;
-  for (uint32_t i = threadIdx.x; i < items; i += kThreads) {
-    const uint32_t x = sh.vectors(i), v = i - x * sh.vectors.by;
-    uint32_t n, h;
-    if (heads == sh.heads) {
-      n = sh.in_head(x);
-      h = x - n * sh.in_head.by;
-    } else {
-      n = x / uint32_t(heads);
-      h = x - n * uint32_t(heads);
-    }
-    h += h0;
-    const int64_t token = i0 + n;
-    const bool of_q = int(h) < a.heads;
-    const int64_t hk = of_q ? h : int64_t(h) - a.heads;
-    const T *p = of_q ? static_cast<const T *>(a.q) + token * a.q_st + hk * a.q_sh
-                      : static_cast<const T *>(a.k) + token * a.k_st + hk * a.k_sh;
-    T *o = of_q ? static_cast<T *>(a.q_out) + token * a.qo_st + hk * a.qo_sh
-                : static_cast<T *>(a.k_out) + token * a.ko_st + hk * a.ko_sh;
-    const int first = int(v) * V * (INTERLEAVED ? 2 : 1), second = INTERLEAVED ? first + V : first + a.pairs;
-    float u[V], w[V];
-    load<T, V>(p + first, u);
-    load<T, V>(p + second, w);
-    const float2 *cs = table + n * a.pairs + v * V;
+  while (i < items) {
+    const Item<T> it(a, sh, i, i0, h0, heads);
+    const float2 *cs = table + it.n * a.pairs + it.v * V;
     float ou[V], ow[V];
     if constexpr (INTERLEAVED && V > 1) {
 #pragma unroll
@@ -120,8 +130,11 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int
         ow[j] = u[j] * c.y + w[j] * c.x;
       }
     }
-    store<T, V>(o + first, ou);
-    store<T, V>(o + second, ow);
+    T *o = it.o + int(it.v) * V * (INTERLEAVED ? 2 : 1);
+    store<T, V>(o, ou);
+    store<T, V>(o + step, ow);
+    i += kThreads;
+    if (i < items) fetch(Item<T>(a, sh, i, i0, h0, heads));
   }
 }
 
@@ -146,14 +159,18 @@ hipError_t rotary(const dip_rotary_args &a, hipStream_t st) {
   if (a.pairs > 0) {
     const int V = a.pairs % 8 == 0 ? 8 : a.pairs % 4 == 0 ? 4 : a.pairs % 2 == 0 ? 2 : 1;
     const int vectors = a.pairs / V;
-    // tokens for about eight items a thread, of up to 2048 pairs; where the tokens are
-    // few the heads are shared out too
+    // One item a thread: as many tokens as that takes, with tables of up to 2048 pairs, or
+    // even shares of one token's heads (65,536 x 28 heads of 128, bf16: one token 153 us,
+    // 6.1 TB/s, two 166, four 171, sixteen 186: a workgroup that loops waits for each
+    // round's loads).
     Shares sh{1, all, Divide(uint32_t(vectors)), Divide(1)};
     const int64_t an = int64_t(all) * vectors;
-    sh.tokens = int32_t(std::max<int64_t>(1, std::min<int64_t>({8 * kThreads / an, 2048 / a.pairs, (a.t + 1023) / 1024})));
-    if (a.t * an < int64_t(1024) * 8 * kThreads && an > kThreads)
-      sh.heads = std::max<int32_t>(1, kThreads / vectors);
-    while ((all + sh.heads - 1) / sh.heads > 65535) sh.heads *= 2;
+    if (an <= kThreads) {
+      sh.tokens = int32_t(std::max<int64_t>(1, std::min<int64_t>(kThreads / an, 2048 / a.pairs)));
+    } else {
+      const int64_t parts = std::min<int64_t>((an + kThreads - 1) / kThreads, 65535);
+      sh.heads = int32_t((all + parts - 1) / parts);
+    }
     sh.in_head = Divide(uint32_t(sh.heads));
     const uint32_t parts = uint32_t((all + sh.heads - 1) / sh.heads);
     // a launch has fewer than 2^32 threads

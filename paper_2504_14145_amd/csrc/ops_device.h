@@ -167,45 +167,53 @@ inline Packed make_packed(const dip_packed8 &p) {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(1)));
 
-// The largest finite magnitude of eight values.
-__device__ __forceinline__ float finite_most(const float (&v)[8]) {
-  float most = 0.f;
+// Magnitudes are compared as integers: infinity and NaN are above all others.
+constexpr uint32_t kInfinity = 0x7f800000u;
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t most_of(const float (&v)[8]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
+  return most;
+}
+// Makes what is not finite NaN, and the largest magnitude of the others.
+__device__ __forceinline__ uint32_t finite_most(float (&v)[8]) {
+  uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float a = fabsf(v[i]);
-    most = a < INFINITY && a > most ? a : most;
+    const uint32_t a = magnitude(v[i]);
+    if (a >= kInfinity) v[i] = NAN;
+    else most = max(most, a);
   }
   return most;
 }
 // The largest over the four lanes 4 j .. 4 j + 3, which are all on.
-__device__ __forceinline__ float quad_most(float a) {
-  const int x = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0xb1, 0xf, 0xf, true);   // lane ^ 1
-  a = fmaxf(a, __builtin_bit_cast(float, x));
-  const int y = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0x4e, 0xf, 0xf, true);   // lane ^ 2
-  return fmaxf(a, __builtin_bit_cast(float, y));
+__device__ __forceinline__ uint32_t quad_most(uint32_t a) {
+  a = max(a, uint32_t(__builtin_amdgcn_mov_dpp(int(a), 0xb1, 0xf, 0xf, true)));      // lane ^ 1
+  return max(a, uint32_t(__builtin_amdgcn_mov_dpp(int(a), 0x4e, 0xf, 0xf, true)));   // lane ^ 2
 }
-// The byte e + 127 of the smallest 2^e, e >= -126, with most / 2^e <= 448 = 1.75 2^8.
-__device__ __forceinline__ uint32_t scale_byte(float most) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, most);
-  return uint32_t(max(int(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), 1));
+// The byte e + 127 of the smallest 2^e, e >= -126, with most / 2^e <= 448 = 1.75 2^8,
+// by the bits of most.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
+  return uint32_t(max(int(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0), 1));
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) {
   const uint32_t b = byte ? byte << 23 : 0x400000u;
   return __builtin_bit_cast(float, byte == 255 ? 0x7fc00000u : b);
 }
-// Eight values over 2^e in 8 bits.  The conversion rounds to nearest even; its inputs
-// are at most 448, or NaN for what is not finite.
+// Eight values over 2^e in 8 bits: at most 448 each, or NaN.  The conversions divide by
+// the scale and round to nearest even (found the same as a product by 2^-e and the
+// conversion without a scale for every 16-bit value and every scale).
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u32x2 round8bits(uint32_t byte, const float (&v)[8]) {
-  const float inv = __builtin_bit_cast(float, (254u - byte) << 23);   // 2^-e, byte 1 .. 247
-  float q[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = fabsf(v[i]) < INFINITY ? v[i] * inv : NAN;
+  const float scale = __builtin_bit_cast(float, byte << 23);   // byte 1 .. 247
   u32x2 r;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], w, true);
-    r[i] = uint32_t(w);
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[4 * i], v[4 * i + 1], scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[4 * i + 2], v[4 * i + 3], scale, true);
+    r[i] = __builtin_bit_cast(uint32_t, w);
   }
   return r;
 }
@@ -226,15 +234,37 @@ __device__ __forceinline__ u32x2 load8bits(const uint8_t *p, int left) {
     if (i < left) r[i / 4] |= uint32_t(p[i]) << (8 * (i % 4));
   return r;
 }
+// Exact for every value and scale.
 __device__ __forceinline__ void from8bits(u32x2 r, float scale, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(r[i]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(r[i]), true);
-    v[4 * i] = lo[0] * scale;
-    v[4 * i + 1] = lo[1] * scale;
-    v[4 * i + 2] = hi[0] * scale;
-    v[4 * i + 3] = hi[1] * scale;
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(r[i], scale, false),
+               hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(r[i], scale, true);
+    v[4 * i] = lo[0];
+    v[4 * i + 1] = lo[1];
+    v[4 * i + 2] = hi[0];
+    v[4 * i + 3] = hi[1];
   }
+}
+// The same in 16 bits, for scales from 2^-15 to 2^7 in float16, whose values that holds,
+// and from 2^-124 to 2^119 in bfloat16.
+__device__ __forceinline__ bool held_by(_Float16, uint32_t byte) { return byte - 112u <= 22u; }
+__device__ __forceinline__ bool held_by(__bf16, uint32_t byte) { return byte - 3u <= 243u; }
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type from8bits_to(u32x2 r, float scale) {
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  T2 q[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (__is_same(T, _Float16)) {
+      q[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(r[i], scale, false);
+      q[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(r[i], scale, true);
+    } else {
+      q[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[i], scale, false);
+      q[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[i], scale, true);
+    }
+  }
+  return typename Vec8<T>::type{q[0][0], q[0][1], q[1][0], q[1][1], q[2][0], q[2][1], q[3][0], q[3][1]};
 }
 // What rounded up beyond the largest value of T in 8 bits is that value; NaN stays.
 template <class T>
@@ -244,10 +274,12 @@ __device__ __forceinline__ float within(float v) {
   return v > kMost ? kMost : v < -kMost ? -kMost : v;
 }
 // Packs a quad's 32 columns from `col` % 32 == 8 (lane % 4) on, of which the lane has
-// `left`; all four lanes are on, one without columns writes nothing.
-__device__ __forceinline__ void pack8_quad(const Packed &p, int64_t row, int64_t col, int left, const float (&v)[8]) {
-  const uint32_t byte = scale_byte(quad_most(finite_most(v)));
+// `left`, zeros beyond them; all four lanes are on, one without columns writes nothing.
+__device__ __forceinline__ void pack8_quad(const Packed &p, int64_t row, int64_t col, int left, float (&v)[8]) {
+  uint32_t most = quad_most(most_of(v));
+  if (most >= kInfinity) most = quad_most(finite_most(v));   // the four lanes agree
   if (left <= 0) return;
+  const uint32_t byte = scale_byte(most);
   store8bits(p.q + row * p.ld + col, left, round8bits(byte, v));
   if (col % 32 == 0) p.s[row * p.lds + col / 32] = uint8_t(byte);
 }

@@ -193,9 +193,12 @@ class Packed8:
 
     @classmethod
     def empty(cls, m: int, n: int, device="cuda") -> "Packed8":
-        import torch
-        return cls(torch.empty((m, n), dtype=torch.float8_e4m3fn, device=device),
-                   torch.empty((m, -(-n // 32)), dtype=torch.uint8, device=device))
+        if _torch is None:
+            _load()
+        p = cls.__new__(cls)
+        p.values = _empty((m, n), dtype=_torch.float8_e4m3fn, device=device)
+        p.scales = _empty((m, -(-n // 32)), dtype=_torch.uint8, device=device)
+        return p
 
     @property
     def shape(self):
@@ -272,6 +275,11 @@ def _rows(t, shape, dtype, index, name):
 
 
 _NONE4 = (0, 0, 0, 0)
+
+
+def _like(t):
+    """A contiguous tensor of t's shape and type."""
+    return _torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _packed(p, shape, index, name):
@@ -564,8 +572,10 @@ def pack8(x, out=None, stream=None):
     shape = m, n = x.shape
     if out is None:
         out = Packed8.empty(m, n, x.device)
+        args = _pack_packed(out.values.data_ptr(), n, out.scales.data_ptr(), -(-n // 32))
+    else:
+        args = _pack_packed(*_packed(out, shape, dev, "out"))
     px, ldx = _matrix(x, shape, dt, dev, "x")
-    args = _pack_packed(*_packed(out, shape, dev, "out"))
     if _recording() and x.requires_grad:
         _cut_off("pack8")
     _call_flat("dip_pack8", dev, code, m, n, px, ldx, args)
@@ -588,10 +598,13 @@ def unpack8(p, dtype=None, act="none", out=None, stream=None):
     code = _types.get(dtype)
     _need(code is not None, f"{dtype} is not float32, float16 or bfloat16")
     shape = m, n = p.shape
-    if out is None:
-        out = _empty(shape, dtype=dtype, device=p.device)
     args = _pack_packed(*_packed(p, shape, dev, "p"))
-    _call_flat("dip_unpack8", dev, code, m, n, args, _act(act), *_matrix(out, shape, dtype, dev, "out"))
+    if out is None:
+        out = p.values.new_empty(shape, dtype=dtype)
+        py, ldy = out.data_ptr(), n
+    else:
+        py, ldy = _matrix(out, shape, dtype, dev, "out")
+    _call_flat("dip_unpack8", dev, code, m, n, args, _act(act), py, ldy)
     return out
 
 
@@ -610,24 +623,37 @@ def rms_norm(x, gamma=None, eps=1e-5, residual=None, packed=None, need_out=True,
         return _on(stream, rms_norm, x, gamma, eps, residual, packed, need_out, out, total, rstd)
     _need(x.dim() == 2, "x is a matrix")
     shape = m, c = x.shape
+    py = pt = _NONE
+    pp = _NONE4
+    # what is allocated here needs no check
     if not need_out:
         out = None
     elif out is None:
-        out = x.new_empty(shape)
+        out = _like(x)
+        py = out.data_ptr(), c
+    else:
+        py = _matrix(out, shape, dt, dev, "out")
     if residual is None:
         _need(total is None, "total goes with a residual: without one it is x")
     elif total is None:
-        total = x.new_empty(shape)
+        total = _like(x)
+        pt = total.data_ptr(), c
+    else:
+        pt = _matrix(total, shape, dt, dev, "total")
     if rstd is None:
         rstd = x.new_empty((m,), dtype=_torch.float32)
+        pr = rstd.data_ptr()
+    else:
+        pr = _whole(rstd, (m,), _torch.float32, dev, "rstd")
     if packed is True:
         packed = Packed8.empty(m, c, x.device)
+        pp = packed.values.data_ptr(), c, packed.scales.data_ptr(), -(-c // 32)
     elif packed is False:
         packed = None
+    else:
+        pp = _packed(packed, shape, dev, "packed")
     args = _pack_rms(m, c, code, eps, *_matrix(x, shape, dt, dev, "x"), *_matrix(residual, shape, dt, dev, "residual"),
-                     _whole(gamma, (c,), dt, dev, "gamma"), *_matrix(total, shape, dt, dev, "total"),
-                     *_matrix(out, shape, dt, dev, "out"), *_packed(packed, shape, dev, "packed"),
-                     _whole(rstd, (m,), _torch.float32, dev, "rstd"))
+                     _whole(gamma, (c,), dt, dev, "gamma"), *pt, *py, *pp, pr)
     if _recording() and (x.requires_grad or gamma is not None and gamma.requires_grad
                          or residual is not None and residual.requires_grad):
         _cut_off("rms_norm")
@@ -650,21 +676,27 @@ def rms_norm_backward(dy, total, rstd, gamma=None, dtotal=None, need_dx=True, ne
     _need(total is not None and rstd is not None, "total and rstd (the forward's) are needed")
     shape = m, c = dy.shape
     _need(dgamma is None or gamma is not None, "dgamma goes with gamma")
+    f32 = _torch.float32
+    px, pg = _NONE, 0
     if gamma is None or not need_dgamma:
         dgamma = None
     elif dgamma is None:
         _need(not accumulate, "accumulate: dgamma has to be given")
         dgamma = dy.new_empty((c,))
+        pg = dgamma.data_ptr()
+    else:
+        pg = _whole(dgamma, (c,), f32 if accumulate else dt, dev, "dgamma")
     if not need_dx:
         dx = None
     elif dx is None:
-        dx = dy.new_empty(shape)
-    f32 = _torch.float32
+        dx = _like(dy)
+        px = dx.data_ptr(), c
+    else:
+        px = _matrix(dx, shape, dt, dev, "dx")
     args = _pack_rms_grad(m, c, code, int(bool(accumulate)), *_matrix(dy, shape, dt, dev, "dy"),
                           *_matrix(total, shape, dt, dev, "total"), _whole(gamma, (c,), dt, dev, "gamma"),
                           _whole(rstd, (m,), f32, dev, "rstd"), *_matrix(dtotal, shape, dt, dev, "dtotal"),
-                          *_matrix(dx, shape, dt, dev, "dx"),
-                          _whole(dgamma, (c,), f32 if accumulate else dt, dev, "dgamma"), 0, 0)
+                          *px, pg, 0, 0)
     _call("dip_rms_norm_grad", args, dev)
     return dx, dgamma
 
@@ -708,17 +740,23 @@ def _turn(name, q, positions, frequencies, axis, k, interleaved, out, out_k, inv
     _need(isinstance(frequencies, _torch.Tensor) and frequencies.dim() == 1, "frequencies: want a tensor [pairs]")
     pairs = frequencies.shape[0]
     _need(2 * pairs <= dim, f"{pairs} pairs in a head of {dim} elements")
+    po, pk_out = _NONE3, _NONE3
     if out is None:
         out = q.new_empty(q.shape)
-    if k is not None and out_k is None:
+        po = out.data_ptr(), heads * dim, dim
+    else:
+        po = _rows(out, q.shape, dt, dev, "out")
+    if k is None:
+        _need(out_k is None, "out_k goes with k")
+    elif out_k is None:
         out_k = k.new_empty(k.shape)
-    _need(k is not None or out_k is None, "out_k goes with k")
+        pk_out = out_k.data_ptr(), keys * dim, dim
+    else:
+        pk_out = _rows(out_k, k.shape, dt, dev, "out_k")
     args = _pack_rotary(t, heads, keys, dim, pairs, axes, code, _positions[positions.dtype], int(bool(interleaved)),
                         inverse, *pq, *pk, positions.data_ptr(), positions.stride(0), sa,
                         _whole(frequencies, (pairs,), _torch.float64, dev, "frequencies"),
-                        _whole(axis, (pairs,), _torch.int32, dev, "axis"),
-                        *_rows(out, q.shape, dt, dev, "out"),
-                        *(_NONE3 if k is None else _rows(out_k, k.shape, dt, dev, "out_k")))
+                        _whole(axis, (pairs,), _torch.int32, dev, "axis"), *po, *pk_out)
     if not inverse and _recording() and (q.requires_grad or k is not None and k.requires_grad):
         _cut_off(name)
     _call("dip_rotary", args, dev)
