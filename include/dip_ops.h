@@ -303,7 +303,7 @@ int dip_rms_norm_grad(const dip_rms_norm_grad_args *a, void *stream);
  * itself (same pointer and strides). */
 typedef struct {
   int64_t t;                 /* tokens                                          */
-  int32_t heads, keys;       /* heads of q and of k                             */
+  int32_t heads, keys;       /* heads of q and of k, up to 65,536 together      */
   int32_t dim, pairs, axes;  /* elements a head, up to 2048; 2 pairs <= dim     */
   int32_t dtype, pos_type, interleaved, inverse;
   const void *q;             /* [t][heads][dim]                                 */

@@ -377,7 +377,7 @@ int check_rotary(const dip_rotary_args *a) {
   if (!a || !known_type(a->dtype) || a->pos_type < DIP_POS_I32 || a->pos_type > DIP_POS_F32) return DIP_E_INVAL;
   if (a->t < 0 || a->heads < 0 || a->keys < 0 || a->dim < 0 || a->pairs < 0 || a->axes < 0 || 2 * int64_t(a->pairs) > a->dim)
     return DIP_E_INVAL;
-  if (a->t >= kMaxRows || a->dim > 2048 || int64_t(a->heads) + a->keys > (int64_t(1) << 20)) return DIP_E_RANGE;
+  if (a->t >= kMaxRows || a->dim > 2048 || int64_t(a->heads) + a->keys > 65536) return DIP_E_RANGE;
   OPS_CHECK(check_heads(a->q, a, a->heads, a->q_st, a->q_sh));
   OPS_CHECK(check_heads(a->q_out, a, a->heads, a->qo_st, a->qo_sh));
   OPS_CHECK(check_heads(a->k, a, a->keys, a->k_st, a->k_sh));

@@ -87,11 +87,14 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
         uint32_t scale[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          bits[u] = load8bits(g.kept.q + (row + 8 * u) * g.kept.ld + col, left);
+          bits[u] = load8bits(g.kept.q + (row + 8 * u) * g.kept.ld, int(col), int(g.n));
           scale[u] = g.kept.s[(row + 8 * u) * g.kept.lds + col / 32];
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) from8bits(bits[u], scale_of(scale[u]), z[u]);
+        for (int u = 0; u < U; ++u) {
+          place8bits(int(col), int(g.n), bits[u]);
+          from8bits(bits[u], scale_of(scale[u]), z[u]);
+        }
       } else if (g.pre) {
 #pragma unroll
         for (int u = 0; u < U; ++u) load8(pre + (row + 8 * u) * g.ldp, left, z[u]);

@@ -555,7 +555,7 @@ __global__ __launch_bounds__(256) void join_kept_kernel(int64_t m, int64_t n, Ke
   float kept[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) kept[j] = v[j];
-  pack8_quad(e.kept, row, col, left, kept);
+  pack8_quad(e.kept, row, int(col), left, kept);
   if (left <= 0) return;
   Epilogue rest = e;
   rest.bias = nullptr;

@@ -11,20 +11,22 @@ constexpr int kThreads = 256;
 // Eight columns of a row a thread, four threads a scale; `per` is a multiple of four,
 // so that those are of one wave and all there.
 template <class T>
-__global__ __launch_bounds__(kThreads) void pack8_kernel(uint32_t items, uint32_t row0, Divide per, int64_t n,
+__global__ __launch_bounds__(kThreads) void pack8_kernel(uint32_t items, uint32_t row0, Divide per, int n,
                                                          const T *x, int64_t ldx, Packed out) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
   if (i >= items) return;
   const uint32_t in = per(i);
-  const int64_t row = int64_t(row0) + in, col = int64_t(i - in * per.by) * 8;
-  const int left = int(min(int64_t(8), n - col));
+  const int64_t row = int64_t(row0) + in;
+  const int col = int(i - in * per.by) * 8, left = min(8, n - col), by = Held<T>::moved(col, n);
+  Held<T> h;
+  h.get(x + row * ldx, col, n);
   if constexpr (sizeof(T) == 2) {
     // magnitudes compared and rounded two at a time, as they lie in memory
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     typedef T T2 __attribute__((ext_vector_type(2)));
-    const auto t = take8(x + row * ldx + col, left);
-    const u32x4 w = __builtin_bit_cast(u32x4, t) & 0x7fff7fffu;
+    const u32x4 words = h.words(by), w = words & 0x7fff7fffu;
+    const auto t = __builtin_bit_cast(typename Vec8<T>::type, words);
     auto two = [&](int j) { return __builtin_bit_cast(u16x2, uint32_t(w[j])); };
     const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(0), two(1)),
                                               __builtin_elementwise_max(two(2), two(3)));
@@ -48,28 +50,29 @@ __global__ __launch_bounds__(kThreads) void pack8_kernel(uint32_t items, uint32_
         r[j] = __builtin_bit_cast(uint32_t, q);
       }
       store8bits(out.q + row * out.ld + col, left, r);
-      if (col % 32 == 0) out.s[row * out.lds + col / 32] = uint8_t(byte);
+      if ((col & 31) == 0) out.s[row * out.lds + (col >> 5)] = uint8_t(byte);
       return;
     }
   }
   float v[8];
-  load8(x + row * ldx + col, left, v);
+  h.to(by, v);
   pack8_quad(out, row, col, left, v);
 }
 
 template <class T, bool ACT>
-__global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint32_t row0, Divide per, int64_t n,
-                                                           Packed x, int act, T *y, int64_t ldy, int64_t fill) {
+__global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint32_t row0, Divide per, int n,
+                                                           Packed x, int act, T *y, int64_t ldy, int fill) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
   if (i >= items) return;
   const uint32_t in = per(i);
-  const int64_t row = int64_t(row0) + in, col = int64_t(i - in * per.by) * 8;
-  const int left = int(min(int64_t(8), n - col));
+  const int64_t row = int64_t(row0) + in;
+  const int col = int(i - in * per.by) * 8;
   u32x2 bits = {0, 0};
   uint32_t byte = 127;
-  if (left > 0) {
-    bits = load8bits(x.q + row * x.ld + col, left);
-    byte = x.s[row * x.lds + col / 32];
+  if (col < n) {
+    bits = load8bits(x.q + row * x.ld, col, n);
+    byte = x.s[row * x.lds + (col >> 5)];
+    place8bits(col, n, bits);
   }
   T *out = y + row * ldy + col;
   if constexpr (!ACT && sizeof(T) == 2) {
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint3
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
-  store8(out, int(min(int64_t(8), fill - col)), v);   // beyond n act(0) = 0
+  put8(out, min(8, fill - col), v);   // beyond n act(0) = 0
 }
 
 // f(items, row0, Divide(per)) over launches of fewer than 2^31 items.
@@ -113,14 +116,14 @@ hipError_t pieces(int64_t m, int64_t per, F &&f) {
 template <class T>
 hipError_t pack(int64_t m, int64_t n, const void *x, int64_t ldx, const Packed &out, hipStream_t st) {
   return pieces(m, (n + 31) / 32 * 4, [&](dim3 grid, uint32_t items, uint32_t row0, const Divide &per) {
-    pack8_kernel<T><<<grid, dim3(kThreads), 0, st>>>(items, row0, per, n, static_cast<const T *>(x), ldx, out);
+    pack8_kernel<T><<<grid, dim3(kThreads), 0, st>>>(items, row0, per, int(n), static_cast<const T *>(x), ldx, out);
   });
 }
 template <class T>
 hipError_t unpack(int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill, hipStream_t st) {
   return pieces(m, (fill + 7) / 8, [&](dim3 grid, uint32_t items, uint32_t row0, const Divide &per) {
     auto go = [&](auto kernel) {
-      kernel<<<grid, dim3(kThreads), 0, st>>>(items, row0, per, n, x, act, static_cast<T *>(y), ldy, fill);
+      kernel<<<grid, dim3(kThreads), 0, st>>>(items, row0, per, int(n), x, act, static_cast<T *>(y), ldy, int(fill));
     };
     act != DIP_ACT_NONE ? go(unpack8_kernel<T, true>) : go(unpack8_kernel<T, false>);
   });

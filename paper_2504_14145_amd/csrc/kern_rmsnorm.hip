@@ -14,79 +14,38 @@
 namespace dipops {
 namespace {
 
-// columns of a row held in registers: 1024 threads have 128 each, and the gradient's
-// next row has to fit beside its own
-constexpr int kHeldMost = 16384, kGradHeldMost = 8192;
+// Columns of a row held in registers; up to the second number the gradient's next row
+// fits beside its own, and gamma (1024 threads have 128 registers each).
+constexpr int kHeldMost = 16384, kAheadMost = 8192;
 
-// Over LANES consecutive threads, a power of two; beyond a wave s holds two sets of
-// the waves' values in turn, so that one barrier a sum is enough.
+// A row's threads: LANES of a wave, a power of two from four on, or, LANES 0, the whole
+// workgroup, as many waves as the row fills.
 template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v, float *s, int &turn) {
+struct Lanes {
+  static constexpr bool kWide = LANES == 0;
+  static constexpr int kMost = kWide ? 1024 : 256;           // threads a workgroup
+  static constexpr int kRows = kWide ? 1 : 256 / LANES;      // rows a workgroup has at once
+  static __device__ __forceinline__ int count() { return kWide ? int(blockDim.x) : LANES; }
+  static __device__ __forceinline__ int mine() { return kWide ? int(threadIdx.x) : int(threadIdx.x) % LANES; }
+  static __device__ __forceinline__ int row() { return kWide ? 0 : int(threadIdx.x) / LANES; }
+  // Their sum; beyond a wave s holds two sets of the waves' values in turn, so that one
+  // barrier a sum is enough.
+  static constexpr int kSums = kWide ? 32 : 1;
+  static __device__ __forceinline__ float sum(float v, float *s, int &turn) {
 #pragma unroll
-  for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) v += __shfl_xor(v, d);
-  if constexpr (LANES > 64) {
-    float *q = s + turn * (LANES / 64);
-    turn ^= 1;
-    if (threadIdx.x % 64 == 0) q[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = 0.f;
+    for (int d = 1; d < (kWide ? 64 : LANES); d *= 2) v += __shfl_xor(v, d);
+    if constexpr (kWide) {
+      const int waves = int(blockDim.x) / 64;
+      if (waves == 1) return v;
+      float *q = s + turn * 16;
+      turn ^= 1;
+      if (threadIdx.x % 64 == 0) q[threadIdx.x / 64] = v;
+      __syncthreads();
+      v = int(threadIdx.x % 16) < waves ? q[threadIdx.x % 16] : 0.f;
 #pragma unroll
-    for (int i = 0; i < LANES / 64; ++i) v += q[i];
-  }
-  return v;
-}
-
-// Columns c .. c + 7 of a row of n, as they lie in memory; zeros beyond it.  Where the
-// row ends inside them the eight that end with it are read and moved into place: all
-// lanes read whole vectors, and element by element the last lane costs a chain of loads.
-template <class T>
-struct Held {
-  static constexpr int kWords = sizeof(T) * 2;   // 32-bit words of eight
-  typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
-  typedef Words WordsAny __attribute__((aligned(sizeof(T))));
-  Words t;
-  __device__ __forceinline__ void get(const T *row, int c, int n) {
-    const int left = n - c;
-    if (left >= 8) {
-      t = *reinterpret_cast<const WordsAny *>(row + c);
-    } else if (left <= 0) {
-      t = Words(0);
-    } else if (n >= 8) {
-      t = *reinterpret_cast<const WordsAny *>(row + n - 8);
-      const int by = 8 - left;   // elements to move down
-      if constexpr (sizeof(T) == 2) {
-        if (by & 1) {
-#pragma unroll
-          for (int i = 0; i < kWords; ++i) t[i] = t[i] >> 16 | (i + 1 < kWords ? t[i + 1] << 16 : 0u);
-        }
-      }
-      constexpr int per = sizeof(T) == 2 ? 2 : 1;   // elements a word
-#pragma unroll
-      for (int d = 1; d < kWords; d *= 2) {
-        if (by / per & d) {
-#pragma unroll
-          for (int i = 0; i < kWords; ++i) t[i] = i + d < kWords ? t[i + d] : 0u;
-        }
-      }
-    } else {
-      float v[8];
-      load8(row + c, left, v);
-      put(v);
+      for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
     }
-  }
-  __device__ __forceinline__ void put(const float (&v)[8]) {
-    T e[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = T(v[i]);
-    t = __builtin_bit_cast(Words, e);
-  }
-  __device__ __forceinline__ void to(float (&v)[8]) const {
-    struct Elements {
-      T e[8];
-    };
-    const Elements e = __builtin_bit_cast(Elements, t);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = float(e.e[i]);
+    return v;
   }
 };
 
@@ -97,17 +56,17 @@ __device__ __forceinline__ void gamma8(const void *gamma, int c, int n, float (&
   if (gamma) {
     Held<T> h;
     h.get(static_cast<const T *>(gamma), c, n);
-    h.to(g);
+    h.to(Held<T>::moved(c, n), g);
   }
 }
 
 // t = x + residual of eight columns, rounded to the type.
 template <class T>
-__device__ __forceinline__ void total8(const Held<T> &x, const Held<T> &r, bool residual, float (&v)[8]) {
-  x.to(v);
+__device__ __forceinline__ void total8(const Held<T> &x, const Held<T> &r, bool residual, int by, float (&v)[8]) {
+  x.to(by, v);
   if (residual) {
     float q[8];
-    r.to(q);
+    r.to(by, q);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = float(T(v[i] + q[i]));
   }
@@ -139,51 +98,51 @@ __device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed 
     const float t = v[q] * g[q];   // exact of 2-byte types
     y[q] = fmaf(t, rstd.v, t * rstd.rest);
   }
-  if (a.y && left > 0) store8(static_cast<T *>(a.y) + row * a.ldy + c, left, y);
+  if (a.y && left > 0) put8(static_cast<T *>(a.y) + row * a.ldy + c, left, y);
   if constexpr (PACK) pack8_quad(p, row, c, left, y);   // zeros beyond the row, or NaN
 }
 
-// LANES threads a row, at least four, NV vectors a thread.
+// NV vectors a thread.
 template <class T, int LANES, int NV, bool PACK>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_rows_kernel(dip_rms_norm_args a, int64_t row0, Packed p) {
-  constexpr int kThreads = LANES < 256 ? 256 : LANES, kRows = kThreads / LANES;
-  __shared__ float s[2 * (LANES > 64 ? LANES / 64 : 1)];
+__global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_norm_args a, int64_t row0, Packed p) {
+  typedef Lanes<LANES> L;
+  __shared__ float s[L::kSums];
   int turn = 0;
-  const int t = threadIdx.x % LANES, n = int(a.c);
-  const int64_t row = row0 + int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+  const int t = L::mine(), lanes = L::count(), n = int(a.c);
+  const int64_t row = row0 + int64_t(blockIdx.x) * L::kRows + L::row();
   if (row >= a.m) return;   // all lanes of a row
   Held<T> x[NV], r[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int c = (t + j * LANES) * 8;
+    const int c = (t + j * lanes) * 8;
     x[j].get(static_cast<const T *>(a.x) + row * a.ldx, c, n);
     if (a.residual) r[j].get(static_cast<const T *>(a.residual) + row * a.ldr, c, n);
   }
   float v[NV][8], sum = 0.f;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    total8(x[j], r[j], a.residual != nullptr, v[j]);
+    total8(x[j], r[j], a.residual != nullptr, Held<T>::moved((t + j * lanes) * 8, n), v[j]);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum += v[j][q] * v[j][q];
   }
   if (a.total) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (t + j * LANES) * 8;
-      if (c < n) store8(static_cast<T *>(a.total) + row * a.ldt + c, n - c, v[j]);
+      const int c = (t + j * lanes) * 8;
+      if (c < n) put8(static_cast<T *>(a.total) + row * a.ldt + c, n - c, v[j]);
     }
   }
-  const Rstd rstd(lanes_sum<LANES>(sum, s, turn), n, a.eps);
+  const Rstd rstd(L::sum(sum, s, turn), n, a.eps);
   if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) write8<T, PACK>(a, p, row, (t + j * LANES) * 8, rstd, v[j]);
+  for (int j = 0; j < NV; ++j) write8<T, PACK>(a, p, row, (t + j * lanes) * 8, rstd, v[j]);
 }
 
 // Rows of any length: a workgroup goes over its row twice.  Where the sum is stored a
 // thread reads back what it wrote (the residual may be gone: they may be one array).
 template <class T, bool PACK>
 __global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int64_t row0, Packed p) {
-  __shared__ float s[2 * 16];
+  __shared__ float s[Lanes<0>::kSums];
   int turn = 0;
   const int t = threadIdx.x, n = int(a.c);
   const int64_t row = row0 + blockIdx.x;
@@ -206,9 +165,9 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int
     first(c, v);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum += v[q] * v[q];
-    if (total) store8(total + c, n - c, v);
+    if (total) put8(total + c, n - c, v);
   }
-  const Rstd rstd(lanes_sum<1024>(sum, s, turn), n, a.eps);
+  const Rstd rstd(Lanes<0>::sum(sum, s, turn), n, a.eps);
   if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
   for (int c = t * 8; c < (n + 31) / 32 * 32; c += 1024 * 8) {
     float v[8] = {};
@@ -225,16 +184,19 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int
 // A workgroup goes over rows j, j + gridDim.x, .. (kRows at a time) and keeps the sums
 // of dgamma of its columns on the way: partial[j][c].
 template <class T, int LANES, int NV>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_grad_kernel(dip_rms_norm_grad_args a, float *partial) {
-  constexpr int kThreads = LANES < 256 ? 256 : LANES, kRows = kThreads / LANES;
-  __shared__ float s[2 * (LANES > 64 ? LANES / 64 : 1)];
+__global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_grad_kernel(dip_rms_norm_grad_args a, float *partial) {
+  typedef Lanes<LANES> L;
+  constexpr int kRows = L::kRows;
+  __shared__ float s[L::kSums];
   __shared__ float sums[kRows > 1 ? kRows * LANES * NV * 8 : 1];
   int turn = 0;
-  const int t = threadIdx.x % LANES, n = int(a.c);
-  const float inv = 1.f / float(n);
-  float g[NV][8], sg[NV][8] = {};
+  const int t = L::mine(), lanes = L::count(), n = int(a.c);
+  constexpr bool kAhead = NV == 1;
+  float g[kAhead ? NV : 1][8], sg[NV][8] = {};
+  if constexpr (kAhead) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) gamma8<T>(a.gamma, (t + j * LANES) * 8, n, g[j]);
+    for (int j = 0; j < NV; ++j) gamma8<T>(a.gamma, (t + j * lanes) * 8, n, g[j]);
+  }
   // the next row is asked for before this one's sum is waited for
   Held<T> xn[NV], dn[NV], tn[NV];
   float rn = 0.f;
@@ -242,55 +204,57 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_grad_kernel(dip
     rn = a.rstd[row];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (t + j * LANES) * 8;
+      const int c = (t + j * lanes) * 8;
       xn[j].get(static_cast<const T *>(a.total) + row * a.ldt, c, n);
       dn[j].get(static_cast<const T *>(a.dy) + row * a.ldy, c, n);
       if (a.dtotal && a.dx) tn[j].get(static_cast<const T *>(a.dtotal) + row * a.lddt, c, n);
     }
   };
   const int64_t step = int64_t(gridDim.x) * kRows;
-  int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
-  if (row < a.m) fetch(row);
+  int64_t row = int64_t(blockIdx.x) * kRows + L::row();
+  if (kAhead && row < a.m) fetch(row);
   for (; row < a.m; row += step) {   // all lanes of a row
+    if (!kAhead) fetch(row);
     const float rstd = rn;
-    float xh[NV][8], h[NV][8], along[NV][8], dot = 0.f;
+    float xh[NV][8], h[NV][8], dot = 0.f;
+    Held<T> along[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      xn[j].to(xh[j]);
-      dn[j].to(h[j]);
-      if (a.dtotal && a.dx) tn[j].to(along[j]);
-      else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) along[j][q] = 0.f;
-      }
+      const int c = (t + j * lanes) * 8, by = Held<T>::moved(c, n);
+      xn[j].to(by, xh[j]);
+      dn[j].to(by, h[j]);
+      along[j] = tn[j];
+      if constexpr (!kAhead) gamma8<T>(a.gamma, c, n, g[0]);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         xh[j][q] *= rstd;
         sg[j][q] += h[j][q] * xh[j][q];
-        h[j][q] *= g[j][q];
+        h[j][q] *= g[kAhead ? j : 0][q];
         dot += h[j][q] * xh[j][q];
       }
     }
-    if (row + step < a.m) fetch(row + step);
+    if (kAhead && row + step < a.m) fetch(row + step);
     if (!a.dx) continue;
-    dot = lanes_sum<LANES>(dot, s, turn) * inv;
+    dot = L::sum(dot, s, turn) / float(n);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (t + j * LANES) * 8;
+      const int c = (t + j * lanes) * 8;
+      float v[8] = {};
+      if (a.dtotal) along[j].to(Held<T>::moved(c, n), v);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) h[j][q] = along[j][q] + rstd * (h[j][q] - xh[j][q] * dot);
-      if (c < n) store8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, h[j]);
+      for (int q = 0; q < 8; ++q) v[q] += rstd * (h[j][q] - xh[j][q] * dot);
+      if (c < n) put8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, v);
     }
   }
   if (!partial) return;
   if constexpr (kRows > 1) {   // its rows' sums, in their order
-    float *mine = sums + (threadIdx.x / LANES) * (LANES * NV * 8);
+    float *mine = sums + L::row() * (LANES * NV * 8);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int q = 0; q < 8; ++q) mine[(t + j * LANES) * 8 + q] = sg[j][q];
     __syncthreads();
-    for (int c = threadIdx.x; c < n; c += kThreads) {
+    for (int c = threadIdx.x; c < n; c += 256) {
       float v = sums[c];
       for (int i = 1; i < kRows; ++i) v += sums[i * (LANES * NV * 8) + c];
       partial[int64_t(blockIdx.x) * n + c] = v;
@@ -298,8 +262,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_grad_kernel(dip
   } else {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (t + j * LANES) * 8;
-      if (c < n) store8(partial + int64_t(blockIdx.x) * n + c, n - c, sg[j]);
+      const int c = (t + j * lanes) * 8;
+      if (c < n) put8(partial + int64_t(blockIdx.x) * n + c, n - c, sg[j]);
     }
   }
 }
@@ -307,21 +271,21 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_grad_kernel(dip
 // Few rows: dx by workgroups of kRows rows, and dgamma beside them by workgroups of 64
 // columns that read the rows again, out of the caches: one launch, no workspace.
 template <class T, class G, int LANES, int NV>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel(dip_rms_norm_grad_args a, int row_blocks) {
-  constexpr int kThreads = LANES < 256 ? 256 : LANES, kRows = kThreads / LANES;
-  __shared__ float s[2 * (LANES > 64 ? LANES / 64 : 1)];
-  __shared__ float sums[kThreads / 8][64 + 2];
+__global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_few_grad_kernel(dip_rms_norm_grad_args a, int row_blocks) {
+  typedef Lanes<LANES> L;
+  __shared__ float s[L::kSums];
+  __shared__ float sums[L::kMost / 8][64 + 2];
   const int n = int(a.c);
   if (int(blockIdx.x) < row_blocks) {
     int turn = 0;
-    const int t = threadIdx.x % LANES;
-    const int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+    const int t = L::mine(), lanes = L::count();
+    const int64_t row = int64_t(blockIdx.x) * L::kRows + L::row();
     if (row >= a.m) return;   // all lanes of a row
     const float rstd = a.rstd[row];
     Held<T> x[NV], d[NV], along[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (t + j * LANES) * 8;
+      const int c = (t + j * lanes) * 8;
       x[j].get(static_cast<const T *>(a.total) + row * a.ldt, c, n);
       d[j].get(static_cast<const T *>(a.dy) + row * a.ldy, c, n);
       if (a.dtotal) along[j].get(static_cast<const T *>(a.dtotal) + row * a.lddt, c, n);
@@ -330,9 +294,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float g[8];
-      gamma8<T>(a.gamma, (t + j * LANES) * 8, n, g);
-      x[j].to(xh[j]);
-      d[j].to(h[j]);
+      gamma8<T>(a.gamma, (t + j * lanes) * 8, n, g);
+      const int by = Held<T>::moved((t + j * lanes) * 8, n);
+      x[j].to(by, xh[j]);
+      d[j].to(by, h[j]);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         xh[j][q] *= rstd;
@@ -340,30 +305,31 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel
         dot += h[j][q] * xh[j][q];
       }
     }
-    dot = lanes_sum<LANES>(dot, s, turn) / float(n);
+    dot = L::sum(dot, s, turn) / float(n);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (t + j * LANES) * 8;
+      const int c = (t + j * lanes) * 8;
       float v[8] = {};
-      if (a.dtotal) along[j].to(v);
+      if (a.dtotal) along[j].to(Held<T>::moved(c, n), v);
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[q] += rstd * (h[j][q] - xh[j][q] * dot);
-      if (c < n) store8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, v);
+      if (c < n) put8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, v);
     }
     return;
   }
   const int c0 = (int(blockIdx.x) - row_blocks) * 64, c = c0 + int(threadIdx.x % 8) * 8, ty = threadIdx.x / 8;
   float sum[8] = {};
   if (c < n) {
-    // rows ty, ty + kThreads / 8, ..: four at a time, their loads first
+    // rows ty, ty + step, ..: four at a time, their loads first
     const T *x = static_cast<const T *>(a.total), *dy = static_cast<const T *>(a.dy);
-    constexpr int kStep = kThreads / 8;
-    for (int64_t row = ty; row < a.m; row += 4 * kStep) {
+    const int step = int(blockDim.x) / 8;
+    const int by = Held<T>::moved(c, n);
+    for (int64_t row = ty; row < a.m; row += 4 * step) {
       Held<T> p[4], q[4];
       float r[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int64_t at = row + u * kStep;
+        const int64_t at = row + u * step;
         r[u] = 0.f;
         if (at < a.m) {
           r[u] = a.rstd[at];
@@ -376,8 +342,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         float v[8], w[8];
-        p[u].to(v);
-        q[u].to(w);
+        p[u].to(by, v);
+        q[u].to(by, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += w[i] * (v[i] * r[u]);
       }
@@ -389,7 +355,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel
   if (threadIdx.x < 64 && c0 + int(threadIdx.x) < n) {
     float v = 0.f;
 #pragma unroll 8
-    for (int i = 0; i < kThreads / 8; ++i) v += sums[i][threadIdx.x];
+    for (int i = 0; i < int(blockDim.x) / 8; ++i) v += sums[i][threadIdx.x];
     G *out = static_cast<G *>(a.dgamma) + c0 + threadIdx.x;
     if (a.accumulate) v += float(*out);
     *out = G(v);
@@ -399,7 +365,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_few_grad_kernel
 // Rows of any length: dx by a workgroup that goes over its row twice.
 template <class T>
 __global__ __launch_bounds__(1024) void rms_long_grad_kernel(dip_rms_norm_grad_args a, int64_t row0) {
-  __shared__ float s[2 * 16];
+  __shared__ float s[Lanes<0>::kSums];
   int turn = 0;
   const int t = threadIdx.x, n = int(a.c);
   const int64_t row = row0 + blockIdx.x;
@@ -420,14 +386,14 @@ __global__ __launch_bounds__(1024) void rms_long_grad_kernel(dip_rms_norm_grad_a
 #pragma unroll
     for (int q = 0; q < 8; ++q) dot += h[q] * xh[q];
   }
-  dot = lanes_sum<1024>(dot, s, turn) / float(n);
+  dot = Lanes<0>::sum(dot, s, turn) / float(n);
   for (int c = t * 8; c < n; c += 1024 * 8) {
     float xh[8], h[8], along[8] = {};
     both(c, xh, h);
     if (a.dtotal) load8(static_cast<const T *>(a.dtotal) + row * a.lddt + c, n - c, along);
 #pragma unroll
     for (int q = 0; q < 8; ++q) h[q] = along[q] + rstd * (h[q] - xh[q] * dot);
-    store8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, h);
+    put8(static_cast<T *>(a.dx) + row * a.lddx + c, n - c, h);
   }
 }
 
@@ -465,41 +431,47 @@ __global__ __launch_bounds__(256) void rms_no_columns_kernel(int64_t n, float r,
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) rstd[i] = r;
 }
 
-// f(lanes, vectors) for a row of c columns that registers hold.  Up to 4096 columns the
-// gradient, which has more to hold, takes 512 threads of one vector (65,536 x 3584 bf16
-// 318 us, 256 threads of two 325).
-template <bool GRAD, class F>
-void shape(int64_t c, F &&f) {
-  const auto i = [](auto v) { return v; };
+// How a row of c columns that registers hold is shared out: lanes of a wave (0: the
+// workgroup), vectors a thread, threads a workgroup.
+struct Shape {
+  int lanes, vectors, threads;
+  int rows() const { return lanes ? 256 / lanes : 1; }
+};
+Shape shape_of(int64_t c, int vectors) {
+  const int v = int((c + 7) / 8);
+  int lanes = 4;
+  while (lanes < v) lanes *= 2;
+  if (lanes <= 64) return Shape{lanes, 1, 256};
+  return Shape{0, vectors, (v + 64 * vectors - 1) / (64 * vectors) * 64};
+}
+// f(LANES, NV)
+template <class F>
+void with(const Shape &s, F &&f) {
   using std::integral_constant;
-#define DIP_SHAPE(LANES, NV) \
-  if (c <= LANES * NV * 8) return f(i(integral_constant<int, LANES>{}), i(integral_constant<int, NV>{}))
-  DIP_SHAPE(4, 1);
-  DIP_SHAPE(8, 1);
-  DIP_SHAPE(16, 1);
-  DIP_SHAPE(32, 1);
-  DIP_SHAPE(64, 1);
-  DIP_SHAPE(64, 2);
-  DIP_SHAPE(256, 1);
-  if constexpr (GRAD) {
-    DIP_SHAPE(512, 1);
-  } else {
-    DIP_SHAPE(256, 2);
+  const integral_constant<int, 1> one;
+  switch (s.lanes) {
+    case 4: return f(integral_constant<int, 4>{}, one);
+    case 8: return f(integral_constant<int, 8>{}, one);
+    case 16: return f(integral_constant<int, 16>{}, one);
+    case 32: return f(integral_constant<int, 32>{}, one);
+    case 64: return f(integral_constant<int, 64>{}, one);
+    default:
+      if (s.vectors == 1) f(integral_constant<int, 0>{}, one);
+      else f(integral_constant<int, 0>{}, integral_constant<int, 2>{});
   }
-  DIP_SHAPE(512, 2);
-  DIP_SHAPE(1024, 2);
-#undef DIP_SHAPE
 }
-template <bool GRAD>
-int lanes_of(int64_t c) {
-  int lanes = 1024;
-  shape<GRAD>(c, [&](auto l, auto) { lanes = l; });
-  return lanes;
-}
+// one vector a thread as far as a workgroup goes: 2^26 elements, two would take, us, bf16
+// 4096 columns 95 (93), float32 199 (186); gradient 3584 columns 325 (318)
+Shape row_shape(int64_t c) { return shape_of(c, c <= kAheadMost ? 1 : 2); }
 
-// Rows up to which dgamma is summed beside dx
-constexpr int64_t kFewRows = 256;
-bool few_rows(const dip_rms_norm_grad_args &a) { return a.m <= kFewRows && a.c <= kGradHeldMost && a.dx && a.dgamma; }
+// Bytes of a column up to which dgamma is summed beside dx in one launch: 768 rows of
+// 2-byte types, 384 of float32.  In two launches a call takes 12 us and more, host
+// included; in one 7, and at bf16 1024 rows of 512, 4096 and 8192 columns 7.8, 12.2 and
+// 20.5 (two: 12.3, 12.6, 17.5), float32 600 of 1024 and 2048 13.7 and 18.8 (12.2, 13).
+constexpr int64_t kFewBytes = 1536;
+bool few_rows(const dip_rms_norm_grad_args &a) {
+  return a.m * (a.dtype == DIP_F32 ? 4 : 2) <= kFewBytes && a.c <= kHeldMost && a.dgamma;
+}
 
 struct GradPlan {
   int64_t blocks = 1, chunk = 0;   // workgroups that each leave a row of partial sums; rows a chunk (long rows)
@@ -507,15 +479,19 @@ struct GradPlan {
 };
 GradPlan grad_plan(const dip_rms_norm_grad_args &a) {
   GradPlan p;
-  if (a.c > kGradHeldMost) {
+  if (a.c > kHeldMost) {
     const int64_t cols = (a.c + 255) / 256;
     p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + 15) / 16, 2048 / cols));
     p.chunk = (a.m + p.blocks - 1) / p.blocks;
   } else {
-    const int lanes = lanes_of<true>(a.c), rows = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
-    // eight waves a CU: more keep no more loads on their way, leave more sums, and run
-    // into each other (65,536 x 3584 bf16: 256 workgroups of 512 318 us, 512 332, 1024 357)
-    p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + rows - 1) / rows, std::max(1, 512 / threads) * 256));
+    // As many workgroups as have about 30 KB a CU on their way, the next rows not counted:
+    // more leave more sums and run into each other (2^26 elements bf16, us by KB a CU:
+    // 264 columns 12.7 144, 25 118; 512 24.6 101, 49 109; 2051 12.3 160, 25 139, 37 131;
+    // 65,536 x 3584 21.5 318, 43 332, 86 357).
+    const Shape h = row_shape(a.c);
+    const int64_t bytes = h.rows() * a.c * (a.dtype == DIP_F32 ? 4 : 2) * (a.dtotal && a.dx ? 3 : 2);
+    const int64_t a_cu = std::max<int64_t>(1, (30720 + bytes / 2) / bytes);
+    p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + h.rows() - 1) / h.rows(), std::min<int64_t>(a_cu, 2048 / h.threads) * 256));
   }
   p.bytes = a.dgamma && !few_rows(a) ? up16(p.blocks * a.c * 4) : 0;
   return p;
@@ -525,7 +501,7 @@ template <class T, bool PACK>
 hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
   const Packed p = make_packed(a.packed);
   // a launch has fewer than 2^32 threads
-  const int64_t most = (int64_t(1) << 31) / (a.c > kHeldMost ? 1024 : lanes_of<false>(a.c));
+  const int64_t most = (int64_t(1) << 31) / 1024;
   for (int64_t row0 = 0; row0 < a.m; row0 += most) {
     dip_rms_norm_args b = a;
     b.m = std::min(a.m, row0 + most);
@@ -533,10 +509,10 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
     if (a.c > kHeldMost) {
       rms_long_kernel<T, PACK><<<dim3(uint32_t(rows)), dim3(1024), 0, st>>>(b, row0, p);
     } else {
-      shape<false>(a.c, [&](auto l, auto v) {
-        constexpr int kLanes = decltype(l)::value, kThreads = kLanes < 256 ? 256 : kLanes, kRows = kThreads / kLanes;
-        rms_rows_kernel<T, kLanes, decltype(v)::value, PACK>
-            <<<dim3(uint32_t((rows + kRows - 1) / kRows)), dim3(kThreads), 0, st>>>(b, row0, p);
+      const Shape h = row_shape(a.c);
+      with(h, [&](auto l, auto v) {
+        rms_rows_kernel<T, decltype(l)::value, decltype(v)::value, PACK>
+            <<<dim3(uint32_t((rows + h.rows() - 1) / h.rows())), dim3(h.threads), 0, st>>>(b, row0, p);
       });
     }
     const hipError_t e = hipGetLastError();
@@ -548,20 +524,19 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
 template <class T>
 hipError_t backward(const dip_rms_norm_grad_args &a, hipStream_t st) {
   if (few_rows(a)) {
-    shape<true>(a.c, [&](auto l, auto v) {
-      constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value, kThreads = kLanes < 256 ? 256 : kLanes;
-      if constexpr (kLanes * kNV * 8 <= kGradHeldMost) {
-        const int rows = int((a.m + kThreads / kLanes - 1) / (kThreads / kLanes));
-        const dim3 grid(uint32_t(rows + (a.c + 63) / 64));
-        if (a.accumulate) rms_few_grad_kernel<T, float, kLanes, kNV><<<grid, dim3(kThreads), 0, st>>>(a, rows);
-        else rms_few_grad_kernel<T, T, kLanes, kNV><<<grid, dim3(kThreads), 0, st>>>(a, rows);
-      }
+    const Shape h = row_shape(a.c);
+    with(h, [&](auto l, auto v) {
+      constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value;
+      const int rows = a.dx ? int((a.m + h.rows() - 1) / h.rows()) : 0;
+      const dim3 grid(uint32_t(rows + (a.c + 63) / 64));
+      if (a.accumulate) rms_few_grad_kernel<T, float, kLanes, kNV><<<grid, dim3(h.threads), 0, st>>>(a, rows);
+      else rms_few_grad_kernel<T, T, kLanes, kNV><<<grid, dim3(h.threads), 0, st>>>(a, rows);
     });
     return hipGetLastError();
   }
   const GradPlan p = grad_plan(a);
   float *partial = a.dgamma ? static_cast<float *>(a.workspace) : nullptr;
-  if (a.c > kGradHeldMost) {
+  if (a.c > kHeldMost) {
     const int64_t most = int64_t(1) << 21;
     for (int64_t row0 = 0; a.dx && row0 < a.m; row0 += most) {
       rms_long_grad_kernel<T><<<dim3(uint32_t(std::min(most, a.m - row0))), dim3(1024), 0, st>>>(a, row0);
@@ -572,10 +547,10 @@ hipError_t backward(const dip_rms_norm_grad_args &a, hipStream_t st) {
       rms_long_dgamma_kernel<T>
           <<<dim3(uint32_t((a.c + 255) / 256), uint32_t(p.blocks)), dim3(256), 0, st>>>(a, p.chunk, partial);
   } else {
-    shape<true>(a.c, [&](auto l, auto v) {
-      constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value, kThreads = kLanes < 256 ? 256 : kLanes;
-      if constexpr (kLanes * kNV * 8 <= kGradHeldMost)
-        rms_grad_kernel<T, kLanes, kNV><<<dim3(uint32_t(p.blocks)), dim3(kThreads), 0, st>>>(a, partial);
+    const Shape h = row_shape(a.c);
+    with(h, [&](auto l, auto v) {
+      rms_grad_kernel<T, decltype(l)::value, decltype(v)::value>
+          <<<dim3(uint32_t(p.blocks)), dim3(h.threads), 0, st>>>(a, partial);
     });
   }
   const hipError_t e = hipGetLastError();

@@ -14,7 +14,7 @@
 namespace dipops {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;   // at most
 
 __device__ __forceinline__ double position(const dip_rotary_args &a, int64_t at) {
   switch (a.pos_type) {
@@ -64,10 +64,11 @@ template <class T>
 struct Item {
   const T *p;
   T *o;
-  uint32_t v, n;   // vector of the head, token of the workgroup
-  __device__ __forceinline__ Item(const dip_rotary_args &a, const Shares &sh, uint32_t i, int64_t i0, int h0, int heads) {
+  uint32_t first, n;   // first pair, token of the workgroup
+  __device__ __forceinline__ Item(const dip_rotary_args &a, const Shares &sh, int V, uint32_t i, int64_t i0, int h0,
+                                  int heads) {
     const uint32_t x = sh.vectors(i);
-    v = i - x * sh.vectors.by;
+    first = min((i - x * sh.vectors.by) * V, uint32_t(a.pairs - V));
     n = heads == sh.heads ? sh.in_head(x) : x / uint32_t(heads);
     const int h = int(x - n * uint32_t(heads)) + h0;
     const int64_t token = i0 + n;
@@ -80,24 +81,24 @@ struct Item {
   }
 };
 
-// V pairs a thread.
+// V pairs a thread; a head's last vector ends with its pairs and has some of the one
+// before, which come out the same.  All loads are before the barrier and all stores
+// behind it, and a head is one workgroup's: outputs may be the inputs.
 template <class T, int V, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int64_t token0, Shares sh) {
   extern __shared__ float2 table[];   // [tokens][pairs]: cosine, sine
   const int64_t i0 = token0 + int64_t(blockIdx.x) * sh.tokens;
   const int tokens = int(min(int64_t(sh.tokens), a.t - i0)), all = a.heads + a.keys;
   const int h0 = int(blockIdx.y) * sh.heads, heads = min(sh.heads, all - h0);
-  const uint32_t items = uint32_t(tokens) * uint32_t(heads) * sh.vectors.by;
-  const int step = INTERLEAVED ? V : a.pairs;   // from an item's first vector to its second
+  const bool on = threadIdx.x < uint32_t(tokens) * uint32_t(heads) * sh.vectors.by;
+  const Item<T> it(a, sh, V, on ? threadIdx.x : 0, i0, h0, heads);
+  const int at = int(it.first) * (INTERLEAVED ? 2 : 1), step = INTERLEAVED ? V : a.pairs;
   float u[V], w[V];
-  auto fetch = [&](const Item<T> &it) __attribute__((always_inline)) {
-    const T *p = it.p + int(it.v) * V * (INTERLEAVED ? 2 : 1);
-    load<T, V>(p, u);
-    load<T, V>(p + step, w);
-  };
-  uint32_t i = threadIdx.x;
-  if (i < items) fetch(Item<T>(a, sh, i, i0, h0, heads));   // on its way while the table is made
-  for (int j = threadIdx.x; j < tokens * a.pairs; j += kThreads) {
+  if (on) {   // on their way while the table is made
+    load<T, V>(it.p + at, u);
+    load<T, V>(it.p + at + step, w);
+  }
+  for (int j = threadIdx.x; j < tokens * a.pairs; j += blockDim.x) {
     const int n = j / a.pairs, pair = j - n * a.pairs, axis = a.axis[pair];
     float2 cs = {1.f, 0.f};
     if (axis >= 0 && axis < a.axes) {
@@ -109,33 +110,28 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int
     table[j] = cs;
   }
   __syncthreads();
-  while (i < items) {
-    const Item<T> it(a, sh, i, i0, h0, heads);
-    const float2 *cs = table + it.n * a.pairs + it.v * V;
-    float ou[V], ow[V];
-    if constexpr (INTERLEAVED && V > 1) {
+  if (!on) return;
+  const float2 *cs = table + it.n * a.pairs + it.first;
+  float ou[V], ow[V];
+  if constexpr (INTERLEAVED && V > 1) {
 #pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        const float2 c = cs[j], d = cs[V / 2 + j];
-        ou[2 * j] = u[2 * j] * c.x - u[2 * j + 1] * c.y;
-        ou[2 * j + 1] = u[2 * j] * c.y + u[2 * j + 1] * c.x;
-        ow[2 * j] = w[2 * j] * d.x - w[2 * j + 1] * d.y;
-        ow[2 * j + 1] = w[2 * j] * d.y + w[2 * j + 1] * d.x;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float2 c = cs[j];
-        ou[j] = u[j] * c.x - w[j] * c.y;
-        ow[j] = u[j] * c.y + w[j] * c.x;
-      }
+    for (int j = 0; j < V / 2; ++j) {
+      const float2 c = cs[j], d = cs[V / 2 + j];
+      ou[2 * j] = u[2 * j] * c.x - u[2 * j + 1] * c.y;
+      ou[2 * j + 1] = u[2 * j] * c.y + u[2 * j + 1] * c.x;
+      ow[2 * j] = w[2 * j] * d.x - w[2 * j + 1] * d.y;
+      ow[2 * j + 1] = w[2 * j] * d.y + w[2 * j + 1] * d.x;
     }
-    T *o = it.o + int(it.v) * V * (INTERLEAVED ? 2 : 1);
-    store<T, V>(o, ou);
-    store<T, V>(o + step, ow);
-    i += kThreads;
-    if (i < items) fetch(Item<T>(a, sh, i, i0, h0, heads));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float2 c = cs[j];
+      ou[j] = u[j] * c.x - w[j] * c.y;
+      ow[j] = u[j] * c.y + w[j] * c.x;
+    }
   }
+  store<T, V>(it.o + at, ou);
+  store<T, V>(it.o + at + step, ow);
 }
 
 // Elements 2 pairs .. dim - 1 of every head, where the output is not the input.
@@ -157,24 +153,25 @@ template <class T>
 hipError_t rotary(const dip_rotary_args &a, hipStream_t st) {
   const int all = a.heads + a.keys;
   if (a.pairs > 0) {
-    const int V = a.pairs % 8 == 0 ? 8 : a.pairs % 4 == 0 ? 4 : a.pairs % 2 == 0 ? 2 : 1;
-    const int vectors = a.pairs / V;
-    // One item a thread: as many tokens as that takes, with tables of up to 2048 pairs, or
-    // even shares of one token's heads (65,536 x 28 heads of 128, bf16: one token 153 us,
-    // 6.1 TB/s, two 166, four 171, sixteen 186: a workgroup that loops waits for each
-    // round's loads).
+    const int V = a.pairs >= 8 ? 8 : a.pairs >= 4 ? 4 : a.pairs >= 2 ? 2 : 1;
+    const int vectors = (a.pairs + V - 1) / V;   // at most 128
+    // One item a thread: as many tokens as 256 threads take, with tables of up to 2048
+    // pairs; or one token by a workgroup of its items, in even shares where they are many
+    // (65,536 x 28 heads of 128, bf16: one token 153 us, 6.1 TB/s, two 166, four 171,
+    // sixteen 186: a workgroup that loops waits for each round's loads).
     Shares sh{1, all, Divide(uint32_t(vectors)), Divide(1)};
     const int64_t an = int64_t(all) * vectors;
-    if (an <= kThreads) {
-      sh.tokens = int32_t(std::max<int64_t>(1, std::min<int64_t>(kThreads / an, 2048 / a.pairs)));
+    if (an <= 256) {
+      sh.tokens = int32_t(std::max<int64_t>(1, std::min<int64_t>(256 / an, 2048 / a.pairs)));
     } else {
       const int64_t parts = std::min<int64_t>((an + kThreads - 1) / kThreads, 65535);
-      sh.heads = int32_t((all + parts - 1) / parts);
+      sh.heads = int32_t(std::min<int64_t>((all + parts - 1) / parts, kThreads / vectors));
     }
     sh.in_head = Divide(uint32_t(sh.heads));
     const uint32_t parts = uint32_t((all + sh.heads - 1) / sh.heads);
+    const int threads = (sh.tokens * sh.heads * vectors + 63) / 64 * 64;
     // a launch has fewer than 2^32 threads
-    const int64_t blocks = std::max<int64_t>(1, ((int64_t(1) << 31) / kThreads) / parts), most = blocks * sh.tokens;
+    const int64_t blocks = std::max<int64_t>(1, ((int64_t(1) << 31) / threads) / parts), most = blocks * sh.tokens;
     for (int64_t token0 = 0; token0 < a.t; token0 += most) {
       dip_rotary_args b = a;
       b.t = std::min(a.t, token0 + most);
@@ -182,8 +179,8 @@ hipError_t rotary(const dip_rotary_args &a, hipStream_t st) {
       const size_t lds = size_t(sh.tokens) * a.pairs * sizeof(float2);
       auto go = [&](auto v) {
         constexpr int kV = decltype(v)::value;
-        if (a.interleaved) rotary_kernel<T, kV, true><<<grid, dim3(kThreads), lds, st>>>(b, token0, sh);
-        else rotary_kernel<T, kV, false><<<grid, dim3(kThreads), lds, st>>>(b, token0, sh);
+        if (a.interleaved) rotary_kernel<T, kV, true><<<grid, dim3(threads), lds, st>>>(b, token0, sh);
+        else rotary_kernel<T, kV, false><<<grid, dim3(threads), lds, st>>>(b, token0, sh);
       };
       if (V == 8) go(std::integral_constant<int, 8>{});
       else if (V == 4) go(std::integral_constant<int, 4>{});

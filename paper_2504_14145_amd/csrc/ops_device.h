@@ -108,6 +108,87 @@ __device__ __forceinline__ void store8(T *p, int left, const float (&v)[8]) {
   }
 }
 
+// ------------------------------------------------------------ ends of rows
+
+// Columns c .. c + 7 of a row of n, zeros beyond it.  Where the row ends inside them the
+// eight that end with it are read, and moved into place when they are used: all lanes
+// read whole vectors (element by element the last lane costs a chain of loads), and no
+// lane waits for its loads before it has asked for all of them.
+template <class T>
+struct Held {
+  static constexpr int kWords = sizeof(T) * 2;   // 32-bit words of eight
+  typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
+  typedef Words WordsAny __attribute__((aligned(sizeof(T))));
+  Words t;
+  __device__ __forceinline__ void get(const T *row, int c, int n) {
+    if (n >= 8) {
+      t = *reinterpret_cast<const WordsAny *>(row + min(c, n - 8));
+    } else {
+      float v[8];
+      load8(row, n, v);
+      T e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = T(v[i]);   // exact
+      t = __builtin_bit_cast(Words, e);
+    }
+  }
+  // by: elements to move down, 8 and more for a vector beyond the row
+  static __device__ __forceinline__ int moved(int c, int n) { return n >= 8 ? max(c - (n - 8), 0) : c; }
+  __device__ __forceinline__ Words words(int by) const {
+    Words w = t;
+    if (by) {
+      if constexpr (sizeof(T) == 2) {
+        if (by & 1) {
+#pragma unroll
+          for (int i = 0; i < kWords; ++i) w[i] = w[i] >> 16 | (i + 1 < kWords ? w[i + 1] << 16 : 0u);
+        }
+      }
+      constexpr int per = sizeof(T) == 2 ? 2 : 1;   // elements a word
+#pragma unroll
+      for (int d = 1; d < kWords; d *= 2) {
+        if (by / per & d) {
+#pragma unroll
+          for (int i = 0; i < kWords; ++i) w[i] = i + d < kWords ? w[i + d] : 0u;
+        }
+      }
+      if (by >= 8) w = Words(0);
+    }
+    return w;
+  }
+  __device__ __forceinline__ void to(int by, float (&v)[8]) const {
+    struct Elements {
+      T e[8];
+    };
+    const Elements e = __builtin_bit_cast(Elements, words(by));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = float(e.e[i]);
+  }
+};
+
+// Stores `left` of eight columns, at a row's end four, two and one at once.
+template <class T>
+__device__ __forceinline__ void put8(T *p, int left, const float (&v)[8]) {
+  if (left >= 8) return store8(p, 8, v);
+  float w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = v[i];
+  if (left & 4) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef T4 T4Any __attribute__((aligned(sizeof(T))));
+    *reinterpret_cast<T4Any *>(p) = T4{T(w[0]), T(w[1]), T(w[2]), T(w[3])};
+    p += 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = w[i + 4];
+  }
+  if (left & 2) {
+    p[0] = T(w[0]);
+    p[1] = T(w[1]);
+    p += 2;
+    w[0] = w[2];
+  }
+  if (left & 1) p[0] = T(w[0]);
+}
+
 // ------------------------------------------------------------ activations
 
 // 1 / (1 + 2^t) with the hardware's exponential and reciprocal: within 1e-6 of
@@ -220,19 +301,32 @@ __device__ __forceinline__ u32x2 round8bits(uint32_t byte, const float (&v)[8]) 
 __device__ __forceinline__ void store8bits(uint8_t *p, int left, u32x2 r) {
   if (left >= 8) {
     *reinterpret_cast<u32x2_any *>(p) = r;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = uint8_t(r[i / 4] >> (8 * (i % 4)));
+    return;
   }
+  uint32_t w = r[0];
+  if (left & 4) {
+    typedef uint32_t u32_any __attribute__((aligned(1)));
+    *reinterpret_cast<u32_any *>(p) = w;
+    p += 4;
+    w = r[1];
+  }
+  if (left & 2) {
+    p[0] = uint8_t(w);
+    p[1] = uint8_t(w >> 8);
+    p += 2;
+    w >>= 16;
+  }
+  if (left & 1) p[0] = uint8_t(w);
 }
-__device__ __forceinline__ u32x2 load8bits(const uint8_t *p, int left) {
-  if (left >= 8) return *reinterpret_cast<const u32x2_any *>(p);
-  u32x2 r = {0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < left) r[i / 4] |= uint32_t(p[i]) << (8 * (i % 4));
-  return r;
+// Columns c .. c + 7, c < n, of a row of n; as Held: moved into place behind the loads.
+__device__ __forceinline__ u32x2 load8bits(const uint8_t *row, int c, int n) {
+  if (n >= 8) return *reinterpret_cast<const u32x2_any *>(row + min(c, n - 8));
+  uint64_t r = 0;
+  for (int i = 0; i < n; ++i) r |= uint64_t(row[i]) << (8 * i);   // c is 0
+  return __builtin_bit_cast(u32x2, r);
+}
+__device__ __forceinline__ void place8bits(int c, int n, u32x2 &r) {
+  if (n >= 8 && c > n - 8) r = __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, r) >> (8 * (c - (n - 8))));
 }
 // Exact for every value and scale.
 __device__ __forceinline__ void from8bits(u32x2 r, float scale, float (&v)[8]) {
@@ -275,13 +369,13 @@ __device__ __forceinline__ float within(float v) {
 }
 // Packs a quad's 32 columns from `col` % 32 == 8 (lane % 4) on, of which the lane has
 // `left`, zeros beyond them; all four lanes are on, one without columns writes nothing.
-__device__ __forceinline__ void pack8_quad(const Packed &p, int64_t row, int64_t col, int left, float (&v)[8]) {
+__device__ __forceinline__ void pack8_quad(const Packed &p, int64_t row, int col, int left, float (&v)[8]) {
   uint32_t most = quad_most(most_of(v));
   if (most >= kInfinity) most = quad_most(finite_most(v));   // the four lanes agree
   if (left <= 0) return;
   const uint32_t byte = scale_byte(most);
   store8bits(p.q + row * p.ld + col, left, round8bits(byte, v));
-  if (col % 32 == 0) p.s[row * p.lds + col / 32] = uint8_t(byte);
+  if ((col & 31) == 0) p.s[row * p.lds + (col >> 5)] = uint8_t(byte);
 }
 
 // ------------------------------------------------------------ dropout
