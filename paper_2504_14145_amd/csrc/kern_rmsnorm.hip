@@ -31,17 +31,18 @@ struct Lanes {
   // Their sum; beyond a wave s holds two sets of the waves' values in turn, so that one
   // barrier a sum is enough.
   static constexpr int kSums = kWide ? 32 : 1;
-  static __device__ __forceinline__ float sum(float v, float *s, int &turn) {
+  template <class F>
+  static __device__ __forceinline__ F sum(F v, F *s, int &turn) {
 #pragma unroll
     for (int d = 1; d < (kWide ? 64 : LANES); d *= 2) v += __shfl_xor(v, d);
     if constexpr (kWide) {
       const int waves = int(blockDim.x) / 64;
       if (waves == 1) return v;
-      float *q = s + turn * 16;
+      F *q = s + turn * 16;
       turn ^= 1;
       if (threadIdx.x % 64 == 0) q[threadIdx.x / 64] = v;
       __syncthreads();
-      v = int(threadIdx.x % 16) < waves ? q[threadIdx.x % 16] : 0.f;
+      v = int(threadIdx.x % 16) < waves ? q[threadIdx.x % 16] : F(0);
 #pragma unroll
       for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
     }
@@ -73,16 +74,17 @@ __device__ __forceinline__ void total8(const Held<T> &x, const Held<T> &r, bool 
 }
 
 // 1 / sqrt(sum / n + eps) and what its rounding left off, by one step of Newton's
-// iteration on the residual: the norm and its 8 bits are then as good as a product of
-// exact factors (the root's rounding would put a whole row off by it).
+// iteration on the residual.  The threads' sums, whose errors average out, are joined in
+// float64: nothing puts a whole row off by more than 2^-28.
 struct Rstd {
   float v, rest;
-  __device__ __forceinline__ Rstd(float sum, int n, float eps) {
-    const float m = sum / float(n) + eps;
+  __device__ __forceinline__ Rstd(double sum, double inv, float eps) {   // inv: 1 / n
+    const double mean = fma(sum, inv, double(eps));
+    const float m = float(mean), low = float(mean - double(m));
     v = 1.f / sqrtf(m);
     const float t = m * v, below = fmaf(m, v, -t);
-    const float off = fmaf(-below, v, fmaf(-t, v, 1.f));   // 1 - m v^2
-    rest = fabsf(off) < 1e-3f ? 0.5f * v * off : 0.f;      // not of an infinity or zero
+    const float off = fmaf(-fmaf(low, v, below), v, fmaf(-t, v, 1.f));   // 1 - mean v^2
+    rest = fabsf(off) < 1e-3f ? 0.5f * v * off : 0.f;                    // not of an infinity or zero
   }
 };
 
@@ -99,14 +101,39 @@ __device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed 
     y[q] = fmaf(t, rstd.v, t * rstd.rest);
   }
   if (a.y && left > 0) put8(static_cast<T *>(a.y) + row * a.ldy + c, left, y);
-  if constexpr (PACK) pack8_quad(p, row, c, left, y);   // zeros beyond the row, or NaN
+  if constexpr (PACK) {
+    // A float32 that ends in nineteen zeros may be the middle of two 8-bit values, on
+    // which rounding has put what lies beside it: one in 2^19.  It goes to its side.
+    constexpr uint32_t kLow = 0x7ffffu;
+    uint32_t low = kLow;
+    if (left >= 8) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) low = min(low, magnitude(y[q]) & kLow);
+    } else if (left > 0) {   // not the zeros beyond the row
+#pragma unroll
+      for (int q = 0; q < 8; ++q) low = q < left ? min(low, magnitude(y[q]) & kLow) : low;
+    }
+    if (low == 0) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float t = v[q] * g[q];
+        const float beside = fmaf(t, rstd.v, -y[q]) + fmaf(t, rstd.rest, fmaf(v[q], g[q], -t) * rstd.v);
+        const uint32_t bits = magnitude(y[q]);
+        if ((bits & kLow) == 0 && bits - 1 < kInfinity - 1 && beside != 0.f) {
+          const bool out = (beside > 0.f) == (y[q] > 0.f);
+          y[q] = copysignf(__builtin_bit_cast(float, bits + (out ? 1u : ~0u)), y[q]);
+        }
+      }
+    }
+    pack8_quad(p, row, c, left, y);   // zeros beyond the row, or NaN
+  }
 }
 
 // NV vectors a thread.
 template <class T, int LANES, int NV, bool PACK>
-__global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_norm_args a, int64_t row0, Packed p) {
+__global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_norm_args a, int64_t row0, double inv, Packed p) {
   typedef Lanes<LANES> L;
-  __shared__ float s[L::kSums];
+  __shared__ double s[L::kSums];
   int turn = 0;
   const int t = L::mine(), lanes = L::count(), n = int(a.c);
   const int64_t row = row0 + int64_t(blockIdx.x) * L::kRows + L::row();
@@ -132,7 +159,7 @@ __global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_n
       if (c < n) put8(static_cast<T *>(a.total) + row * a.ldt + c, n - c, v[j]);
     }
   }
-  const Rstd rstd(L::sum(sum, s, turn), n, a.eps);
+  const Rstd rstd(L::sum(double(sum), s, turn), inv, a.eps);
   if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
 #pragma unroll
   for (int j = 0; j < NV; ++j) write8<T, PACK>(a, p, row, (t + j * lanes) * 8, rstd, v[j]);
@@ -141,8 +168,8 @@ __global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_n
 // Rows of any length: a workgroup goes over its row twice.  Where the sum is stored a
 // thread reads back what it wrote (the residual may be gone: they may be one array).
 template <class T, bool PACK>
-__global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int64_t row0, Packed p) {
-  __shared__ float s[Lanes<0>::kSums];
+__global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int64_t row0, double inv, Packed p) {
+  __shared__ double s[Lanes<0>::kSums];
   int turn = 0;
   const int t = threadIdx.x, n = int(a.c);
   const int64_t row = row0 + blockIdx.x;
@@ -167,7 +194,7 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int
     for (int q = 0; q < 8; ++q) sum += v[q] * v[q];
     if (total) put8(total + c, n - c, v);
   }
-  const Rstd rstd(Lanes<0>::sum(sum, s, turn), n, a.eps);
+  const Rstd rstd(Lanes<0>::sum(double(sum), s, turn), inv, a.eps);
   if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
   for (int c = t * 8; c < (n + 31) / 32 * 32; c += 1024 * 8) {
     float v[8] = {};
@@ -507,12 +534,12 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
     b.m = std::min(a.m, row0 + most);
     const int64_t rows = b.m - row0;
     if (a.c > kHeldMost) {
-      rms_long_kernel<T, PACK><<<dim3(uint32_t(rows)), dim3(1024), 0, st>>>(b, row0, p);
+      rms_long_kernel<T, PACK><<<dim3(uint32_t(rows)), dim3(1024), 0, st>>>(b, row0, 1.0 / double(a.c), p);
     } else {
       const Shape h = row_shape(a.c);
       with(h, [&](auto l, auto v) {
         rms_rows_kernel<T, decltype(l)::value, decltype(v)::value, PACK>
-            <<<dim3(uint32_t((rows + h.rows() - 1) / h.rows())), dim3(h.threads), 0, st>>>(b, row0, p);
+            <<<dim3(uint32_t((rows + h.rows() - 1) / h.rows())), dim3(h.threads), 0, st>>>(b, row0, 1.0 / double(a.c), p);
       });
     }
     const hipError_t e = hipGetLastError();
