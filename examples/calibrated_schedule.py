@@ -2,9 +2,10 @@
 
     python examples/calibrated_schedule.py [--workload 2] [--candidates 4096]
 
-1. runs one layer block of each module's sizes (the MLP without a gate) forward
-   and backward with the stage operators, kept and recomputed, and checks that both
-   give the same gradients;
+1. runs one layer block of each module's sizes (the MLP without a gate; of a language
+   model behind a root-mean-square norm) forward and backward with the stage
+   operators, its activations kept, recomputed and kept in 8 bits, and checks that the
+   first two give the same gradients and how far the third's are from them;
 2. times the operators at the workload's token counts and fits the cost tables'
    coefficients to them (kinds without an operator here keep a factor of 1 on
    the card's nominal rates);
@@ -27,23 +28,28 @@ from paper_2504_14145_amd import calibrate  # noqa: E402
 from paper_2504_14145_amd.stage import Block  # noqa: E402
 from workloads.operators import N_KINDS, SEGMENT_MODELS, operator_table  # noqa: E402
 
+# four significant bits: off by at most 2^-4 of a value, evenly spread within it 2^-4 /
+# sqrt(3), beside the roundings of the bf16 products
+FAR = 2.0 ** -4 / 3 ** 0.5 + 2.0 ** -6
 MI355X = {"flops": 2.5e15, "mem_bw": 8e12, "net_bw": 153e9}
 
 
 def run_block(spec, tokens, tp):
-    block = Block(spec.hidden, spec.ffn, p=0.1, tp=tp)
+    block = Block(spec.hidden, spec.ffn, p=0.1, tp=tp, norm="rms" if spec.gated else "layer")
     x = torch.randn((tokens, spec.hidden), device="cuda").bfloat16()
     dy = torch.randn_like(x)
     grads = []
-    for keep in (True, False):
+    for keep in (True, False, 8):
         for g in block.grads.values():
             g.zero_()
         _, saved = block.forward(x, seed=7, keep=keep)
         dx = block.backward(dy, saved)
         grads.append([dx] + [g.clone() for g in block.grads.values()])
-    same = all(torch.equal(a, b) for a, b in zip(*grads))
+    same = all(torch.equal(a, b) for a, b in zip(*grads[:2]))
     print(f"{spec.name}: {tokens} tokens, recomputed gradients {'equal' if same else 'DIFFER FROM'} the kept ones")
-    return same
+    far = [float((a.float() - b.float()).norm() / a.float().norm()) for a, b in zip(grads[0], grads[2]) if a.any()]
+    print(f"{spec.name}: kept in 8 bits, gradients within {max(far):.1%} of their norm")
+    return same and max(far) < FAR
 
 
 def main():

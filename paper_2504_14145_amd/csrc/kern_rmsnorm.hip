@@ -528,7 +528,8 @@ template <class T, bool PACK>
 hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
   const Packed p = make_packed(a.packed);
   // a launch has fewer than 2^32 threads
-  const int64_t most = (int64_t(1) << 31) / 1024;
+  const Shape h = row_shape(a.c);
+  const int64_t most = (int64_t(1) << 31) / (a.c > kHeldMost ? 1024 : h.threads / h.rows());
   for (int64_t row0 = 0; row0 < a.m; row0 += most) {
     dip_rms_norm_args b = a;
     b.m = std::min(a.m, row0 + most);
@@ -536,7 +537,6 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
     if (a.c > kHeldMost) {
       rms_long_kernel<T, PACK><<<dim3(uint32_t(rows)), dim3(1024), 0, st>>>(b, row0, 1.0 / double(a.c), p);
     } else {
-      const Shape h = row_shape(a.c);
       with(h, [&](auto l, auto v) {
         rms_rows_kernel<T, decltype(l)::value, decltype(v)::value, PACK>
             <<<dim3(uint32_t((rows + h.rows() - 1) / h.rows())), dim3(h.threads), 0, st>>>(b, row0, 1.0 / double(a.c), p);
