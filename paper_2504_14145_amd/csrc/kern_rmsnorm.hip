@@ -218,7 +218,7 @@ __global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_grad_kernel(dip_rms_n
   __shared__ float sums[kRows > 1 ? kRows * LANES * NV * 8 : 1];
   int turn = 0;
   const int t = L::mine(), lanes = L::count(), n = int(a.c);
-  constexpr bool kAhead = NV == 1;
+  constexpr bool kAhead = LANES > 0 || NV == 1;
   float g[kAhead ? NV : 1][8], sg[NV][8] = {};
   if constexpr (kAhead) {
 #pragma unroll
@@ -464,13 +464,23 @@ struct Shape {
   int lanes, vectors, threads;
   int rows() const { return lanes ? 256 / lanes : 1; }
 };
-Shape shape_of(int64_t c, int vectors) {
+// Up to 512 columns as many lanes as a row has vectors, to the next power of two.  Up to
+// 1024 a wave with two vectors a lane (2^26 bf16 elements, us: 515 columns 125, by two
+// waves 143; gradient of 768 103, 112), but for float32's gradient, whose registers
+// leave two waves a SIMD (640 columns 374, by two waves 206).  Beyond that one vector a
+// thread as far as a workgroup goes: two would take, bf16 4096 columns, 95 (93), float32
+// 199 (186); gradient of 65,536 x 3584 325 (318).
+Shape row_shape(int64_t c, bool heavy) {
   const int v = int((c + 7) / 8);
   int lanes = 4;
   while (lanes < v) lanes *= 2;
   if (lanes <= 64) return Shape{lanes, 1, 256};
+  if (v <= 128 && !heavy) return Shape{64, 2, 256};
+  const int vectors = c <= kAheadMost ? 1 : 2;
   return Shape{0, vectors, (v + 64 * vectors - 1) / (64 * vectors) * 64};
 }
+Shape forward_shape(const dip_rms_norm_args &a) { return row_shape(a.c, false); }
+Shape grad_shape(const dip_rms_norm_grad_args &a) { return row_shape(a.c, a.dtype == DIP_F32); }
 // f(LANES, NV)
 template <class F>
 void with(const Shape &s, F &&f) {
@@ -481,16 +491,14 @@ void with(const Shape &s, F &&f) {
     case 8: return f(integral_constant<int, 8>{}, one);
     case 16: return f(integral_constant<int, 16>{}, one);
     case 32: return f(integral_constant<int, 32>{}, one);
-    case 64: return f(integral_constant<int, 64>{}, one);
+    case 64:
+      if (s.vectors == 1) return f(integral_constant<int, 64>{}, one);
+      return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     default:
       if (s.vectors == 1) f(integral_constant<int, 0>{}, one);
       else f(integral_constant<int, 0>{}, integral_constant<int, 2>{});
   }
 }
-// one vector a thread as far as a workgroup goes: 2^26 elements, two would take, us, bf16
-// 4096 columns 95 (93), float32 199 (186); gradient 3584 columns 325 (318)
-Shape row_shape(int64_t c) { return shape_of(c, c <= kAheadMost ? 1 : 2); }
-
 // Bytes of a column up to which dgamma is summed beside dx in one launch: 768 rows of
 // 2-byte types, 384 of float32.  In two launches a call takes 12 us and more, host
 // included; in one 7, and at bf16 1024 rows of 512, 4096 and 8192 columns 7.8, 12.2 and
@@ -515,7 +523,7 @@ GradPlan grad_plan(const dip_rms_norm_grad_args &a) {
     // more leave more sums and run into each other (2^26 elements bf16, us by KB a CU:
     // 264 columns 12.7 144, 25 118; 512 24.6 101, 49 109; 2051 12.3 160, 25 139, 37 131;
     // 65,536 x 3584 21.5 318, 43 332, 86 357).
-    const Shape h = row_shape(a.c);
+    const Shape h = grad_shape(a);
     const int64_t bytes = h.rows() * a.c * (a.dtype == DIP_F32 ? 4 : 2) * (a.dtotal && a.dx ? 3 : 2);
     const int64_t a_cu = std::max<int64_t>(1, (30720 + bytes / 2) / bytes);
     p.blocks = std::max<int64_t>(1, std::min<int64_t>((a.m + h.rows() - 1) / h.rows(), std::min<int64_t>(a_cu, 2048 / h.threads) * 256));
@@ -528,7 +536,7 @@ template <class T, bool PACK>
 hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
   const Packed p = make_packed(a.packed);
   // a launch has fewer than 2^32 threads
-  const Shape h = row_shape(a.c);
+  const Shape h = forward_shape(a);
   const int64_t most = (int64_t(1) << 31) / (a.c > kHeldMost ? 1024 : h.threads / h.rows());
   for (int64_t row0 = 0; row0 < a.m; row0 += most) {
     dip_rms_norm_args b = a;
@@ -551,13 +559,15 @@ hipError_t forward(const dip_rms_norm_args &a, hipStream_t st) {
 template <class T>
 hipError_t backward(const dip_rms_norm_grad_args &a, hipStream_t st) {
   if (few_rows(a)) {
-    const Shape h = row_shape(a.c);
+    const Shape h = grad_shape(a);
     with(h, [&](auto l, auto v) {
       constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value;
-      const int rows = a.dx ? int((a.m + h.rows() - 1) / h.rows()) : 0;
-      const dim3 grid(uint32_t(rows + (a.c + 63) / 64));
-      if (a.accumulate) rms_few_grad_kernel<T, float, kLanes, kNV><<<grid, dim3(h.threads), 0, st>>>(a, rows);
-      else rms_few_grad_kernel<T, T, kLanes, kNV><<<grid, dim3(h.threads), 0, st>>>(a, rows);
+      if constexpr (!(sizeof(T) == 4 && kLanes == 64 && kNV == 2)) {   // not a shape of float32's
+        const int rows = a.dx ? int((a.m + h.rows() - 1) / h.rows()) : 0;
+        const dim3 grid(uint32_t(rows + (a.c + 63) / 64));
+        if (a.accumulate) rms_few_grad_kernel<T, float, kLanes, kNV><<<grid, dim3(h.threads), 0, st>>>(a, rows);
+        else rms_few_grad_kernel<T, T, kLanes, kNV><<<grid, dim3(h.threads), 0, st>>>(a, rows);
+      }
     });
     return hipGetLastError();
   }
@@ -574,10 +584,11 @@ hipError_t backward(const dip_rms_norm_grad_args &a, hipStream_t st) {
       rms_long_dgamma_kernel<T>
           <<<dim3(uint32_t((a.c + 255) / 256), uint32_t(p.blocks)), dim3(256), 0, st>>>(a, p.chunk, partial);
   } else {
-    const Shape h = row_shape(a.c);
+    const Shape h = grad_shape(a);
     with(h, [&](auto l, auto v) {
-      rms_grad_kernel<T, decltype(l)::value, decltype(v)::value>
-          <<<dim3(uint32_t(p.blocks)), dim3(h.threads), 0, st>>>(a, partial);
+      constexpr int kLanes = decltype(l)::value, kNV = decltype(v)::value;
+      if constexpr (!(sizeof(T) == 4 && kLanes == 64 && kNV == 2))   // not a shape of float32's
+        rms_grad_kernel<T, kLanes, kNV><<<dim3(uint32_t(p.blocks)), dim3(h.threads), 0, st>>>(a, partial);
     });
   }
   const hipError_t e = hipGetLastError();

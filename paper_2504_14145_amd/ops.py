@@ -200,6 +200,16 @@ class Packed8:
         p.scales = _empty((m, -(-n // 32)), dtype=_torch.uint8, device=device)
         return p
 
+    @classmethod
+    def _of(cls, x) -> "Packed8":
+        """Room for the device matrix x."""
+        m, n = x.shape
+        p = cls.__new__(cls)
+        p.values = _torch.empty_like(x, dtype=_torch.float8_e4m3fn) if x.is_contiguous() else \
+            x.new_empty((m, n), dtype=_torch.float8_e4m3fn)
+        p.scales = x.new_empty((m, -(-n // 32)), dtype=_torch.uint8)
+        return p
+
     @property
     def shape(self):
         return self.values.shape
@@ -571,7 +581,7 @@ def pack8(x, out=None, stream=None):
     _need(x.dim() == 2, "x is a matrix")
     shape = m, n = x.shape
     if out is None:
-        out = Packed8.empty(m, n, x.device)
+        out = Packed8._of(x)
         args = _pack_packed(out.values.data_ptr(), n, out.scales.data_ptr(), -(-n // 32))
     else:
         args = _pack_packed(*_packed(out, shape, dev, "out"))
@@ -646,7 +656,7 @@ def rms_norm(x, gamma=None, eps=1e-5, residual=None, packed=None, need_out=True,
     else:
         pr = _whole(rstd, (m,), _torch.float32, dev, "rstd")
     if packed is True:
-        packed = Packed8.empty(m, c, x.device)
+        packed = Packed8._of(x)
         pp = packed.values.data_ptr(), c, packed.scales.data_ptr(), -(-c // 32)
     elif packed is False:
         packed = None
