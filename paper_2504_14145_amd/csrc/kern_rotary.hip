@@ -2,10 +2,14 @@
 // token turned by the angles of its positions.
 //
 // Bound by memory, every head read and written once; a token's sines and cosines are
-// as many as one head has pairs and serve all heads.  A workgroup takes a few tokens
-// and a share of their heads, puts the tokens' sines and cosines into LDS (the angle
-// in turns in float64, less its whole turns: far positions lose nothing) and goes over
-// the heads, a vector of pairs a thread.
+// as many as one head has pairs and serve all heads.  A workgroup takes a token or a
+// few, or a share of one token's heads: it asks for all its pairs, a vector a thread,
+// puts the sines and cosines into LDS meanwhile (the angle in turns in float64, less its
+// whole turns: far positions lose nothing), and turns and stores.
+// bf16, 65,536 tokens of 56 heads of 128: 313 to 324 us, 5.9 TB/s; 28 heads of q alone
+// 153, 6.1.  2^26 elements of 16 + 16 heads, us: 128 elements a head 54, 112 57, 72 58,
+// 20 (4 + 4 heads) 66; one head of q and k each 86, sines and cosines then being as many
+// as pairs.
 #include <algorithm>
 #include <type_traits>
 

@@ -341,7 +341,8 @@ __device__ __forceinline__ void from8bits(u32x2 r, float scale, float (&v)[8]) {
   }
 }
 // The same in 16 bits, for scales from 2^-15 to 2^7 in float16, whose values that holds,
-// and from 2^-124 to 2^119 in bfloat16.
+// and from 2^-124 to 2^119 in bfloat16 (float32: up to 2^119).
+__device__ __forceinline__ bool held_by(float, uint32_t byte) { return byte <= 246u; }
 __device__ __forceinline__ bool held_by(_Float16, uint32_t byte) { return byte - 112u <= 22u; }
 __device__ __forceinline__ bool held_by(__bf16, uint32_t byte) { return byte - 3u <= 243u; }
 template <class T>
