@@ -134,7 +134,8 @@ def test_norm_refusals(lib, change, code):
     (dict(dgamma=AT + 2, accumulate=1), dip.E_INVAL), (dict(workspace_bytes=0), dip.E_CAPACITY),
     (dict(workspace=AT + 8), dip.E_INVAL), (dict(dtype=3), dip.E_INVAL), (dict(m=1 << 31), dip.E_RANGE)])
 def test_norm_gradient_refusals(lib, change, code):
-    a = ops._RmsNormGrad(m=4, c=40, dtype=ops.BF16, dy=AT, ldy=40, total=AT, ldt=40, gamma=AT, rstd=AT, dtotal=AT, lddt=40,
+    # more rows than those whose gradient needs no workspace
+    a = ops._RmsNormGrad(m=1000, c=40, dtype=ops.BF16, dy=AT, ldy=40, total=AT, ldt=40, gamma=AT, rstd=AT, dtotal=AT, lddt=40,
                          dx=AT, lddx=40, dgamma=AT, workspace=AT, workspace_bytes=1 << 24)
     for k, v in change.items():
         setattr(a, k, v)
