@@ -767,7 +767,8 @@ def _turn(name, q, positions, frequencies, axis, k, interleaved, out, out_k, inv
                         inverse, *pq, *pk, positions.data_ptr(), positions.stride(0), sa,
                         _whole(frequencies, (pairs,), _torch.float64, dev, "frequencies"),
                         _whole(axis, (pairs,), _torch.int32, dev, "axis"), *po, *pk_out)
-    if not inverse and _recording() and (q.requires_grad or k is not None and k.requires_grad):
+    if not inverse and _recording() and (q.requires_grad or k is not None and k.requires_grad or positions.requires_grad
+                                         or frequencies.requires_grad):
         _cut_off(name)
     _call("dip_rotary", args, dev)
     return out if k is None else (out, out_k)

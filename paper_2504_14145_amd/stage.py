@@ -152,7 +152,7 @@ class Projection:
 
     def _parts(self, qkv):
         """The heads of q, k and v in a product's output."""
-        v = qkv.view(qkv.shape[0], -1, self.dim)
+        v = qkv.view(qkv.shape[0], self.heads + 2 * self.keys, self.dim)
         return v[:, :self.heads], v[:, self.heads:self.heads + self.keys], v[:, self.heads + self.keys:]
 
     def forward(self, x, positions, residual=None, keep=True):

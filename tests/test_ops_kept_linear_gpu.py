@@ -90,7 +90,9 @@ def test_accumulated_gradients(dtype):
     check(130, 150, 77, dtype, grad_type=torch.float32, x_act="silu", seed=5)
 
 
-@pytest.mark.parametrize("m,n,k", [(300, 520, 264), (2000, 1500, 512), (64, 100, 4096), (4100, 2200, 256)])
+# 128 x 128 tiles one and two a CU, split, 256 x 256, 192 x 128
+@pytest.mark.parametrize("m,n,k", [(300, 520, 264), (2000, 1500, 512), (64, 100, 4096), (4100, 2200, 256), (5000, 4096, 64),
+                                   (1152, 3840, 512)])
 def test_the_output_has_the_bits_of_the_call_without(m, n, k):
     """Tiles of every size, whole and split: keeping pre changes nothing else, and what
     is kept is what packing the float32 values would have kept."""
@@ -135,6 +137,34 @@ def test_values_kept_as_nan_and_zeros():
     assert torch.equal(dw.cpu().isnan(), bad)
     assert dx.cpu().isnan().any(1).nonzero().flatten().tolist() == [7]
     assert db.cpu().isnan().nonzero().flatten().tolist() == [9]
+
+
+@pytest.mark.parametrize("m,n,k", [(40, 100, 64), (300, 520, 264), (64, 100, 4096), (2100, 2080, 64), (4100, 2200, 256)])
+def test_sums_that_are_not_finite_stay_alone(m, n, k):
+    """Columns with an infinite or NaN bias, and a row of NaN, in tiles of every size,
+    whole and split: NaN there, and the scales of the 32 columns go by the others."""
+    g = torch.Generator().manual_seed(n)
+    x, w, b = ((torch.randn(s, generator=g) * c).to(BF16) for s, c in (((m, k), 1.0), ((n, k), k ** -0.5), ((n,), 0.5)))
+    off = b.clone()
+    off[5], off[37], off[n - 1] = float("inf"), float("-inf"), float("nan")
+    off[40:45] = float("nan")
+    x[m // 2, 3] = float("nan")
+    pre = ops.Packed8.empty(m, n)
+    y = ops.linear(x.cuda(), w.cuda(), off.cuda(), act="silu", pre=pre)
+    bad = ~torch.isfinite(off)[None, :].expand(m, n).clone()
+    bad[m // 2] = True
+    got = unpack(pre.values, pre.scales)
+    assert torch.equal(got.isnan(), bad)
+    x[m // 2] = 0
+    ref = Linear(x, w, b, None, "silu", None)
+    rows = torch.arange(m) != m // 2
+    # a finite stand-in for the bad columns that no scale goes by
+    q = pre.values.cpu().float()
+    q[bad] = 0
+    z, bound = torch.where(bad, 0.0, ref.z), torch.where(bad, 0.0, ref.z_bound)
+    assert_kept(q[rows].to(F8), pre.scales.cpu()[rows], z[rows], bound[rows], "pre")
+    assert bool((pre.scales.cpu()[m // 2] == 1).all())
+    assert torch.isfinite(y.cpu()[rows][:, torch.isfinite(off)]).all()
 
 
 def test_empty():

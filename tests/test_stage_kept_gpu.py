@@ -164,6 +164,19 @@ def test_projection_gradients(t, h, heads, keys, dim, sections, inter, keep):
         near(block.grads[n], p.grad, n, NEAR[keep])
 
 
+@pytest.mark.parametrize("keep", [True, 8, False])
+def test_a_piece_without_tokens(keep):
+    block, pro = Block(64, 128, act="silu", norm="rms"), Projection(64, 2, 1, 16, (4, 4))
+    x, pos = torch.empty((0, 64), dtype=BF16, device="cuda"), torch.empty((0, 2), dtype=torch.int32, device="cuda")
+    y, saved = block.forward(x, keep=keep)
+    assert y.shape == (0, 64) and block.backward(y, saved).shape == (0, 64)
+    q, k, v, total, saved = pro.forward(x, pos, residual=x, keep=keep)
+    assert q.shape == (0, 2, 16) and k.shape == v.shape == (0, 1, 16)
+    assert pro.backward(q, k, v, saved, dtotal=x).shape == (0, 64)
+    for g in (*block.grads.values(), *pro.grads.values()):
+        assert not g.any()
+
+
 def test_shares_of_a_projection_add_up():
     h, heads, keys, dim, t = 96, 4, 2, 24, 50
     whole = Projection(h, heads, keys, dim, (4, 8), seed=1)
