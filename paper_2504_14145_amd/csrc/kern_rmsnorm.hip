@@ -23,6 +23,55 @@ namespace {
 // fits beside its own, and gamma (1024 threads have 128 registers each).
 constexpr int kHeldMost = 16384, kAheadMost = 8192;
 
+// The sum over LANES consecutive lanes of a wave, the same in all of them: neighbours,
+// pairs, fours and eights within a row of sixteen, then rows and halves, without a way
+// through the LDS.  What a step exchanges is already the same in the group that it
+// comes from, so mirrored lanes serve.
+template <class F>
+__device__ __forceinline__ F exchanged(F v, int step) {
+  constexpr int kWords = sizeof(F) / 4;
+  struct Words {
+    int w[kWords];
+  };
+  Words a = __builtin_bit_cast(Words, v);
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    if (step == 1) a.w[i] = __builtin_amdgcn_mov_dpp(a.w[i], 0xb1, 0xf, 0xf, true);         // lane ^ 1
+    else if (step == 2) a.w[i] = __builtin_amdgcn_mov_dpp(a.w[i], 0x4e, 0xf, 0xf, true);    // lane ^ 2
+    else if (step == 4) a.w[i] = __builtin_amdgcn_mov_dpp(a.w[i], 0x141, 0xf, 0xf, true);   // 7 - lane of eight
+    else a.w[i] = __builtin_amdgcn_mov_dpp(a.w[i], 0x140, 0xf, 0xf, true);                  // 15 - lane of sixteen
+  }
+  return __builtin_bit_cast(F, a);
+}
+// The sum of a value and that 16 (HALVES: 32) lanes away.
+template <bool HALVES, class F>
+__device__ __forceinline__ F swapped_sum(F v) {
+  constexpr int kWords = sizeof(F) / 4;
+  struct Words {
+    uint32_t w[kWords];
+  };
+  Words a = __builtin_bit_cast(Words, v), b = a;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    if constexpr (HALVES) {
+      const auto r = __builtin_amdgcn_permlane32_swap(a.w[i], b.w[i], false, false);
+      a.w[i] = r[0], b.w[i] = r[1];
+    } else {
+      const auto r = __builtin_amdgcn_permlane16_swap(a.w[i], b.w[i], false, false);
+      a.w[i] = r[0], b.w[i] = r[1];
+    }
+  }
+  return __builtin_bit_cast(F, a) + __builtin_bit_cast(F, b);
+}
+template <int LANES, class F>
+__device__ __forceinline__ F lanes_sum(F v) {
+#pragma unroll
+  for (int d = 1; d < (LANES < 16 ? LANES : 16); d *= 2) v += exchanged(v, d);
+  if constexpr (LANES > 16) v = swapped_sum<false>(v);
+  if constexpr (LANES > 32) v = swapped_sum<true>(v);
+  return v;
+}
+
 // A row's threads: LANES of a wave, a power of two from four on, or, LANES 0, the whole
 // workgroup, as many waves as the row fills.
 template <int LANES>
@@ -38,8 +87,7 @@ struct Lanes {
   static constexpr int kSums = kWide ? 32 : 1;
   template <class F>
   static __device__ __forceinline__ F sum(F v, F *s, int &turn) {
-#pragma unroll
-    for (int d = 1; d < (kWide ? 64 : LANES); d *= 2) v += __shfl_xor(v, d);
+    v = lanes_sum<(kWide ? 64 : LANES)>(v);
     if constexpr (kWide) {
       const int waves = int(blockDim.x) / 64;
       if (waves == 1) return v;
@@ -47,9 +95,7 @@ struct Lanes {
       turn ^= 1;
       if (threadIdx.x % 64 == 0) q[threadIdx.x / 64] = v;
       __syncthreads();
-      v = int(threadIdx.x % 16) < waves ? q[threadIdx.x % 16] : F(0);
-#pragma unroll
-      for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
+      v = lanes_sum<16>(int(threadIdx.x % 16) < waves ? q[threadIdx.x % 16] : F(0));
     }
     return v;
   }
