@@ -251,11 +251,12 @@ typedef u32x2 u32x2_any __attribute__((aligned(1)));
 // Magnitudes are compared as integers: infinity and NaN are above all others.
 constexpr uint32_t kInfinity = 0x7f800000u;
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+// By the three-operand maximum, which passes over NaN: those are NaN in 8 bits anyway.
 __device__ __forceinline__ uint32_t most_of(const float (&v)[8]) {
-  uint32_t most = 0;
+  float most = fmaxf(fabsf(v[0]), fabsf(v[1]));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
-  return most;
+  for (int i = 2; i < 8; i += 2) most = fmaxf(fmaxf(most, fabsf(v[i])), fabsf(v[i + 1]));
+  return magnitude(most);
 }
 // Makes what is not finite NaN, and the largest magnitude of the others.
 __device__ __forceinline__ uint32_t finite_most(float (&v)[8]) {
