@@ -233,6 +233,16 @@ int linear_grad(const dip_linear_grad_args *a, const dip_packed8 *x8, int32_t x_
   const void *g = a->dy;
   int64_t ldg = a->ldy;
   float *partial = reinterpret_cast<float *>(ws + p.partial_at);
+  PackJob px, pw;
+  const Operand w = place(a->w, a->dx ? a->n : 0, a->k, a->ldw, true, ws, p.w_at, &pw);
+  Operand x;
+  Restore rx{};
+  if (x8) {
+    x = Operand{p.x_at >= 0 ? ws + p.x_at : nullptr, up8(a->k), true};
+    if (p.x_at >= 0) rx = Restore{make_packed(*x8), a->m, int32_t(a->k), x_act, ws + p.x_at, up8(a->k)};
+  } else {
+    x = place(a->x, a->dw ? a->m : 0, a->k, a->ldx, true, ws, p.x_at, &px);
+  }
   if (p.g_at >= 0 || p.sums_at >= 0) {
     GradIn gi{};
     gi.m = a->m;
@@ -250,23 +260,20 @@ int linear_grad(const dip_linear_grad_args *a, const dip_packed8 *x8, int32_t x_
     }
     gi.row_chunks = p.chunks ? p.chunks : grad_row_chunks(a->m, a->n);
     gi.partial = a->db ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr;
-    OPS_CHECK(hip_code(launch_grad_in(a->dtype, gi, st)));
+    if (rx.m && grad_in_kept_fits(gi, rx, pw)) {
+      OPS_CHECK(hip_code(launch_grad_in_kept(a->dtype, gi, rx, pw, st)));
+      rx.m = 0;
+      pw = PackJob{};
+    } else {
+      OPS_CHECK(hip_code(launch_grad_in(a->dtype, gi, st)));
+    }
   }
   if (a->db && a->n > 0 && !(a->m == 0 && a->accumulate))
     OPS_CHECK(hip_code(launch_sum_rows(SumRows{reinterpret_cast<const float *>(ws + p.sums_at), p.chunks, a->n, a->n,
                                                a->db, nullptr, a->accumulate},
                                        a->grad_dtype, st)));
-  PackJob px, pw;
-  Operand x;
-  if (x8) {
-    x = Operand{p.x_at >= 0 ? ws + p.x_at : nullptr, up8(a->k), true};
-    if (p.x_at >= 0)
-      OPS_CHECK(hip_code(launch_unpack8(a->dtype, a->m, a->k, make_packed(*x8), x_act, ws + p.x_at, up8(a->k),
-                                        up8(a->k), st)));
-  } else {
-    x = place(a->x, a->dw ? a->m : 0, a->k, a->ldx, true, ws, p.x_at, &px);
-  }
-  const Operand w = place(a->w, a->dx ? a->n : 0, a->k, a->ldw, true, ws, p.w_at, &pw);
+  if (rx.m)
+    OPS_CHECK(hip_code(launch_unpack8(a->dtype, rx.m, rx.n, rx.x, rx.act, rx.out, rx.ldo, rx.ldo, st)));
   OPS_CHECK(pack(a->dtype, px, pw, st));
   if (a->dx && a->m > 0 && a->k > 0) {
     Epilogue e{};

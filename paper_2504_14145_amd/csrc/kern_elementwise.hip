@@ -65,13 +65,13 @@ hipError_t dropout_add(int64_t m, int64_t n, const void *x, int64_t ldx, const v
 // rows, sixteen rows at a time, and adds its eight row lanes at the end; the
 // chunks' sums are added in their order by sum_rows_kernel.  65,536 x 2560 with
 // GELU 217 us (4.6 TB/s; the slope's arithmetic is the rest).
+typedef float GradSums[8][256 + 8];
 template <class T, bool KEPT>
-__global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
-  __shared__ float s[8][256 + 8];
+__device__ __forceinline__ void grad_in_block(const GradIn &g, uint32_t bx, uint32_t by, GradSums &s) {
   const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-  const int64_t col = int64_t(blockIdx.x) * 256 + tx * 8;
+  const int64_t col = int64_t(bx) * 256 + tx * 8;
   const int64_t per = (g.m + g.row_chunks - 1) / g.row_chunks;
-  const int64_t r0 = per * blockIdx.y, r1 = min(r0 + per, g.m);
+  const int64_t r0 = per * by, r1 = min(r0 + per, g.m);
   const int left = int(max(int64_t(0), min(int64_t(8), g.n - col)));
   float sum[8] = {};
   if (left > 0) {
@@ -131,12 +131,45 @@ __global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
   for (int j = 0; j < 8; ++j) s[ty][tx * 8 + j] = sum[j];
   __syncthreads();
   const int c = threadIdx.x;
-  const int64_t out = int64_t(blockIdx.x) * 256 + c;
+  const int64_t out = int64_t(bx) * 256 + c;
   if (out < g.n) {
     float v = 0.f;
     for (int i = 0; i < 8; ++i) v += s[i][c];
-    g.partial[int64_t(blockIdx.y) * g.n + out] = v * g.drop.scale;
+    g.partial[int64_t(by) * g.n + out] = v * g.drop.scale;
   }
+}
+template <class T, bool KEPT>
+__global__ __launch_bounds__(kThreads) void grad_in_kernel(GradIn g) {
+  __shared__ GradSums s;
+  grad_in_block<T, KEPT>(g, blockIdx.x, blockIdx.y, s);
+}
+
+// The same beside x restored from 8 bits and w copied where that is needed, in one
+// launch: three passes that do not need each other, of which small ones leave most of the
+// card idle.  Time of a whole backward pass with three launches and with one: 51.4 and
+// 42.6 us at 1201 x 1795 x 1027 fp16, 413 and 409 at 8192 x 4096 x 3584 bf16.
+struct Restoring {
+  Restore x;
+  Divide per;
+  uint32_t items, x_blocks, g_cols, g_blocks;
+};
+template <class T, bool KEPT, bool ACT>
+__global__ __launch_bounds__(kThreads) void grad_in_kept_kernel(GradIn g, Restoring r, PackJob w) {
+  __shared__ GradSums s;
+  uint32_t b = blockIdx.x;
+  if (b < r.g_blocks) {
+    const uint32_t by = b / r.g_cols;
+    return grad_in_block<T, KEPT>(g, b - by * r.g_cols, by, s);
+  }
+  b -= r.g_blocks;
+  if (b < r.x_blocks) {
+    const uint32_t i = b * kThreads + threadIdx.x;
+    if (i >= r.items) return;
+    const uint32_t row = r.per(i);
+    const int col = int(i - row * r.per.by) * 8;
+    return restore8<T, ACT>(r.x.x, row, col, r.x.n, r.x.act, static_cast<T *>(r.x.out) + int64_t(row) * r.x.ldo + col, 8);
+  }
+  pack_item<T>(w, int64_t(b - r.x_blocks) * kThreads + threadIdx.x);
 }
 
 // 64 columns a workgroup, LANES threads a column.
@@ -201,6 +234,33 @@ hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream) {
   auto go = [&](auto kernel) { kernel<<<grid, dim3(kThreads), 0, stream>>>(g); };
   if (dtype == DIP_BF16) g.kept.q ? go(grad_in_kernel<__bf16, true>) : go(grad_in_kernel<__bf16, false>);
   else g.kept.q ? go(grad_in_kernel<_Float16, true>) : go(grad_in_kernel<_Float16, false>);
+  return hipGetLastError();
+}
+
+// Up to 2^22 vectors of x: larger passes fill the card by themselves, and x restored from
+// a large array has too few waves in flight beside the gradient's registers and LDS (k
+// 2560, n 256, gelu of x and of the product: 112.4 us apart and together at 16,384 rows,
+// 244 apart and 262 together at 32,768; 784 and 812 at 131,072 without an activation of x).
+bool grad_in_kept_fits(const GradIn &g, const Restore &x, const PackJob &w) {
+  const int64_t items = x.m * (x.ldo / 8), pack = w.rows * (w.ldo / 8);
+  const int64_t blocks = (items + pack) / kThreads + 2 + (g.n + 255) / 256 * g.row_chunks;
+  return items <= (int64_t(1) << 22) && blocks < kMaxTiles;
+}
+
+hipError_t launch_grad_in_kept(int dtype, const GradIn &g, const Restore &x, const PackJob &w, hipStream_t stream) {
+  const int64_t per = x.ldo / 8, items = x.m * per, pack = w.rows * (w.ldo / 8);
+  Restoring r{x, Divide(uint32_t(per)), uint32_t(items), uint32_t((items + kThreads - 1) / kThreads),
+              uint32_t((g.n + 255) / 256), 0};
+  r.g_blocks = r.g_cols * uint32_t(g.row_chunks);
+  const dim3 grid(r.g_blocks + r.x_blocks + uint32_t((pack + kThreads - 1) / kThreads));
+  auto go = [&](auto kernel) { kernel<<<grid, dim3(kThreads), 0, stream>>>(g, r, w); };
+  auto typed = [&](auto t) {
+    typedef decltype(t) T;
+    if (g.kept.q) x.act != DIP_ACT_NONE ? go(grad_in_kept_kernel<T, true, true>) : go(grad_in_kept_kernel<T, true, false>);
+    else x.act != DIP_ACT_NONE ? go(grad_in_kept_kernel<T, false, true>) : go(grad_in_kept_kernel<T, false, false>);
+  };
+  if (dtype == DIP_BF16) typed(__bf16());
+  else typed(_Float16());
   return hipGetLastError();
 }
 

@@ -643,13 +643,7 @@ template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(PackJob a, PackJob b, uint32_t blocks_a) {
   const bool second = blockIdx.x >= blocks_a;
   const PackJob &j = second ? b : a;
-  const uint32_t per = uint32_t(j.ldo / 8);
-  const int64_t i = int64_t(blockIdx.x - (second ? blocks_a : 0)) * 256 + threadIdx.x;
-  if (i >= j.rows * per) return;
-  const int64_t row = i / per, col = (i - row * per) * 8;
-  float v[8];
-  load8(static_cast<const T *>(j.p) + row * j.ld + col, int(min(int64_t(8), j.cols - col)), v);
-  store8(static_cast<T *>(j.out) + row * j.ldo + col, 8, v);
+  pack_item<T>(j, int64_t(blockIdx.x - (second ? blocks_a : 0)) * 256 + threadIdx.x);
 }
 
 }  // namespace

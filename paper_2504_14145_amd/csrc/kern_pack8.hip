@@ -79,39 +79,7 @@ __global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint3
   const uint32_t in = per(i);
   const int64_t row = int64_t(row0) + in;
   const int col = int(i - in * per.by) * 8;
-  u32x2 bits = {0, 0};
-  uint32_t byte = 127;
-  if (col < n) {
-    bits = load8bits(x.q + row * x.ld, col, n);
-    byte = x.s[row * x.lds + (col >> 5)];
-    place8bits(col, n, bits);
-  }
-  T *out = y + row * ldy + col;
-  if constexpr (!ACT && sizeof(T) == 2) {
-    if (held_by(T(), byte) && fill - col >= 8) {
-      *reinterpret_cast<typename Any8<T>::type *>(out) = from8bits_to<T>(bits, scale_of(byte));
-      return;
-    }
-  }
-  float v[8];
-  from8bits(bits, scale_of(byte), v);
-  if constexpr (ACT) {
-    if (act == DIP_ACT_SILU) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_SILU);
-    } else if (act == DIP_ACT_GELU) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_GELU);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_RELU);
-    }
-  }
-  if (!held_by(T(), byte)) {   // an activation makes nothing larger
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
-  }
-  put8(out, min(8, fill - col), v);   // beyond n act(0) = 0
+  restore8<T, ACT>(x, row, col, n, act, y + row * ldy + col, min(8, fill - col));
 }
 
 // f(items, row0, Divide(per)) over launches of fewer than 2^31 items.

@@ -369,6 +369,43 @@ __device__ __forceinline__ float within(float v) {
                           : __is_same(T, _Float16) ? 65504.f : 3.389531389e38f;   // (2 - 2^-7) 2^127
   return v > kMost ? kMost : v < -kMost ? -kMost : v;
 }
+// Columns col .. col + 7 of act of a row in 8 bits, of which n exist, to `left` columns
+// from out on: zeros beyond n.
+template <class T, bool ACT>
+__device__ __forceinline__ void restore8(const Packed &x, int64_t row, int col, int n, int act, T *out, int left) {
+  u32x2 bits = {0, 0};
+  uint32_t byte = 127;
+  if (col < n) {
+    bits = load8bits(x.q + row * x.ld, col, n);
+    byte = x.s[row * x.lds + (col >> 5)];
+    place8bits(col, n, bits);
+  }
+  if constexpr (!ACT && sizeof(T) == 2) {
+    if (held_by(T(), byte) && left >= 8) {
+      *reinterpret_cast<typename Any8<T>::type *>(out) = from8bits_to<T>(bits, scale_of(byte));
+      return;
+    }
+  }
+  float v[8];
+  from8bits(bits, scale_of(byte), v);
+  if constexpr (ACT) {
+    if (act == DIP_ACT_SILU) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_SILU);
+    } else if (act == DIP_ACT_GELU) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_GELU);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_RELU);
+    }
+  }
+  if (!held_by(T(), byte)) {   // an activation makes nothing larger
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
+  }
+  put8(out, left, v);   // beyond n act(0) = 0
+}
 // Packs a quad's 32 columns from `col` % 32 == 8 (lane % 4) on, of which the lane has
 // `left`, zeros beyond them; all four lanes are on, one without columns writes nothing.
 __device__ __forceinline__ void pack8_quad(const Packed &p, int64_t row, int col, int left, float (&v)[8]) {

@@ -70,6 +70,16 @@ struct PackJob {
   int64_t ldo = 8;
 };
 hipError_t launch_pack(int dtype, const PackJob &a, const PackJob &b, hipStream_t stream);
+// vector i of a job, if it has that many
+template <class T>
+__device__ __forceinline__ void pack_item(const PackJob &j, int64_t i) {
+  const uint32_t per = uint32_t(j.ldo / 8);
+  if (i >= j.rows * per) return;
+  const int64_t row = i / per, col = (i - row * per) * 8;
+  float v[8];
+  load8(static_cast<const T *>(j.p) + row * j.ld + col, int(min(int64_t(8), j.cols - col)), v);
+  store8(static_cast<T *>(j.out) + row * j.ldo + col, 8, v);
+}
 
 // g = D(dy) act'(pre), without the factor of D's kept elements, to out (ld a
 // multiple of 8, padding columns zero; null: not wanted), and its column sums with
@@ -88,6 +98,18 @@ struct GradIn {
 };
 int32_t grad_row_chunks(int64_t m, int64_t n);
 hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream);
+// act of x [m][n] in 8 bits to out (16-byte aligned, ldo a multiple of 8), zeros in
+// columns n .. ldo - 1
+struct Restore {
+  Packed x;
+  int64_t m;
+  int32_t n, act;
+  void *out;
+  int64_t ldo;
+};
+// All three in one launch, where that is faster and has the threads; w may have no rows.
+bool grad_in_kept_fits(const GradIn &g, const Restore &x, const PackJob &w);
+hipError_t launch_grad_in_kept(int dtype, const GradIn &g, const Restore &x, const PackJob &w, hipStream_t stream);
 // out0[j] (+)= the sum over the rows of partial[rows][ld] of column j, and out1[j]
 // of column c + j, j < c, in an order that depends on the sizes alone; either may
 // be null.

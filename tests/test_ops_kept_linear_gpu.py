@@ -126,6 +126,25 @@ def test_one_of_x_and_pre_kept():
     assert none is None and torch.equal(dw, want[1])
 
 
+@pytest.mark.parametrize("dtype", (BF16, F16))
+@pytest.mark.parametrize("m,n,k", [(1, 33, 7), (45, 8, 1), (700, 1030, 803), (2300, 40, 2056), ((1 << 20) + 70, 9, 61)])
+def test_gradients_have_the_bits_of_values_unpacked_before(m, n, k, dtype):
+    """x restored beside the gradient of the activation or apart, w copied or read in
+    place, sums of dy alone: the values and so the products are those of the call on
+    unpacked arrays."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    x8, pre8, w, dy = ops.pack8(normal(m, k)), ops.pack8(normal(m, n)), normal(n, k), normal(m, n)
+    xs, ps = ops.unpack8(x8, dtype), ops.unpack8(pre8, dtype)
+    for act, x_act, drop in (("silu", "none", None), ("gelu", "relu", ops.Dropout(0.2, 9, offset=2, row0=1)), ("none", "relu", None)):
+        x = torch.relu(xs) if x_act == "relu" else xs
+        kw = {"act": act, "dropout": drop}
+        want = ops.linear_backward(dy, x, w, pre=ps if act != "none" else None, **kw)
+        for pre in ((ps, pre8) if act != "none" else (None,)):
+            got = ops.linear_backward(dy, x8, w, x_act=x_act, pre=pre, **kw)
+            assert all(torch.equal(a, b) for a, b in zip(want, got)), (act, x_act)
+
+
 def test_values_kept_as_nan_and_zeros():
     """A NaN kept in x or pre reaches the sums that hold it, and no others."""
     g = torch.Generator().manual_seed(6)
