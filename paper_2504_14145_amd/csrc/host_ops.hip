@@ -154,6 +154,7 @@ LinearPlan plan_linear(const dip_linear_args *a, bool kept = false) {
 
 struct GradPlan {
   GemmPlan dx, dw;
+  bool pair = false;
   int64_t g_at = -1, x_at = -1, w_at = -1, sums_at = -1, partial_at = 0, total = 0;
   int32_t chunks = 0;
 };
@@ -181,7 +182,9 @@ GradPlan plan_grad(const dip_linear_grad_args *a, bool x8 = false) {
     p.dw = plan_gemm(a->n, a->k, a->m, false);
     partial = partial > p.dw.bytes ? partial : p.dw.bytes;
   }
-  p.partial_at = s.take(partial);   // the two products run one after the other
+  // the two products run one after the other, or in one launch
+  p.pair = a->dx && a->dw && a->k > 0 && pair_gemms(a->m, a->k, p.dx, a->n, a->k, p.dw);
+  p.partial_at = s.take(p.pair ? p.dx.bytes + p.dw.bytes : partial);
   p.total = s.total;
   return p;
 }
@@ -275,24 +278,21 @@ int linear_grad(const dip_linear_grad_args *a, const dip_packed8 *x8, int32_t x_
   if (rx.m)
     OPS_CHECK(hip_code(launch_unpack8(a->dtype, rx.m, rx.n, rx.x, rx.act, rx.out, rx.ldo, rx.ldo, st)));
   OPS_CHECK(pack(a->dtype, px, pw, st));
-  if (a->dx && a->m > 0 && a->k > 0) {
-    Epilogue e{};
-    e.out = a->dx;
-    e.ldo = a->lddx;
-    e.scale = drop.scale;
-    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->m, a->k, a->n, Operand{g, ldg, false}, w, e, p.dx,
-                                   partial, st)));
-  }
-  if (a->dw && a->n > 0 && a->k > 0) {
-    Epilogue e{};
-    e.out = a->dw;
-    e.ldo = a->lddw;
-    e.scale = drop.scale;
-    e.out_f32 = a->grad_dtype == DIP_F32;
-    e.accumulate = a->accumulate != 0;
-    OPS_CHECK(hip_code(launch_gemm(a->dtype, a->n, a->k, a->m, Operand{g, ldg, true}, x, e, p.dw,
-                                   partial, st)));
-  }
+  Gemm gx{a->m, a->k, a->n, Operand{g, ldg, false}, w, {}, p.dx, partial};
+  gx.e.out = a->dx;
+  gx.e.ldo = a->lddx;
+  gx.e.scale = drop.scale;
+  Gemm gw{a->n, a->k, a->m, Operand{g, ldg, true}, x, {}, p.dw, p.pair ? partial + p.dx.bytes / 4 : partial};
+  gw.e.out = a->dw;
+  gw.e.ldo = a->lddw;
+  gw.e.scale = drop.scale;
+  gw.e.out_f32 = a->grad_dtype == DIP_F32;
+  gw.e.accumulate = a->accumulate != 0;
+  if (p.pair) return hip_code(launch_gemm_pair(a->dtype, gx, gw, st));
+  if (a->dx && a->m > 0 && a->k > 0)
+    OPS_CHECK(hip_code(launch_gemm(a->dtype, gx.m, gx.n, gx.k, gx.a, gx.b, gx.e, gx.plan, gx.partial, st)));
+  if (a->dw && a->n > 0 && a->k > 0)
+    OPS_CHECK(hip_code(launch_gemm(a->dtype, gw.m, gw.n, gw.k, gw.a, gw.b, gw.e, gw.plan, gw.partial, st)));
   return DIP_OK;
 }
 

@@ -262,26 +262,31 @@ constexpr int kForward = 0, kGradient = 1, kGradientAny = 2, kPartial = 3, kForw
 template <int KIND>
 using EpilogueOf = std::conditional_t<KIND == kForwardKept, KeptEpilogue, Epilogue>;
 
-// out tile BM x BN by WM x WN waves.
+// LDS of a workgroup
+template <int BM, int BN, int R>
+constexpr int kRing = R * (BM + BN) * kStep * 2;
+
+// out tile BM x BN by WM x WN waves: the id-th of part `part` of the contraction, in
+// kRing<BM, BN, R> bytes of LDS at s.
 template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R, int KIND>
-__global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
-                                                            Operand b, EpilogueOf<KIND> e, Split split) {
+__device__ __forceinline__ void gemm_tile(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
+                                          const EpilogueOf<KIND> &e, const Split &split, unsigned char *s,
+                                          uint32_t id, uint32_t part) {
   constexpr bool kIsForward = KIND == kForward || KIND == kForwardKept;
   typedef typename Vec8<T>::type V;
   constexpr int kThreads = 64 * WM * WN;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
   typedef Stage<A_K, BM, kThreads> StageA;
   typedef Stage<B_K, BN, kThreads> StageB;
-  constexpr int kBuf = StageA::kBytes + StageB::kBytes;
-  __shared__ __align__(1024) unsigned char s[R * kBuf];
+  static_assert(kRing<BM, BN, R> == R * (StageA::kBytes + StageB::kBytes));
   const uint32_t lds = lds_address(s);
   const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64);
   uint32_t tm, tn;
-  tile_of(blockIdx.x, uint32_t((m + BM - 1) / BM), uint32_t((n + BN - 1) / BN), tm, tn);
+  tile_of(id, uint32_t((m + BM - 1) / BM), uint32_t((n + BN - 1) / BN), tm, tn);
   const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
   int64_t k0 = 0, k1 = k;
   if constexpr (KIND == kPartial) {
-    k0 = int64_t(blockIdx.y) * split.steps * kStep;
+    k0 = int64_t(part) * split.steps * kStep;
     k1 = min(k, k0 + split.steps * kStep);
   }
   StageA sa;
@@ -438,7 +443,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
     };
     if constexpr (KIND == kPartial) {
       // rows of the partial product are padded to eight columns
-      float *q = split.partial + (int64_t(blockIdx.y) * m + row) * split.n8 + col0;
+      float *q = split.partial + (int64_t(part) * m + row) * split.n8 + col0;
 #pragma unroll
       for (int p = 0; p < P; ++p)
         if (row < m && cols[p] > 0) store8(q + 32 * p, 8, v[p]);
@@ -516,6 +521,39 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_
       fragments(i_, v);
       finish(decltype(i_)::value, v);
     });
+  }
+}
+
+template <class T, bool A_K, bool B_K, int BM, int BN, int WM, int WN, int R, int KIND>
+__global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(int64_t m, int64_t n, int64_t k, Operand a,
+                                                            Operand b, EpilogueOf<KIND> e, Split split) {
+  __shared__ __align__(1024) unsigned char s[kRing<BM, BN, R>];
+  gemm_tile<T, A_K, B_K, BM, BN, WM, WN, R, KIND>(m, n, k, a, b, e, split, s, blockIdx.x, blockIdx.y);
+}
+
+// Both gradients' products in one launch, in 128 x 128 tiles of which two fit a CU: of
+// small ones neither fills the card, and each waits for its slowest workgroup.  The
+// splits, and so the results' bits, are those of two launches.
+struct Product {
+  int64_t m, n, k;
+  Operand a, b;
+  Epilogue e;
+  Split split;
+  uint32_t first, tiles;   // its first workgroup, and tiles a part
+};
+template <class T, int DX, int DW>
+__global__ __launch_bounds__(256, 2) void gemm_pair_kernel(Product x, Product w) {
+  __shared__ __align__(1024) unsigned char s[kRing<128, 128, 2>];
+  const uint32_t b = blockIdx.x;
+  const bool of_x = x.first ? b >= x.first : b < w.first;
+  if (of_x) {
+    const uint32_t part = (b - x.first) / x.tiles;
+    gemm_tile<T, false, true, 128, 128, 2, 2, 2, DX>(x.m, x.n, x.k, x.a, x.b, x.e, x.split, s,
+                                                     b - x.first - part * x.tiles, part);
+  } else {
+    const uint32_t part = (b - w.first) / w.tiles;
+    gemm_tile<T, true, true, 128, 128, 2, 2, 2, DW>(w.m, w.n, w.k, w.a, w.b, w.e, w.split, s,
+                                                    b - w.first - part * w.tiles, part);
   }
 }
 
@@ -637,6 +675,37 @@ hipError_t pick(int64_t m, int64_t n, int64_t k, const Operand &a, const Operand
   }
 }
 
+template <class T>
+hipError_t run_pair(const Gemm &x, const Gemm &w, hipStream_t stream) {
+  auto product = [](const Gemm &g) {
+    return Product{g.m, g.n, g.k, g.a, g.b, g.e, Split{g.partial, g.plan.steps, (g.n + 7) / 8 * 8}, 0,
+                   uint32_t((g.m + 127) / 128 * ((g.n + 127) / 128))};
+  };
+  Product px = product(x), pw = product(w);
+  const uint32_t nx = px.tiles * uint32_t(x.plan.splits), nw = pw.tiles * uint32_t(w.plan.splits);
+  // the longer workgroups first
+  if (x.plan.steps >= w.plan.steps) pw.first = nx;
+  else px.first = nw;
+  auto go = [&](auto kernel) { kernel<<<dim3(nx + nw), dim3(256), 0, stream>>>(px, pw); };
+  auto of_dx = [&](auto dx) {
+    constexpr int DX = decltype(dx)::value;
+    if (w.plan.splits > 1) go(gemm_pair_kernel<T, DX, kPartial>);
+    else if (w.e.out_f32 || w.e.accumulate) go(gemm_pair_kernel<T, DX, kGradientAny>);
+    else go(gemm_pair_kernel<T, DX, kGradient>);
+  };
+  if (x.plan.splits > 1) of_dx(std::integral_constant<int, kPartial>{});
+  else of_dx(std::integral_constant<int, kGradient>{});
+  hipError_t rc = hipGetLastError();
+  for (const Gemm *g : {&x, &w}) {
+    if (rc != hipSuccess || g->plan.splits <= 1) continue;
+    const Split s{g->partial, g->plan.steps, (g->n + 7) / 8 * 8};
+    join_kernel<T><<<dim3(uint32_t((g->m * (s.n8 / 8) + 255) / 256)), dim3(256), 0, stream>>>(g->m, g->n, g->e, s,
+                                                                                             g->plan.splits);
+    rc = hipGetLastError();
+  }
+  return rc;
+}
+
 // Copies one or two arrays to where the products can take them: 16-byte aligned,
 // the stride a multiple of 8, zeros in the columns up to it.  One launch for both.
 template <class T>
@@ -660,13 +729,13 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJob a, PackJob b, uint32_
 // costs its partial products' way through the caches: 65,536 x 3584 x 2560's
 // weight gradient takes 1328 us whole, 932 in 7 parts; 1152 x 1792 x 3840 26 whole,
 // 40 in 2.
+struct Shape {
+  int64_t bm, bn, slots;
+  double step_us, fixed_us;
+};
+constexpr Shape shapes[] = {
+    {256, 256, 256, 1.35, 8.0}, {128, 128, 512, 0.78, 4.0}, {128, 128, 256, 0.45, 3.5}, {192, 128, 256, 0.62, 4.5}};
 GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows) {
-  struct Shape {
-    int64_t bm, bn, slots;
-    double step_us, fixed_us;
-  };
-  constexpr Shape shapes[] = {
-      {256, 256, 256, 1.35, 8.0}, {128, 128, 512, 0.78, 4.0}, {128, 128, 256, 0.45, 3.5}, {192, 128, 256, 0.62, 4.5}};
   const int64_t steps = (k + kStep - 1) / kStep;
   GemmPlan best;
   double least = 0;
@@ -679,9 +748,10 @@ GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows) {
       if (splits > 1 && (steps + each - 1) / each != splits) continue;
       const double rounds = double((tiles * splits + s.slots - 1) / s.slots);
       const double join = splits > 1 ? 4.0 + double(splits) * double(m) * double(n) * 8 / 6e6 : 0.0;
-      const double us = rounds * (double(each) * s.step_us + s.fixed_us) + join;
-      if (least != 0 && us >= least) continue;
-      least = us;
+      const double us = rounds * (double(each) * s.step_us + s.fixed_us);
+      if (least != 0 && us + join >= least) continue;
+      least = us + join;
+      best.us = us;
       best.tile = tile;
       best.splits = int(splits);
       best.steps = each;
@@ -701,6 +771,27 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
   if (!a.k_rows && !b.k_rows) return pick<_Float16, false, false>(m, n, k, a, b, e, plan, partial, stream);
   if (!a.k_rows) return pick<_Float16, false, true>(m, n, k, a, b, e, plan, partial, stream);
   return pick<_Float16, true, true>(m, n, k, a, b, e, plan, partial, stream);
+}
+
+// By the same figures: all workgroups at the rate of two a CU, or the longest alone.  The
+// two products one after the other and in one launch, us, m x k x n in bf16: 512^3 15.7 /
+// 7.7; 300 x 1024 x 1024 18.9 / 11.5; 1152 x 1792 x 3840 51 / 47; 2048^3 44 / 38; 4096 x
+// 2048 x 2048 74 / 68; 65,536 x 512 x 512 122 / 99; 1500 x 3584 x 3584 82 / 82; and not:
+// 4096^3 205 / 247; 8192 x 4096 x 3584 368 / 433; 149 x 4096 x 14336 81 / 84.  Worst seen
+// of those taken: 16,384 x 1024 x 1024 74 / 76.
+bool pair_gemms(int64_t mx, int64_t nx, const GemmPlan &x, int64_t mw, int64_t nw, const GemmPlan &w) {
+  const Shape &two = shapes[1], &one = shapes[2];
+  auto blocks = [&](int64_t m, int64_t n, const GemmPlan &p) {
+    return (m + two.bm - 1) / two.bm * ((n + two.bn - 1) / two.bn) * p.splits;
+  };
+  auto us = [](const Shape &s, int64_t steps) { return double(steps) * s.step_us + s.fixed_us; };
+  const int64_t bx = blocks(mx, nx, x), bw = blocks(mw, nw, w);
+  const double all = (double(bx) * us(two, x.steps) + double(bw) * us(two, w.steps)) / double(two.slots);
+  return bx + bw < kMaxTiles && std::max(all, us(one, std::max(x.steps, w.steps))) <= x.us + w.us;
+}
+
+hipError_t launch_gemm_pair(int dtype, const Gemm &x, const Gemm &w, hipStream_t stream) {
+  return dtype == DIP_BF16 ? run_pair<__bf16>(x, w, stream) : run_pair<_Float16>(x, w, stream);
 }
 
 hipError_t launch_gemm_kept(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,

@@ -41,12 +41,24 @@ struct GemmPlan {
   int32_t tile = 0, splits = 1;
   int64_t steps = 0;           // contraction steps a split
   int64_t bytes = 0;           // of partial products
+  double us = 0;               // expected, without the join
 };
 constexpr int64_t kMaxTiles = int64_t(1) << 24;   // 256-thread workgroups a launch
 GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, bool a_rows);   // by sizes and a's layout (not k_rows)
 hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a,
                        const Operand &b, const Epilogue &e, const GemmPlan &plan, float *partial,
                        hipStream_t stream);
+// The products of dx (a along the contraction, b not) and of dw (neither) in one launch,
+// where that is faster than one after the other; their partial products are apart.
+struct Gemm {
+  int64_t m, n, k;
+  Operand a, b;
+  Epilogue e;
+  GemmPlan plan;
+  float *partial;
+};
+bool pair_gemms(int64_t mx, int64_t nx, const GemmPlan &x, int64_t mw, int64_t nw, const GemmPlan &w);
+hipError_t launch_gemm_pair(int dtype, const Gemm &x, const Gemm &w, hipStream_t stream);
 // a and b along the contraction, pre kept in 8 bits
 hipError_t launch_gemm_kept(int dtype, int64_t m, int64_t n, int64_t k, const Operand &a, const Operand &b,
                             const KeptEpilogue &e, const GemmPlan &plan, float *partial, hipStream_t stream);
