@@ -238,9 +238,9 @@ int dip_linear_grad_kept(const dip_linear_grad_args *a, const dip_packed8 *x, in
 
 /* Root-mean-square norm of m rows of c: t = x + residual rounded to the type (the
  * stream of residuals; x itself without one), rstd = 1 / sqrt(mean(t^2) + eps),
- * y = gamma t rstd.  Squares are summed in float32 by a thread and in float64 over the
- * row: rows whose squares leave float32's range above have rstd 0, below it that of
- * eps.  total (t) may be the residual itself or null; y,
+ * y = gamma t rstd.  Squares are summed in float64, and rstd is rounded once, also of
+ * rows whose squares no float32 holds; one that float32 does not hold is infinite.  total
+ * (t) may be the residual itself or null; y,
  * rstd and packed.values too, where they are not wanted.  packed has y in 8 bits, from
  * the float32 values.  gamma may be null (1). */
 typedef struct {

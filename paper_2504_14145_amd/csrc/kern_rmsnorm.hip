@@ -124,20 +124,29 @@ __device__ __forceinline__ void total8(const Held<T> &x, const Held<T> &r, bool 
   }
 }
 
-// 1 / sqrt(sum / n + eps) and what its rounding left off, by one step of Newton's
-// iteration on the residual.  The threads' sums, whose errors average out, are joined in
-// float64: nothing puts a whole row off by more than 2^-28.
+// 1 / sqrt(sum / n + eps) in float64, from the hardware's estimate and one step of third
+// order, as a float32 and what its rounding left off.  Squares are exact in float64 and
+// summed in it (two instructions an element, no time beside the memory's: 65,536 x 3584
+// with the 8 bits 378 us as with float32 sums, 2^26 elements in rows of 515 to 2051
+// within 1 %), so v + rest is off by 2^-47 at most, of the longest rows, 4096 squares a
+// thread, by 2^-41, however alike the values, and rows whose squares no float32 holds
+// have theirs too.
 struct Rstd {
   float v, rest;
   __device__ __forceinline__ Rstd(double sum, double inv, float eps) {   // inv: 1 / n
     const double mean = fma(sum, inv, double(eps));
-    const float m = float(mean), low = float(mean - double(m));
-    v = 1.f / sqrtf(m);
-    const float t = m * v, below = fmaf(m, v, -t);
-    const float off = fmaf(-fmaf(low, v, below), v, fmaf(-t, v, 1.f));   // 1 - mean v^2
-    rest = fabsf(off) < 1e-3f ? 0.5f * v * off : 0.f;                    // not of an infinity or zero
+    double r = __builtin_amdgcn_rsq(mean);
+    const double t = mean * r, below = fma(mean, r, -t);
+    const double off = fma(-below, r, fma(-t, r, 1.0));                        // 1 - mean r^2
+    r = fabs(off) < 1e-3 ? fma(r * off, fma(off, 0.375, 0.5), r) : r;          // not of an infinity or zero
+    v = float(r);
+    rest = v < INFINITY ? float(r - double(v)) : 0.f;
   }
 };
+__device__ __forceinline__ void add_squares(const float (&v)[8], double &sum) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) sum = fma(double(v[q]), double(v[q]), sum);
+}
 
 // y and its 8 bits from t; of the four lanes that share a scale all are here.
 template <class T, bool PACK>
@@ -196,12 +205,12 @@ __global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_n
     x[j].get(static_cast<const T *>(a.x) + row * a.ldx, c, n);
     if (a.residual) r[j].get(static_cast<const T *>(a.residual) + row * a.ldr, c, n);
   }
-  float v[NV][8], sum = 0.f;
+  float v[NV][8];
+  double sum = 0.0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     total8(x[j], r[j], a.residual != nullptr, Held<T>::moved((t + j * lanes) * 8, n), v[j]);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) sum += v[j][q] * v[j][q];
+    add_squares(v[j], sum);
   }
   if (a.total) {
 #pragma unroll
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(Lanes<LANES>::kMost) void rms_rows_kernel(dip_rms_n
       if (c < n) put8(static_cast<T *>(a.total) + row * a.ldt + c, n - c, v[j]);
     }
   }
-  const Rstd rstd(L::sum(double(sum), s, turn), inv, a.eps);
+  const Rstd rstd(L::sum(sum, s, turn), inv, a.eps);
   if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
 #pragma unroll
   for (int j = 0; j < NV; ++j) write8<T, PACK>(a, p, row, (t + j * lanes) * 8, rstd, v[j]);
@@ -237,15 +246,14 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(dip_rms_norm_args a, int
       for (int i = 0; i < 8; ++i) v[i] = float(T(v[i] + q[i]));
     }
   };
-  float sum = 0.f;
+  double sum = 0.0;
   for (int c = t * 8; c < n; c += 1024 * 8) {
     float v[8];
     first(c, v);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) sum += v[q] * v[q];
+    add_squares(v, sum);
     if (total) put8(total + c, n - c, v);
   }
-  const Rstd rstd(Lanes<0>::sum(double(sum), s, turn), inv, a.eps);
+  const Rstd rstd(Lanes<0>::sum(sum, s, turn), inv, a.eps);
   if (t == 0 && a.rstd) a.rstd[row] = rstd.v;
   for (int c = t * 8; c < (n + 31) / 32 * 32; c += 1024 * 8) {
     float v[8] = {};
