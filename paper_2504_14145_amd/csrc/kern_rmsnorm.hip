@@ -148,6 +148,20 @@ __device__ __forceinline__ void add_squares(const float (&v)[8], double &sum) {
   for (int q = 0; q < 8; ++q) sum = fma(double(v[q]), double(v[q]), sum);
 }
 
+// t rstd as a float32 and what its rounding left off, together to 2^-45.  gamma comes
+// after it: t rstd is at most sqrt(c), where gamma t may leave float32's range though y
+// does not, and y is rounded once.
+struct Normed {
+  float s, e;
+  __device__ __forceinline__ Normed(float t, const Rstd &rstd) {
+    s = t * rstd.v;
+    e = fmaf(t, rstd.rest, fmaf(t, rstd.v, -s));
+  }
+  __device__ __forceinline__ float times(float g) const { return fmaf(s, g, e * g); }
+  // what is left of it beside y = times(g)
+  __device__ __forceinline__ float beside(float g, float y) const { return fmaf(s, g, -y) + e * g; }
+};
+
 // y and its 8 bits from t; of the four lanes that share a scale all are here.
 template <class T, bool PACK>
 __device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed &p, int64_t row, int c, const Rstd &rstd,
@@ -156,14 +170,12 @@ __device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed 
   float g[8], y[8];
   gamma8<T>(a.gamma, c, n, g);
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const float t = v[q] * g[q];   // exact of 2-byte types
-    y[q] = fmaf(t, rstd.v, t * rstd.rest);
-  }
+  for (int q = 0; q < 8; ++q) y[q] = Normed(v[q], rstd).times(g[q]);
   if (a.y && left > 0) put8(static_cast<T *>(a.y) + row * a.ldy + c, left, y);
   if constexpr (PACK) {
     // A float32 that ends in nineteen zeros may be the middle of two 8-bit values, on
-    // which rounding has put what lies beside it: one in 2^19.  It goes to its side.
+    // which rounding has put what lies beside it: one in 2^19.  It goes to its side; what
+    // is nearer than this arithmetic tells counts as the middle.
     constexpr uint32_t kLow = 0x7ffffu;
     uint32_t low = kLow;
     if (left >= 8) {
@@ -176,10 +188,9 @@ __device__ __forceinline__ void write8(const dip_rms_norm_args &a, const Packed 
     if (low == 0) {
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        const float t = v[q] * g[q];
-        const float beside = fmaf(t, rstd.v, -y[q]) + fmaf(t, rstd.rest, fmaf(v[q], g[q], -t) * rstd.v);
+        const float beside = Normed(v[q], rstd).beside(g[q], y[q]);
         const uint32_t bits = magnitude(y[q]);
-        if ((bits & kLow) == 0 && bits - 1 < kInfinity - 1 && beside != 0.f) {
+        if ((bits & kLow) == 0 && bits - 1 < kInfinity - 1 && fabsf(beside) > 0x1p-40f * fabsf(y[q])) {
           const bool out = (beside > 0.f) == (y[q] > 0.f);
           y[q] = copysignf(__builtin_bit_cast(float, bits + (out ? 1u : ~0u)), y[q]);
         }
