@@ -211,7 +211,7 @@ int dip_group_norm_grad(const dip_group_norm_grad_args *a, void *stream);
  * kept as NaN.  What is read may have any bytes: scales 0 and 255 are 2^-127 and NaN.
  * Restored values are exact in float32, and in bfloat16 from 2^-126 on; one that
  * rounded up beyond the largest value of the type it is restored to becomes that
- * value. */
+ * value (through an activation: beyond float32's, before it). */
 typedef struct {
   void *values;              /* [m][n] bytes, ld; any alignment                 */
   int64_t ld;

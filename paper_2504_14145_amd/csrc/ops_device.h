@@ -389,6 +389,10 @@ __device__ __forceinline__ void restore8(const Packed &x, int64_t row, int col, 
   float v[8];
   from8bits(bits, scale_of(byte), v);
   if constexpr (ACT) {
+    if (!held_by(0.f, byte)) {   // before the activation, which of an infinity may be NaN
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = within<float>(v[j]);
+    }
     if (act == DIP_ACT_SILU) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], DIP_ACT_SILU);
