@@ -297,7 +297,8 @@ int dip_rms_norm_grad(const dip_rms_norm_grad_args *a, void *stream);
  * the angle pos[i][axis[j]] freq[j] radians (inverse != 0: by its negative, which is
  * the gradient), (a, b) to (a cos - b sin, a sin + b cos).  Pair j is elements
  * j and pairs + j of the head, or with interleaved != 0 2 j and 2 j + 1; elements from
- * 2 pairs on are copied.  Angles are float64 up to their sine and cosine.  A pair whose
+ * 2 pairs on are copied.  Angles are float64, and so their sines and cosines up to one
+ * rounding to float32.  A pair whose
  * axis is not one of the axes stays as it is.  k with its heads goes along where
  * keys > 0.  Strides in elements, up to 2^46: st between tokens, sh between heads, in
  * either order; pos st and sa between tokens and axes.  An output may be its input

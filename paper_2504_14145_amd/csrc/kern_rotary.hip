@@ -4,11 +4,11 @@
 // Bound by memory, every head read and written once; a token's sines and cosines are
 // as many as one head has pairs and serve all heads.  A workgroup takes a token or a
 // few, or a share of one token's heads: it asks for all its pairs, a vector a thread,
-// puts the sines and cosines into LDS meanwhile (the angle in turns in float64, less its
-// whole turns: far positions lose nothing), and turns and stores.
-// bf16, 65,536 tokens of 56 heads of 128: 313 to 324 us, 5.9 TB/s; 28 heads of q alone
-// 153, 6.1.  2^26 elements of 16 + 16 heads, us: 128 elements a head 54, 112 57, 72 58,
-// 20 (4 + 4 heads) 66; one head of q and k each 86, sines and cosines then being as many
+// puts the sines and cosines into LDS meanwhile (in float64 up to their rounding: far
+// positions lose nothing), and turns and stores.
+// bf16, 65,536 tokens of 56 heads of 128: 319 to 323 us, 5.9 TB/s; 28 heads of q alone
+// 160, 5.9.  2^26 elements of 16 + 16 heads, us: 128 elements a head 47, 112 50, 72 51,
+// 20 (4 + 4 heads) 57; one head of q and k each 69, sines and cosines then being as many
 // as pairs.
 #include <algorithm>
 #include <type_traits>
@@ -21,11 +21,9 @@ namespace {
 constexpr int kThreads = 512;   // at most
 
 __device__ __forceinline__ double position(const dip_rotary_args &a, int64_t at) {
-  switch (a.pos_type) {
-    case DIP_POS_I32: return double(static_cast<const int32_t *>(a.pos)[at]);
-    case DIP_POS_I64: return double(static_cast<const int64_t *>(a.pos)[at]);
-    default: return double(static_cast<const float *>(a.pos)[at]);
-  }
+  if (a.pos_type == DIP_POS_I64) return double(static_cast<const int64_t *>(a.pos)[at]);
+  const int32_t v = static_cast<const int32_t *>(a.pos)[at];
+  return a.pos_type == DIP_POS_I32 ? double(v) : double(__builtin_bit_cast(float, v));
 }
 
 template <class T, int V>
@@ -38,8 +36,11 @@ struct Vector<T, 1> {
   typedef T type, any;
 };
 template <class T, int V>
-__device__ __forceinline__ void load(const T *p, float (&v)[V]) {
-  const typename Vector<T, V>::type t = *reinterpret_cast<const typename Vector<T, V>::any *>(p);
+__device__ __forceinline__ typename Vector<T, V>::type load(const T *p) {
+  return *reinterpret_cast<const typename Vector<T, V>::any *>(p);
+}
+template <class T, int V>
+__device__ __forceinline__ void floats(const typename Vector<T, V>::type &t, float (&v)[V]) {
   if constexpr (V == 1) v[0] = float(t);
   else {
 #pragma unroll
@@ -85,9 +86,31 @@ struct Item {
   }
 };
 
+// (cosine, sine) of an angle in turns: less its whole turns and its nearest quarter by the
+// Taylor series about that, in float64 to 2^-36 of themselves, and rounded once.  (The
+// hardware's way, sincospif of a float32 argument, leaves 2^-23 beside that rounding.)
+__device__ __forceinline__ float2 turned_by(double turns) {
+  turns -= rint(turns);
+  const double quarter = rint(4.0 * turns), a = fma(quarter, -0.25, turns) * 6.283185307179586477, z = a * a;
+  double s = fma(z, -1.0 / 39916800, 1.0 / 362880), c = fma(z, 1.0 / 479001600, -1.0 / 3628800);
+  s = fma(z, s, -1.0 / 5040);
+  c = fma(z, c, 1.0 / 40320);
+  s = fma(z, s, 1.0 / 120);
+  c = fma(z, c, -1.0 / 720);
+  s = fma(z, s, -1.0 / 6);
+  c = fma(z, c, 1.0 / 24);
+  s = fma(a * z, s, a);
+  c = fma(z, c, -0.5);
+  c = fma(z, c, 1.0);
+  const int q = int(quarter);   // -2 .. 2: to (-s, c), (-c, -s) and (s, -c)
+  const float u = float(q & 1 ? s : c), v = float(q & 1 ? c : s);
+  return float2{(q + 1) & 2 ? -u : u, q & 2 ? -v : v};
+}
+
 // V pairs a thread; a head's last vector ends with its pairs and has some of the one
 // before, which come out the same.  All loads are before the barrier and all stores
-// behind it, and a head is one workgroup's: outputs may be the inputs.
+// behind it, and a head is one workgroup's: outputs may be the inputs.  What is loaded
+// stays as it is up to there, so that nothing waits for it before.
 template <class T, int V, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int64_t token0, Shares sh) {
   extern __shared__ float2 table[];   // [tokens][pairs]: cosine, sine
@@ -97,24 +120,32 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(dip_rotary_args a, int
   const bool on = threadIdx.x < uint32_t(tokens) * uint32_t(heads) * sh.vectors.by;
   const Item<T> it(a, sh, V, on ? threadIdx.x : 0, i0, h0, heads);
   const int at = int(it.first) * (INTERLEAVED ? 2 : 1), step = INTERLEAVED ? V : a.pairs;
-  float u[V], w[V];
-  if (on) {   // on their way while the table is made
-    load<T, V>(it.p + at, u);
-    load<T, V>(it.p + at + step, w);
-  }
-  for (int j = threadIdx.x; j < tokens * a.pairs; j += blockDim.x) {
+  const int angles = tokens * a.pairs;
+  auto turns = [&](int j) __attribute__((always_inline)) {   // of the pair's angle; 0 without an axis
     const int n = j / a.pairs, pair = j - n * a.pairs, axis = a.axis[pair];
-    float2 cs = {1.f, 0.f};
-    if (axis >= 0 && axis < a.axes) {
-      double turns = position(a, (i0 + n) * a.p_st + axis * a.p_sa) * a.freq[pair] * 0.15915494309189533577;
-      turns -= rint(turns);
-      sincospif(2.f * float(turns), &cs.y, &cs.x);
-      if (a.inverse) cs.y = -cs.y;
-    }
+    const double f = a.freq[pair] * 0.15915494309189533577;   // asked for with the axis, not behind the position
+    const bool has = uint32_t(axis) < uint32_t(a.axes);
+    const double p = has ? position(a, (i0 + n) * a.p_st + axis * a.p_sa) : 0.0;
+    return has ? p * f : 0.0;
+  };
+  auto put = [&](int j, double turns) __attribute__((always_inline)) {
+    float2 cs = turned_by(turns);
+    if (a.inverse) cs.y = -cs.y;
     table[j] = cs;
+  };
+  typename Vector<T, V>::type ru, rw;
+  if (on) {   // on their way while the table is made
+    ru = load<T, V>(it.p + at);
+    rw = load<T, V>(it.p + at + step);
   }
+  for (int j = threadIdx.x; j < angles; j += blockDim.x) put(j, turns(j));
+  // what overlaps at a head's end another wave may write in its input's place
+  if (a.pairs % V) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (!on) return;
+  float u[V], w[V];
+  floats<T, V>(ru, u);
+  floats<T, V>(rw, w);
   const float2 *cs = table + it.n * a.pairs + it.first;
   float ou[V], ow[V];
   if constexpr (INTERLEAVED && V > 1) {
