@@ -773,21 +773,29 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
   return pick<_Float16, true, true>(m, n, k, a, b, e, plan, partial, stream);
 }
 
-// By the same figures: all workgroups at the rate of two a CU, or the longest alone.  The
-// two products one after the other and in one launch, us, m x k x n in bf16: 512^3 15.7 /
-// 7.7; 300 x 1024 x 1024 18.9 / 11.5; 1152 x 1792 x 3840 51 / 47; 2048^3 44 / 38; 4096 x
-// 2048 x 2048 74 / 68; 65,536 x 512 x 512 122 / 99; 1500 x 3584 x 3584 82 / 82; and not:
-// 4096^3 205 / 247; 8192 x 4096 x 3584 368 / 433; 149 x 4096 x 14336 81 / 84.  Worst seen
-// of those taken: 16,384 x 1024 x 1024 74 / 76.
+// All workgroups at the rate of two a CU, or the longest alone.  With both kinds in one
+// launch a step of two a CU takes 0.9 to 1 us (fitted to 250 sizes of two rounds and more;
+// 0.78 of one kind alone), and beyond one round the last workgroups leave places empty:
+// half a workgroup's time.  Of 420 sizes up to 65,600 x 5200 x 5200 that the price of 0.78
+// without the half took, 48 were slower than one after the other, by up to 23 %; this
+// takes 237 of them and none that is more than 1 % slower, and gives up 3 % and more of
+// 114.  One after the other and in one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8;
+// 2048^3 39.4 / 34.0; 2880 x 256 x 1664 31.9 / 23.4; 3200 x 576 x 2688 42.2 / 34.6; 2176 x
+// 3904 x 448 39.8 / 26.5.  And not: 18,176 x 512 x 7936 305 / 374; 29,440 x 2560 x 1408
+// 364 / 431; 14,336 x 2944 x 5120 641 / 745; 1600 x 2368 x 1856 40.5 / 44.6; given up: 1152
+// x 1792 x 3840 43.9 / 41.5, 4096 x 2048 x 2048 69 / 63, 65,536 x 512 x 512 111 / 94.
 bool pair_gemms(int64_t mx, int64_t nx, const GemmPlan &x, int64_t mw, int64_t nw, const GemmPlan &w) {
   const Shape &two = shapes[1], &one = shapes[2];
+  constexpr double kMixedStep = 0.9;
   auto blocks = [&](int64_t m, int64_t n, const GemmPlan &p) {
     return (m + two.bm - 1) / two.bm * ((n + two.bn - 1) / two.bn) * p.splits;
   };
-  auto us = [](const Shape &s, int64_t steps) { return double(steps) * s.step_us + s.fixed_us; };
+  auto us = [](double step_us, double fixed_us, int64_t steps) { return double(steps) * step_us + fixed_us; };
   const int64_t bx = blocks(mx, nx, x), bw = blocks(mw, nw, w);
-  const double all = (double(bx) * us(two, x.steps) + double(bw) * us(two, w.steps)) / double(two.slots);
-  return bx + bw < kMaxTiles && std::max(all, us(one, std::max(x.steps, w.steps))) <= x.us + w.us;
+  const double tx = us(kMixedStep, two.fixed_us, x.steps), tw = us(kMixedStep, two.fixed_us, w.steps);
+  const double all = (double(bx) * tx + double(bw) * tw) / double(two.slots) + (bx + bw > two.slots ? std::min(tx, tw) / 2 : 0.0);
+  const double alone = us(one.step_us, one.fixed_us, std::max(x.steps, w.steps));
+  return bx + bw < kMaxTiles && std::max(all, alone) <= x.us + w.us;
 }
 
 hipError_t launch_gemm_pair(int dtype, const Gemm &x, const Gemm &w, hipStream_t stream) {
