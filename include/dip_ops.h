@@ -14,8 +14,8 @@
  *   dip_rms_norm     t = x + residual, y = gamma t rstd, also in 8 bits
  *   dip_rms_norm_grad
  *   dip_rotary       queries and keys turned by positions along several axes
- *   dip_pack8        activations kept in 8 bits (a memory strategy of Sec. 5.3
- *   dip_unpack8      between keeping and recomputing), restored, and
+ *   dip_pack8        activations kept in 8 bits (between the memory strategies of
+ *   dip_unpack8      Sec. 5.3, keeping and recomputing), restored, and
  *   dip_linear_kept  written and read by the products and their gradients
  *   dip_linear_grad_kept
  *

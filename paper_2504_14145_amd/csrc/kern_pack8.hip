@@ -2,14 +2,16 @@
 //
 // A value is q 2^e with q of four significant bits and one e for 32 columns: the
 // conversion instructions take such a scale, a kept value is exact in bfloat16, and a
-// group's largest value moves the step of the others only where they are below a
-// 2^-15th of it.  Bound by memory: read once, written once.  A thread has one vector of
+// group's largest value costs the others bits only where they are below a 2^-14th of it
+// (it divides to between 224 and 448, and steps stop shrinking at 2^-6: from 2^-13.8 to
+// 2^-14.8 of it).  Bound by memory: read once, written once.  A thread has one vector of
 // eight columns, and nothing waits but for its own load: two a thread, sixteen columns
 // a thread and non-temporal accesses were 2 to 5 % slower (235 million bf16: 116 us,
 // 6.1 TB/s, either way; 119, 121 with two and four vectors, 123 with sixteen columns).
 // That leaves some 60 instructions a vector before they are what bounds it: hence
 // magnitudes compared as integers two at a time, and whole vectors at the ends of rows
-// (65,536 x 2560 fp16 packed 89 to 100 us, restored 82; through GELU a quarter more;
+// (65,536 x 2560 fp16 packed 87 to 99 us, restored 83 to 86, through GELU 99; float32 144,
+// 145 and 158, 5.8 TB/s without an activation;
 // 2^26 bf16 in rows of 100 44 and 44, where elements one by one at the end took 61 and 75).
 #include <algorithm>
 

@@ -3,12 +3,13 @@
 //
 // Bound by memory: x and the residual read, their sum and the norm written forward,
 // dy, the sum and its gradient read and one array written backward, against some 15
-// operations an element (35 instructions where it is packed too: 60 % of the issue).  A
+// operations an element (36 instructions where it is packed too: 63 % of the issue).  A
 // row of up to 16,384 columns is held in registers from its load to its stores; longer
 // rows are read a second time, out of the caches.  The gradient's workgroups go over
 // rows and keep the sums of dgamma on the way; of few rows dgamma is summed beside dx.
-// bf16, 65,536 x 3584 with the residual: 350 us forward with the 8 bits (6.0 TB/s), 335 +
-// 4 the gradient (5.6); 8192 x 4096 60 and 53; 149 x 4096 4.6 and 4.0 a launch.  Rows
+// bf16, 65,536 x 3584 with the residual: 372 us forward with the 8 bits (5.7 TB/s), 321
+// without, 335 to 344 + 5 the gradient (5.5); 8192 x 4096 56 and 53; 149 x 4096 4.8 and 4.1
+// a launch; 1201 x 1795 float32 7.7 and 7.9 + 5.  Rows
 // beyond 16,384 columns: 4.2 TB/s, and 3 for the gradient, which reads dy and the sum
 // in two launches.
 #include <algorithm>

@@ -12,8 +12,9 @@ Projection is the start of the attention half, up to its heads:
 
     t = x + residual;  n = rms_norm(t);  q, k, v = n w^T + b;  q, k = rotary(q, k)
 
-A forward keeps its activations, keeps them in 8 bits (half the memory or less, and
-gradients of weights that see them rounded to four significant bits) or, under a
+A forward keeps its activations, keeps them in 8 bits (33 / 64 of the memory of 16, and of
+an MLP, whose pre then serves as u too, down to half of that; gradients of weights see
+them rounded to four significant bits) or, under a
 memory strategy that recomputes (Sec. 5.3), only its input; the backward then runs
 the forward again and draws the same dropout mask, which is a function of the layer,
 the sample's seed and the row.  A piece of a sample (Sec. 4) passes the row it starts at, so pieces
