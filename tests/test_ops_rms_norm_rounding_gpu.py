@@ -170,3 +170,15 @@ def test_a_largest_value_beside_the_border_of_two_scales():
     eps = float(torch.tensor(1 - mean))
     _, _, _, p = ops.rms_norm(x.cuda(), g.cuda(), eps=eps, packed=True, need_out=False)
     check_8_bits(p, (x.double() * g.double() / (mean + eps) ** 0.5).cuda(), sure=0)
+
+
+@pytest.mark.parametrize("c", [40, 1027, 3000, 12345, 20000])
+def test_y_in_the_residuals_place(c):
+    g = torch.Generator(device="cuda").manual_seed(c)
+    x, r = (torch.randn((70, c), generator=g, device="cuda").to(BF16) for _ in range(2))
+    w = torch.rand(c, generator=g, device="cuda").to(BF16)
+    want = ops.rms_norm(x, w, residual=r, packed=True)
+    got = ops.rms_norm(x, w, residual=r, packed=True, out=r)
+    assert got[0] is r and all(torch.equal(a, b) for a, b in zip(want[:3], got[:3]))
+    assert torch.equal(want[3].values.view(torch.uint8), got[3].values.view(torch.uint8))
+    assert torch.equal(want[3].scales, got[3].scales)
