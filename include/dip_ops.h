@@ -229,7 +229,9 @@ int dip_unpack8(int32_t dtype, int64_t m, int64_t n, const dip_packed8 *x, int32
 int64_t dip_linear_kept_workspace(const dip_linear_args *a, const dip_packed8 *pre);
 int dip_linear_kept(const dip_linear_args *a, const dip_packed8 *pre, void *stream);
 /* dip_linear_grad from activations kept in 8 bits: x is x_act of the kept matrix,
- * rounded to the type, and slopes are those at the kept pre.  Either may be null: then
+ * rounded to the type (where act rounds g too, x_act's values are taken as two of the
+ * type, so that one of dw's factors is rounded), and slopes are those at the kept pre.
+ * Either may be null: then
  * a->x (x_act not used) or a->pre is read. */
 int64_t dip_linear_grad_kept_workspace(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act,
                                        const dip_packed8 *pre);

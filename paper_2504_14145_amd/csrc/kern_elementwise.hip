@@ -120,6 +120,7 @@ __device__ __forceinline__ void grad_in_block(const GradIn &g, uint32_t bx, uint
           sum[j] += v[u][j];
         }
         if (g.out) store8(static_cast<T *>(g.out) + (row + 8 * u) * g.ldo + col, 8, v[u]);
+        if (g.again) store8(static_cast<T *>(g.again) + (row + 8 * u) * g.ldo + col, 8, v[u]);
       }
     };
     int64_t row = r0 + ty;
@@ -167,7 +168,9 @@ __global__ __launch_bounds__(kThreads) void grad_in_kept_kernel(GradIn g, Restor
     if (i >= r.items) return;
     const uint32_t row = r.per(i);
     const int col = int(i - row * r.per.by) * 8;
-    return restore8<T, ACT>(r.x.x, row, col, r.x.n, r.x.act, static_cast<T *>(r.x.out) + int64_t(row) * r.x.ldo + col, 8);
+    const int64_t at = int64_t(row) * r.x.ldo + col;
+    return restore8<T, ACT>(r.x.x, row, col, r.x.n, r.x.act, static_cast<T *>(r.x.out) + at, 8,
+                            r.x.low ? static_cast<T *>(r.x.low) + at : nullptr);
   }
   pack_item<T>(w, int64_t(b - r.x_blocks) * kThreads + threadIdx.x);
 }

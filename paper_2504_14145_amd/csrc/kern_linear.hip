@@ -776,10 +776,10 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
 // All workgroups at the rate of two a CU, or the longest alone.  With both kinds in one
 // launch a step of two a CU takes 0.9 to 1 us (fitted to 250 sizes of two rounds and more;
 // 0.78 of one kind alone), and beyond one round the last workgroups leave places empty:
-// half a workgroup's time.  Of 420 sizes up to 65,600 x 5200 x 5200 that the price of 0.78
+// half a workgroup's time.  Of 420 random sizes up to 65,600 x 5200 x 5200 that the price of 0.78
 // without the half took, 48 were slower than one after the other, by up to 23 %; this
-// takes 237 of them and none that is more than 1 % slower, and gives up 3 % and more of
-// 114.  One after the other and in one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8;
+// takes 237 of them and none that is more than 1 % slower (of 300 others one, by 2.8 %),
+// and gives up 3 % and more of 114.  One after the other and in one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8;
 // 2048^3 39.4 / 34.0; 2880 x 256 x 1664 31.9 / 23.4; 3200 x 576 x 2688 42.2 / 34.6; 2176 x
 // 3904 x 448 39.8 / 26.5.  And not: 18,176 x 512 x 7936 305 / 374; 29,440 x 2560 x 1408
 // 364 / 431; 14,336 x 2944 x 5120 641 / 745; 1600 x 2368 x 1856 40.5 / 44.6; given up: 1152

@@ -75,13 +75,14 @@ __global__ __launch_bounds__(kThreads) void pack8_kernel(uint32_t items, uint32_
 
 template <class T, bool ACT>
 __global__ __launch_bounds__(kThreads) void unpack8_kernel(uint32_t items, uint32_t row0, Divide per, int n,
-                                                           Packed x, int act, T *y, int64_t ldy, int fill) {
+                                                           Packed x, int act, T *y, int64_t ldy, int fill, T *low) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
   if (i >= items) return;
   const uint32_t in = per(i);
   const int64_t row = int64_t(row0) + in;
   const int col = int(i - in * per.by) * 8;
-  restore8<T, ACT>(x, row, col, n, act, y + row * ldy + col, min(8, fill - col));
+  const int64_t at = row * ldy + col;
+  restore8<T, ACT>(x, row, col, n, act, y + at, min(8, fill - col), low ? low + at : nullptr);
 }
 
 // f(items, row0, Divide(per)) over launches of fewer than 2^31 items.
@@ -104,10 +105,11 @@ hipError_t pack(int64_t m, int64_t n, const void *x, int64_t ldx, const Packed &
   });
 }
 template <class T>
-hipError_t unpack(int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill, hipStream_t st) {
+hipError_t unpack(int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill, hipStream_t st, void *low) {
   return pieces(m, (fill + 7) / 8, [&](dim3 grid, uint32_t items, uint32_t row0, const Divide &per) {
     auto go = [&](auto kernel) {
-      kernel<<<grid, dim3(kThreads), 0, st>>>(items, row0, per, int(n), x, act, static_cast<T *>(y), ldy, int(fill));
+      kernel<<<grid, dim3(kThreads), 0, st>>>(items, row0, per, int(n), x, act, static_cast<T *>(y), ldy, int(fill),
+                                              static_cast<T *>(low));
     };
     act != DIP_ACT_NONE ? go(unpack8_kernel<T, true>) : go(unpack8_kernel<T, false>);
   });
@@ -125,11 +127,11 @@ hipError_t launch_pack8(int dtype, int64_t m, int64_t n, const void *x, int64_t 
 }
 
 hipError_t launch_unpack8(int dtype, int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill,
-                          hipStream_t stream) {
+                          hipStream_t stream, void *low) {
   switch (dtype) {
-    case DIP_F32: return unpack<float>(m, n, x, act, y, ldy, fill, stream);
-    case DIP_F16: return unpack<_Float16>(m, n, x, act, y, ldy, fill, stream);
-    default: return unpack<__bf16>(m, n, x, act, y, ldy, fill, stream);
+    case DIP_F32: return unpack<float>(m, n, x, act, y, ldy, fill, stream, low);
+    case DIP_F16: return unpack<_Float16>(m, n, x, act, y, ldy, fill, stream, low);
+    default: return unpack<__bf16>(m, n, x, act, y, ldy, fill, stream, low);
   }
 }
 

@@ -372,9 +372,11 @@ __device__ __forceinline__ float within(float v) {
 // Columns col .. col + 7 of act of a row in 8 bits, of which n exist, to `left` columns
 // from out on: zeros beyond n.  Behind an activation rounded once to T, which as a
 // product's operand is all that the matrix instructions take (0.0017 of the norm of a bf16
-// gradient, beside as much of its own rounding); without one exact.
+// gradient, beside as much of its own rounding); without one exact.  What the rounding
+// left off goes to `low`, if given.
 template <class T, bool ACT>
-__device__ __forceinline__ void restore8(const Packed &x, int64_t row, int col, int n, int act, T *out, int left) {
+__device__ __forceinline__ void restore8(const Packed &x, int64_t row, int col, int n, int act, T *out, int left,
+                                         T *low = nullptr) {
   u32x2 bits = {0, 0};
   uint32_t byte = 127;
   if (col < n) {
@@ -411,6 +413,13 @@ __device__ __forceinline__ void restore8(const Packed &x, int64_t row, int col, 
     for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
   }
   put8(out, left, v);   // beyond n act(0) = 0
+  if constexpr (ACT) {
+    if (low) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] -= float(T(v[j]));   // exact
+      put8(low, left, v);
+    }
+  }
 }
 // Packs a quad's 32 columns from `col` % 32 == 8 (lane % 4) on, of which the lane has
 // `left`, zeros beyond them; all four lanes are on, one without columns writes nothing.

@@ -102,7 +102,7 @@ struct GradIn {
   int64_t ldy, ldp;
   Drop drop;
   int32_t act;
-  void *out;
+  void *out, *again;         // again: the same once more, or null
   int64_t ldo;
   float *partial;
   int32_t row_chunks;
@@ -111,12 +111,13 @@ struct GradIn {
 int32_t grad_row_chunks(int64_t m, int64_t n);
 hipError_t launch_grad_in(int dtype, const GradIn &g, hipStream_t stream);
 // act of x [m][n] in 8 bits to out (16-byte aligned, ldo a multiple of 8), zeros in
-// columns n .. ldo - 1
+// columns n .. ldo - 1; what rounding it left off to low, laid out like out (null: not
+// wanted)
 struct Restore {
   Packed x;
   int64_t m;
   int32_t n, act;
-  void *out;
+  void *out, *low;
   int64_t ldo;
 };
 // All three in one launch, where that is faster and has the threads; w may have no rows.
@@ -139,9 +140,9 @@ hipError_t launch_dropout_add(int dtype, int64_t m, int64_t n, const void *x, in
 
 hipError_t launch_pack8(int dtype, int64_t m, int64_t n, const void *x, int64_t ldx, const Packed &out,
                         hipStream_t stream);
-// y = act(x), zeros in columns n .. fill - 1
+// y = act(x), zeros in columns n .. fill - 1; low as Restore's, of an activation
 hipError_t launch_unpack8(int dtype, int64_t m, int64_t n, const Packed &x, int act, void *y, int64_t ldy, int64_t fill,
-                          hipStream_t stream);
+                          hipStream_t stream, void *low = nullptr);
 hipError_t launch_rms_norm(const dip_rms_norm_args &a, hipStream_t stream);
 hipError_t launch_rms_norm_grad(const dip_rms_norm_grad_args &a, hipStream_t stream);
 int64_t rms_norm_grad_workspace(const dip_rms_norm_grad_args &a);
