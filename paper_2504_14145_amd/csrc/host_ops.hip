@@ -163,7 +163,7 @@ struct GradPlan {
   // are rounded, and dw would be sqrt(3) of its own rounding's error off in the place of
   // the sqrt(2) that any other product's gradient is; this takes x's part back for one more
   // product (gradients behind GELU, of an x without and behind SiLU, bf16: 1152 x 1792 x
-  // 3840 60 and 79 us, 8192 x 3584 x 4096 408 and 616).
+  // 3840 54 and 79 us, 8192 x 3584 x 4096 408 and 616).
   int64_t rows = 0;
   int64_t g_at = -1, x_at = -1, w_at = -1, sums_at = -1, partial_at = 0, total = 0;
   int32_t chunks = 0;

@@ -773,29 +773,46 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
   return pick<_Float16, true, true>(m, n, k, a, b, e, plan, partial, stream);
 }
 
-// All workgroups at the rate of two a CU, or the longest alone.  With both kinds in one
-// launch a step of two a CU takes 0.9 to 1 us (fitted to 250 sizes of two rounds and more;
-// 0.78 of one kind alone), and beyond one round the last workgroups leave places empty:
-// half a workgroup's time.  Of 420 random sizes up to 65,600 x 5200 x 5200 that the price of 0.78
-// without the half took, 48 were slower than one after the other, by up to 23 %; this
-// takes 237 of them and none that is more than 1 % slower (of 300 others one, by 2.8 %),
-// and gives up 3 % and more of 114.  One after the other and in one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8;
-// 2048^3 39.4 / 34.0; 2880 x 256 x 1664 31.9 / 23.4; 3200 x 576 x 2688 42.2 / 34.6; 2176 x
-// 3904 x 448 39.8 / 26.5.  And not: 18,176 x 512 x 7936 305 / 374; 29,440 x 2560 x 1408
-// 364 / 431; 14,336 x 2944 x 5120 641 / 745; 1600 x 2368 x 1856 40.5 / 44.6; given up: 1152
-// x 1792 x 3840 43.9 / 41.5, 4096 x 2048 x 2048 69 / 63, 65,536 x 512 x 512 111 / 94.
+// Contraction steps of the fullest CU, three for a workgroup's start and end: the longer
+// workgroups first, in turn, and each of the others where most is free.
+int64_t fullest(int64_t blocks_l, int64_t steps_l, int64_t blocks_s, int64_t steps_s) {
+  constexpr int64_t kCus = 256;
+  const int64_t longer = steps_l + 3, shorter = steps_s + 3, each = blocks_l / kCus, rest = blocks_l % kCus;
+  const int64_t low = each * longer, high = low + (rest ? longer : 0);
+  // shorter ones that are done by then
+  auto takes = [&](int64_t t) {
+    return (kCus - rest) * std::max<int64_t>(0, (t - low) / shorter) + rest * std::max<int64_t>(0, (t - high) / shorter);
+  };
+  if (takes(high) >= blocks_s) return high;
+  const int64_t mean = (blocks_l * longer + blocks_s * shorter) / kCus;
+  auto from = [&](int64_t at) {   // in whole ones above it, at least to the mean: one or two tries
+    int64_t t = at + std::max<int64_t>(0, (mean - at + shorter - 1) / shorter) * shorter;
+    while (takes(t) < blocks_s) t += shorter;
+    return t;
+  };
+  return std::max(high, std::min(from(low), from(high)));
+}
+
+// A CU with two workgroups of both kinds takes half a microsecond a step of either, and a
+// second launch three.  Of 719 random sizes up to 65,600 x 5200 x 5200, all of which a price
+// of 0.78 us for a step of two (that of one kind alone) and full CUs took, 84 were slower
+// in one launch than one after the other, by up to 23 %; this takes 498 of them, of which
+// four are, by 1.6 to 3.1 % (of 220 others none by 1 %), and gives up 3 % and more of 109.  One after the other and in
+// one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8; 2048^3 39.4 / 34.0; 2880 x 256 x 1664
+// 31.9 / 23.4; 2176 x 3904 x 448 39.8 / 26.5; 1152 x 1792 x 3840 43.9 / 41.5; 20,000 x 1024 x
+// 1024 99 / 89.  And not: 18,176 x 512 x 7936 305 / 374; 29,440 x 2560 x 1408 364 / 431;
+// 14,336 x 2944 x 5120 641 / 745; 1600 x 2368 x 1856 40.5 / 44.6; given up: 4096 x 2048 x 2048
+// 69 / 63, 65,536 x 512 x 512 111 / 94.
 bool pair_gemms(int64_t mx, int64_t nx, const GemmPlan &x, int64_t mw, int64_t nw, const GemmPlan &w) {
-  const Shape &two = shapes[1], &one = shapes[2];
-  constexpr double kMixedStep = 0.9;
+  const Shape &two = shapes[1];
+  constexpr double kMixedStep = 0.5, kLaunch = 3.0;
   auto blocks = [&](int64_t m, int64_t n, const GemmPlan &p) {
     return (m + two.bm - 1) / two.bm * ((n + two.bn - 1) / two.bn) * p.splits;
   };
-  auto us = [](double step_us, double fixed_us, int64_t steps) { return double(steps) * step_us + fixed_us; };
   const int64_t bx = blocks(mx, nx, x), bw = blocks(mw, nw, w);
-  const double tx = us(kMixedStep, two.fixed_us, x.steps), tw = us(kMixedStep, two.fixed_us, w.steps);
-  const double all = (double(bx) * tx + double(bw) * tw) / double(two.slots) + (bx + bw > two.slots ? std::min(tx, tw) / 2 : 0.0);
-  const double alone = us(one.step_us, one.fixed_us, std::max(x.steps, w.steps));
-  return bx + bw < kMaxTiles && std::max(all, alone) <= x.us + w.us;
+  if (bx + bw >= kMaxTiles) return false;
+  const int64_t steps = x.steps >= w.steps ? fullest(bx, x.steps, bw, w.steps) : fullest(bw, w.steps, bx, x.steps);
+  return kMixedStep * double(steps) <= x.us + w.us + kLaunch;
 }
 
 hipError_t launch_gemm_pair(int dtype, const Gemm &x, const Gemm &w, hipStream_t stream) {
