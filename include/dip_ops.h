@@ -231,8 +231,7 @@ int dip_linear_kept(const dip_linear_args *a, const dip_packed8 *pre, void *stre
 /* dip_linear_grad from activations kept in 8 bits: x is x_act of the kept matrix,
  * rounded to the type (where act rounds g too, x_act's values are taken as two of the
  * type, so that one of dw's factors is rounded), and slopes are those at the kept pre.
- * Either may be null: then
- * a->x (x_act not used) or a->pre is read. */
+ * Either may be null: then a->x (x_act not used) or a->pre is read. */
 int64_t dip_linear_grad_kept_workspace(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act,
                                        const dip_packed8 *pre);
 int dip_linear_grad_kept(const dip_linear_grad_args *a, const dip_packed8 *x, int32_t x_act, const dip_packed8 *pre,
@@ -300,11 +299,10 @@ int dip_rms_norm_grad(const dip_rms_norm_grad_args *a, void *stream);
  * the gradient), (a, b) to (a cos - b sin, a sin + b cos).  Pair j is elements
  * j and pairs + j of the head, or with interleaved != 0 2 j and 2 j + 1; elements from
  * 2 pairs on are copied.  Angles are float64, and so their sines and cosines up to one
- * rounding to float32.  A pair whose
- * axis is not one of the axes stays as it is.  k with its heads goes along where
- * keys > 0.  Strides in elements, up to 2^46: st between tokens, sh between heads, in
- * either order; pos st and sa between tokens and axes.  An output may be its input
- * itself (same pointer and strides). */
+ * rounding to float32.  A pair whose axis is not one of the axes stays as it is.  k with
+ * its heads goes along where keys > 0.  Strides in elements, up to 2^46: st between
+ * tokens, sh between heads, in either order; pos st and sa between tokens and axes.  An
+ * output may be its input itself (same pointer and strides). */
 typedef struct {
   int64_t t;                 /* tokens                                          */
   int32_t heads, keys;       /* heads of q and of k, up to 65,536 together      */

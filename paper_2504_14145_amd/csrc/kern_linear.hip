@@ -775,7 +775,7 @@ hipError_t launch_gemm(int dtype, int64_t m, int64_t n, int64_t k, const Operand
 
 // Contraction steps of the fullest CU, three for a workgroup's start and end: the longer
 // workgroups first, in turn, and each of the others where most is free.
-int64_t fullest(int64_t blocks_l, int64_t steps_l, int64_t blocks_s, int64_t steps_s) {
+static int64_t fullest(int64_t blocks_l, int64_t steps_l, int64_t blocks_s, int64_t steps_s) {
   constexpr int64_t kCus = 256;
   const int64_t longer = steps_l + 3, shorter = steps_s + 3, each = blocks_l / kCus, rest = blocks_l % kCus;
   const int64_t low = each * longer, high = low + (rest ? longer : 0);
@@ -797,12 +797,12 @@ int64_t fullest(int64_t blocks_l, int64_t steps_l, int64_t blocks_s, int64_t ste
 // second launch three.  Of 719 random sizes up to 65,600 x 5200 x 5200, all of which a price
 // of 0.78 us for a step of two (that of one kind alone) and full CUs took, 84 were slower
 // in one launch than one after the other, by up to 23 %; this takes 498 of them, of which
-// four are, by 1.6 to 3.1 % (of 220 others none by 1 %), and gives up 3 % and more of 109.  One after the other and in
-// one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8; 2048^3 39.4 / 34.0; 2880 x 256 x 1664
-// 31.9 / 23.4; 2176 x 3904 x 448 39.8 / 26.5; 1152 x 1792 x 3840 43.9 / 41.5; 20,000 x 1024 x
-// 1024 99 / 89.  And not: 18,176 x 512 x 7936 305 / 374; 29,440 x 2560 x 1408 364 / 431;
-// 14,336 x 2944 x 5120 641 / 745; 1600 x 2368 x 1856 40.5 / 44.6; given up: 4096 x 2048 x 2048
-// 69 / 63, 65,536 x 512 x 512 111 / 94.
+// four are, by 1.6 to 3.1 % (of 220 others none by 1 %), and gives up 3 % and more of 109.
+// One after the other and in one launch, us, m x k x n in bf16: 512^3 15.6 / 7.8; 2048^3
+// 39.4 / 34.0; 2880 x 256 x 1664 31.9 / 23.4; 2176 x 3904 x 448 39.8 / 26.5; 1152 x 1792 x
+// 3840 43.9 / 41.5; 20,000 x 1024 x 1024 99 / 89.  And not: 18,176 x 512 x 7936 305 / 374;
+// 29,440 x 2560 x 1408 364 / 431; 14,336 x 2944 x 5120 641 / 745; 1600 x 2368 x 1856 40.5 /
+// 44.6; given up: 4096 x 2048 x 2048 69 / 63, 65,536 x 512 x 512 111 / 94.
 bool pair_gemms(int64_t mx, int64_t nx, const GemmPlan &x, int64_t mw, int64_t nw, const GemmPlan &w) {
   const Shape &two = shapes[1];
   constexpr double kMixedStep = 0.5, kLaunch = 3.0;
